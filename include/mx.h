@@ -369,6 +369,96 @@ MX_API mx_status mx_linear_static_workspace(const float* x, int64_t M, int64_t K
                                      const void* B_packed, int64_t N, mx_format fb, int32_t layout,
                                      float* Y, int64_t ldy, void* stream);
 
+/*
+ * Paged key/value cache: what a serving program keeps between the steps of a decoder, next to the packed weights.
+ *
+ * A cache is a pool of pages; a page holds `page` consecutive tokens of one request for every key/value head.  Keys and
+ * values are two arrays of the same geometry, data [pages][heads][page][dim]: the tokens of a page and head lie one after
+ * another, so attention streams them, and a page is free for any request.  With f.block = 0 an element is a bfloat16 number
+ * (exps is not used and may be null).  Otherwise the elements are MXInt with blocks of f.block along the head dimension (the
+ * axis the scores are reduced over; Section 3.2: an operator takes quantized inputs): data holds the mantissas, one byte each,
+ * exps [pages][heads][page][dim/f.block] the exponent bytes.  That is the canonical form of a (pages*heads*page) x dim tensor,
+ * so mx_dequantize reads a cache back.
+ * A slot is a token's place in the pool, page_index * page + place in the page.
+ * Built for page a power of two from 16 to 1024, dim a multiple of 16 up to 128, f.block 0, 16 or 32 (dividing dim),
+ * f.mant_bits 8, f.block_rows 1; pages * page must stay below 2^31.  Other legal requests are MX_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    int64_t pages;     /* pages of the pool */
+    int32_t page;      /* tokens per page */
+    int32_t heads;     /* key/value heads */
+    int32_t dim;       /* head dimension */
+    mx_format f;       /* format of the elements; block 0: bfloat16 */
+} mx_cache;
+
+enum { MX_F32 = 0, MX_BF16 = 1 };  /* element type of activations where a call takes either */
+
+/* Bytes of the data / exponent array of the keys (the values need as many again); 0 on a cache that is refused. */
+MX_API size_t mx_cache_data_bytes(mx_cache c);
+MX_API size_t mx_cache_exps_bytes(mx_cache c);
+
+/*
+ * Block table, slots and positions of one step, from the requests' lengths, on the GPU (nothing comes back to the host).
+ * Request b has ctx_len[b] tokens cached and brings new_len[b] more (negative counts as 0); its row of `table`, `width` page
+ * indices, holds the pages of the cached ones.  In request order every request gets the pages it lacks,
+ * ceil((ctx+new)/page) - ceil(ctx/page), from free_pages[0 .. n_free), and they are entered in its row.
+ * A request is refused when its row is too short (it then claims nothing), or when it needs pages and the pages claimed up to
+ * and including it exceed n_free; later requests that need pages are then refused too, others are served.  A refused request's
+ * row stays as it is.
+ * Out: q_start[requests + 1], the running sum of new_len from 0: the place of a request's tokens in the packed token dimension
+ *   (it counts refused requests' tokens too; sums past 2^31 - 1 stay there); kv_len[requests] = ctx + new, 0 for a refused
+ *   request; for each of `tokens` packed tokens slots[t], its place in the pool, and positions[t], its position in its request,
+ *   both -1 for tokens of a refused request or past the last request's; counts[0] = pages taken from the head of free_pages,
+ *   counts[1] = requests refused.  positions and counts may be null.
+ * All arrays are int32, on the device, 4-byte aligned.  page: a power of two from 16 to 1024.  requests <= 16384, else
+ * MX_ERR_UNSUPPORTED.
+ */
+MX_API mx_status mx_cache_plan(const int32_t* ctx_len, const int32_t* new_len, int64_t requests, int32_t page,
+                               const int32_t* free_pages, int64_t n_free, int32_t* table, int64_t width, int64_t tokens,
+                               int32_t* q_start, int32_t* kv_len, int32_t* slots, int32_t* positions, int32_t* counts,
+                               void* stream);
+
+/*
+ * Writes the keys and values of `tokens` tokens into their slots: k and v of element type `type` (MX_F32, MX_BF16), token t's
+ * element (head, d) at k[t*ldk + head*dim + d], ldk, ldv >= heads*dim (so k and v may be slices of one fused projection).  An
+ * element becomes the nearest bfloat16 (ties to even), or the block becomes what mx_quantize makes of it (the same bits).
+ * A token whose slot lies outside [0, pages*page) is skipped.  Two tokens with one slot: either of them.
+ * k and v aligned to their elements (16-byte aligned rows are read faster), cache arrays 16-byte aligned; *_exps may be null
+ * when f.block is 0.
+ */
+MX_API mx_status mx_cache_append(const void* k, const void* v, int32_t type, int64_t tokens, int64_t ldk, int64_t ldv,
+                                 mx_cache c, void* k_data, uint8_t* k_exps, void* v_data, uint8_t* v_exps,
+                                 const int32_t* slots, void* stream);
+
+/*
+ * Causal attention of the requests' new tokens over their pages, grouped heads: request b's new tokens are
+ * q_start[b] .. q_start[b+1]-1 of the packed tokens, and its cache (the new ones included) holds kv_len[b] tokens in the pages
+ * of its row of `table`.  For new token i of n and query head a, with key/value head a / (heads_q / heads):
+ *     o = sum_j p_j v_j,  p = softmax(scale * q . k_j)  over the positions j <= kv_len[b] - n + i.
+ * One new token is decoding, kv_len[b] = n a whole prompt, anything between a chunk.  A token that sees no key (kv_len[b] < n,
+ * as for a request that mx_cache_plan refused, or a token outside every request) gives zeros.
+ * q, out: element type `type`, element (t, a, d) at q[t*ldq + a*dim + d], out[t*ldo + a*dim + d]; aligned to their elements.
+ * Every q, k and v of a position that a request holds must be finite; what lies in a page past kv_len[b] may be anything.
+ * Page indices outside the pool and lengths past the table row do not fault: such a page reads as page 0, such a length counts
+ * as width * page; q_start is clamped to [0, tokens].
+ * max_new, max_len: bounds on the requests' new tokens and lengths as the host knows them.  They only shape the launch: the
+ * result is right for any positive values.
+ * Numerics: products of the exact inputs, scores, softmax statistics and sums in fp32; the probabilities enter
+ * the second product with 16 bits (MX_BF16) or, like q, 24 bits (MX_F32).  Same inputs, same bits.  Cached values and
+ * probabilities below 2^-126 may count as zero.
+ * workspace: mx_cache_attention_workspace_bytes(...) bytes for the same arguments, 256-byte aligned, caller-owned; its first
+ *   65536 bytes must be zero when the call starts and are zero again afterwards, the rest needs no initial value.  Calls that
+ *   may overlap in time need a workspace each.
+ * heads_q a multiple of c.heads; requests <= 16384, else MX_ERR_UNSUPPORTED.
+ */
+MX_API size_t mx_cache_attention_workspace_bytes(mx_cache c, int64_t tokens, int64_t requests, int32_t heads_q,
+                                                 int64_t max_new, int64_t max_len);
+MX_API mx_status mx_cache_attention(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32_t heads_q, mx_cache c,
+                                    const void* k_data, const uint8_t* k_exps, const void* v_data, const uint8_t* v_exps,
+                                    const int32_t* table, int64_t width, const int32_t* q_start, const int32_t* kv_len,
+                                    int64_t requests, int64_t max_new, int64_t max_len, float scale, void* workspace,
+                                    void* out, int64_t ldo, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,13 +19,15 @@ MX_RNE, MX_RTZ = 0, 1
 MX_OK, MX_ERR_BAD_ARG, MX_ERR_UNSUPPORTED, MX_ERR_DEVICE = 0, 1, 2, 3
 MX_LAYOUT_FRAGMENT = 0
 MX_LAYOUT_MATRIX = 1
+MX_F32, MX_BF16 = 0, 1
 
 EXPORTS = ("mx_version", "mx_status_string", "mx_mant_bytes", "mx_exps_bytes", "mx_quantize", "mx_check_finite",
            "mx_dequantize", "mx_cast", "mx_packed_bytes", "mx_pack", "mx_quantize_pack", "mx_quantize_pack_axis0", "mx_unpack",
            "mx_gemm",
            "mx_gemm_q", "mx_attention", "mx_linear", "mx_linear_workspace_bytes", "mx_linear_static_workspace",
            "mx_linear_static_workspace_max", "mx_quantize_minifloat",
-           "mx_dequantize_minifloat")
+           "mx_dequantize_minifloat", "mx_cache_data_bytes", "mx_cache_exps_bytes", "mx_cache_plan", "mx_cache_append",
+           "mx_cache_attention_workspace_bytes", "mx_cache_attention")
 
 
 class mx_format(ctypes.Structure):
@@ -46,6 +48,17 @@ class mx_minifloat_format(ctypes.Structure):
     """Mirror of the C struct of the Block Minifloat / Block Logarithm formats: block, exp_bits, mant_bits, rounding."""
     _fields_ = [("block", ctypes.c_int32), ("exp_bits", ctypes.c_int32), ("mant_bits", ctypes.c_int32),
                 ("rounding", ctypes.c_int32)]
+
+
+class mx_cache(ctypes.Structure):
+    """Mirror of the C struct of a paged key/value cache: pages, page, heads, dim, f (block 0: bfloat16 elements)."""
+    _fields_ = [("pages", ctypes.c_int64), ("page", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("f", mx_format)]
+
+
+def cache_format(pages: int, page: int, heads: int, dim: int, f: Optional[mx_format] = None) -> mx_cache:
+    """A cache of `pages` pages of `page` tokens in MXInt format f, or of bfloat16 elements without one."""
+    return mx_cache(pages, page, heads, dim, f if f is not None else fmt(0, 8))
 
 
 class MxError(RuntimeError):
@@ -92,6 +105,16 @@ def load() -> ctypes.CDLL:
     lib.mx_linear_static_workspace.argtypes = [vp, i64, i64, i64, mx_format, vp, i64, mx_format, i32, vp, i64, vp]
     lib.mx_linear_static_workspace.restype = i32
     lib.mx_linear_static_workspace_max.argtypes, lib.mx_linear_static_workspace_max.restype = [], sz
+    for name in ("mx_cache_data_bytes", "mx_cache_exps_bytes"):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = [mx_cache], sz
+    lib.mx_cache_plan.argtypes = [vp, vp, i64, i32, vp, i64, vp, i64, i64, vp, vp, vp, vp, vp, vp]
+    lib.mx_cache_append.argtypes = [vp, vp, i32, i64, i64, i64, mx_cache, vp, vp, vp, vp, vp, vp]
+    lib.mx_cache_attention_workspace_bytes.argtypes = [mx_cache, i64, i64, i32, i64, i64]
+    lib.mx_cache_attention_workspace_bytes.restype = sz
+    lib.mx_cache_attention.argtypes = [vp, i32, i64, i64, i32, mx_cache, vp, vp, vp, vp, vp, i64, vp, vp, i64, i64, i64,
+                                       ctypes.c_float, vp, vp, i64, vp]
+    for name in ("mx_cache_plan", "mx_cache_append", "mx_cache_attention"):
+        getattr(lib, name).restype = i32
     for name in ("mx_quantize", "mx_dequantize", "mx_cast", "mx_pack", "mx_quantize_pack", "mx_quantize_pack_axis0",
                  "mx_unpack", "mx_gemm",
                  "mx_gemm_q", "mx_attention", "mx_linear", "mx_quantize_minifloat", "mx_dequantize_minifloat"):
@@ -272,6 +295,57 @@ def mx_linear_static_workspace_max() -> int:
     return int(load().mx_linear_static_workspace_max())
 
 
+# The calls of a serving step run many times a second on few tokens, so their pointers go to ctypes as plain integers: an
+# object per pointer costs as much as a small kernel runs.
+def _at(t):
+    return t.data_ptr() if isinstance(t, torch.Tensor) else t
+
+
+def _raw_stream(stream):
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else _stream(stream)
+
+
+def mx_cache_data_bytes(c: mx_cache) -> int:
+    return int(load().mx_cache_data_bytes(c))
+
+
+def mx_cache_exps_bytes(c: mx_cache) -> int:
+    return int(load().mx_cache_exps_bytes(c))
+
+
+def mx_cache_plan(ctx_len, new_len, requests, page, free_pages, n_free, table, width, tokens, q_start, kv_len, slots,
+                  positions, counts, stream=None, check: bool = True) -> int:
+    s = load().mx_cache_plan(_at(ctx_len), _at(new_len), requests, page, _at(free_pages), n_free, _at(table), width, tokens,
+                             _at(q_start), _at(kv_len), _at(slots), _at(positions), _at(counts), _raw_stream(stream))
+    if check:
+        _raise(s, "mx_cache_plan")
+    return s
+
+
+def mx_cache_append(k, v, type, tokens, ldk, ldv, c, k_data, k_exps, v_data, v_exps, slots, stream=None,
+                    check: bool = True) -> int:
+    s = load().mx_cache_append(_at(k), _at(v), type, tokens, ldk, ldv, c, _at(k_data), _at(k_exps), _at(v_data), _at(v_exps),
+                               _at(slots), _raw_stream(stream))
+    if check:
+        _raise(s, "mx_cache_append")
+    return s
+
+
+def mx_cache_attention_workspace_bytes(c: mx_cache, tokens: int, requests: int, heads_q: int, max_new: int,
+                                       max_len: int) -> int:
+    return int(load().mx_cache_attention_workspace_bytes(c, tokens, requests, heads_q, max_new, max_len))
+
+
+def mx_cache_attention(q, type, tokens, ldq, heads_q, c, k_data, k_exps, v_data, v_exps, table, width, q_start, kv_len,
+                       requests, max_new, max_len, scale, workspace, out, ldo, stream=None, check: bool = True) -> int:
+    s = load().mx_cache_attention(_at(q), type, tokens, ldq, heads_q, c, _at(k_data), _at(k_exps), _at(v_data), _at(v_exps),
+                                  _at(table), width, _at(q_start), _at(kv_len), requests, max_new, max_len, scale,
+                                  _at(workspace), _at(out), ldo, _raw_stream(stream))
+    if check:
+        _raise(s, "mx_cache_attention")
+    return s
+
+
 def bound(name: str, *args, stream=None):
     """Marshal the arguments of entry point ``name`` once and return a zero-argument callable that
     issues exactly that call again (status checked).  For loops that launch the same call many times:
@@ -381,4 +455,69 @@ def gemm(A_packed: torch.Tensor, fa: mx_format, B_packed: torch.Tensor, fb: mx_f
     if out is None:
         out = torch.empty((batch, M, N), dtype=torch.float32, device=A_packed.device)
     mx_gemm(batch, M, N, K, A_packed, fa, B_packed, fb, layout, out, N, M * N)
+    return out
+
+
+class Cache:
+    """The arrays of a paged key/value cache and their description ``c``; every place starts as zeros."""
+
+    def __init__(self, pages: int, page: int, heads: int, dim: int, f: Optional[mx_format] = None, device="cuda"):
+        self.c = cache_format(pages, page, heads, dim, f)
+        n, e = mx_cache_data_bytes(self.c), mx_cache_exps_bytes(self.c)
+        if n == 0:
+            raise MxError(MX_ERR_UNSUPPORTED, "cache of %d pages of %d tokens, %d heads of %d" % (pages, page, heads, dim))
+        self.k, self.v = (torch.zeros(n, dtype=torch.uint8, device=device) for _ in range(2))
+        self.k_exps, self.v_exps = (torch.zeros(e, dtype=torch.uint8, device=device) if e else None for _ in range(2))
+
+
+def _activation_type(x: torch.Tensor) -> int:
+    if x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda or x.stride(-1) != 1:
+        raise ValueError("float32 or bfloat16 rows on the GPU are wanted")
+    return MX_F32 if x.dtype == torch.float32 else MX_BF16
+
+
+def cache_plan(ctx_len: torch.Tensor, new_len: torch.Tensor, page: int, free_pages: torch.Tensor, table: torch.Tensor,
+               tokens: int) -> Tuple[torch.Tensor, ...]:
+    """(q_start, kv_len, slots, positions, counts) of a step; ``table`` [requests, width] receives the new pages."""
+    assert table.dim() == 2 and table.is_contiguous() and ctx_len.numel() == new_len.numel() == table.shape[0]
+    for t in (ctx_len, new_len, free_pages, table):
+        assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()
+    q_start, kv_len, slots, positions, counts = (
+        torch.empty(n, dtype=torch.int32, device=table.device) for n in (table.shape[0] + 1, table.shape[0], tokens, tokens, 2))
+    mx_cache_plan(ctx_len, new_len, table.shape[0], page, free_pages, free_pages.numel(), table, table.shape[1], tokens, q_start,
+                  kv_len, slots, positions, counts)
+    return q_start, kv_len, slots, positions, counts
+
+
+def cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+    """k, v: [tokens, heads*dim], float32 or bfloat16, contiguous along the last axis (slices of a projection will do)."""
+    assert k.shape == v.shape and k.shape[1] == cache.c.heads * cache.c.dim and k.dtype == v.dtype and slots.numel() == k.shape[0]
+    assert slots.dtype == torch.int32 and v.is_cuda and v.stride(-1) == 1
+    mx_cache_append(k, v, _activation_type(k), k.shape[0], k.stride(0), v.stride(0), cache.c, cache.k, cache.k_exps, cache.v,
+                    cache.v_exps, slots)
+
+
+def cache_workspace(c: mx_cache, tokens: int, requests: int, heads_q: int, max_new: int, max_len: int, device) -> torch.Tensor:
+    """A zero-filled workspace for mx_cache_attention (its counters must be zero before the first call)."""
+    return torch.zeros(max(1, mx_cache_attention_workspace_bytes(c, tokens, requests, heads_q, max_new, max_len)),
+                       dtype=torch.uint8, device=device)
+
+
+def cache_attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int,
+                    max_len: int, scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q: [tokens, heads_q*dim]; scale: 1/sqrt(dim) unless given.  Returns [tokens, heads_q*dim] in the type of q."""
+    dim, requests = cache.c.dim, table.shape[0]
+    assert table.dim() == 2 and table.is_contiguous() and q_start.numel() == requests + 1 and kv_len.numel() == requests
+    for t in (table, q_start, kv_len):
+        assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()
+    heads_q = q.shape[1] // dim
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype and out.stride(-1) == 1 and q.shape[1] == heads_q * dim
+    if workspace is None:
+        workspace = cache_workspace(cache.c, q.shape[0], requests, heads_q, max_new, max_len, q.device)
+    mx_cache_attention(q, _activation_type(q), q.shape[0], q.stride(0), heads_q, cache.c, cache.k, cache.k_exps, cache.v,
+                       cache.v_exps, table, table.shape[1], q_start, kv_len, requests, max_new, max_len,
+                       dim ** -0.5 if scale is None else scale, workspace, out, out.stride(0))
     return out
