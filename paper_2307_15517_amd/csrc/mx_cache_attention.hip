@@ -1,4 +1,6 @@
 // Attention of new tokens over the paged key/value cache, causal, grouped heads.
+#include <type_traits>
+
 #include "mx_cache.h"
 
 namespace mx {
@@ -94,13 +96,28 @@ __device__ __forceinline__ void store_out(const CacheAttnArgs& a, int64_t at, co
     }
 }
 
-// The row of a pool that holds key `key` of a request (and the ones after it in its page): a page index outside the pool
-// reads as page 0.  `key` is below the request's length and the same for all lanes, so the index comes by a scalar load.
-__device__ __forceinline__ int64_t pool_row(const CacheAttnArgs& a, const int32_t* row_table, int h, int key) {
-    uint32_t id = (uint32_t)row_table[key >> a.page_log2];
-    id = id < a.pages ? id : 0;
-    return (((int64_t)id * a.heads + h) << a.page_log2) + (key & ((1 << a.page_log2) - 1));
-}
+// The pages of one request as a wave walks over its keys: 64 entries of the table row at a time, one per lane, so that a step
+// finds its pages without a load (a scalar load among LDS reads makes every wait for one of them a wait for all).
+struct PageWindow {
+    const int32_t* row_table;
+    int base, last, id;        // id: of page `base` + lane, no further than `last`
+
+    __device__ __forceinline__ PageWindow(const CacheAttnArgs& a, int b, int len)
+        : row_table(a.table + (int64_t)b * a.width), base(-64), last((len - 1) >> a.page_log2), id(0) {}
+    // The row of the pool that holds key `key` of the request (and those after it in its run of sixteen): `key` is below its
+    // length and the same for all lanes.  A page index outside the pool reads as page 0.
+    __device__ __forceinline__ int64_t row(const CacheAttnArgs& a, int h, int key) {
+        const int page = key >> a.page_log2;
+        if (page - base >= 64) {
+            base = page;
+            id = row_table[min(page + (int)(threadIdx.x & 63), last)];
+            asm volatile("" : "+v"(id));       // awaited here, once in 64 pages, and not wherever it might just have been loaded
+        }
+        uint32_t at = (uint32_t)__builtin_amdgcn_readlane(id, page - base);
+        at = at < a.pages ? at : 0;
+        return (((int64_t)at * a.heads + h) << a.page_log2) + (key & ((1 << a.page_log2) - 1));
+    }
+};
 
 template <int TYPE>
 __device__ __forceinline__ void load_q(const CacheAttnArgs& a, int64_t at, float (&v)[8]) {
@@ -193,7 +210,6 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
     // this split's run of keys, in whole blocks of 128
     const int per = (((len + 127) >> 7) + splits - 1) / splits;
     const int begin = min(split * per * 128, len), end = min(begin + per * 128, len);
-    const int32_t* row_table = a.table + (int64_t)b * a.width;
     const int dim = a.dim;
 
     for (int r0 = 0; r0 < rows; r0 += 16) {
@@ -227,10 +243,11 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
         // The two runs of sixteen keys of a block lie in one page each; a run past the end reads the last one again (masked).
         // A block's loads are issued while the one before is computed on; there is one past the end, so that no load is conditional.
         const int last_run = (len - 1) & ~15;
-        auto load = [&](Block& f, int kb) {
+        PageWindow pages(a, b, len);
+        auto load = [&](Block& f, int kb) __attribute__((always_inline)) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const int64_t row = pool_row(a, row_table, h, min(kb + 16 * t, last_run));
+                const int64_t row = pages.row(a, h, min(kb + 16 * t, last_run));
                 const uint8_t* kp = a.k + row * dim * EB;
                 const uint8_t* vp = a.v + row * dim * EB;
                 if constexpr (BLOCK == 0) {
@@ -267,7 +284,7 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
                 }
             }
         };
-        auto compute = [&](Block& f, int kb) {
+        auto compute = [&](Block& f, int kb) __attribute__((always_inline)) {
             v4f s[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -479,6 +496,17 @@ __device__ __forceinline__ int v_place(int key, int chunk) {
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 
+// 16 bytes per lane from memory straight into LDS: lane L's bytes land at lds_addr + 16 L.  Awaited with s_waitcnt vmcnt.
+__device__ __forceinline__ void copy16_to_lds(const uint8_t* uniform_src, uint32_t lane_offset, uint32_t lds_addr) {
+    asm volatile(
+        "s_mov_b32 m0, %2\n\t"
+        "s_nop 0\n\t"
+        "global_load_lds_dwordx4 %0, %1\n\t"
+        :
+        : "v"(lane_offset), "s"(uniform_src), "s"(lds_addr)
+        : "memory", "m0");
+}
+
 // Four keys (rows of V in LDS) of one column per lane: lane l of sixteen gives the place of row l/4, columns 4(l%4).. and
 // receives column l of the four rows.
 __device__ __forceinline__ v2u read_transposed(const uint8_t* p) {
@@ -492,9 +520,7 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
     constexpr int KT = kTileKeys<TYPE>, NT = KT / 32, NK = DT / 16, ND = DT / 32;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
     constexpr int kTensor = KT * DT * 2, kStage = 2 * kTensor;
-    // staging: 16 bytes of the pool per thread and pass
-    constexpr int kPer = 16 / EB, kLanes = DT / kPer, kRows = 256 / kLanes < KT ? 256 / kLanes : KT, kPasses = KT / kRows;
-    constexpr int kStagers = kRows * kLanes;      // threads that stage; waves past them compute only
+    constexpr int kPer = 16, kLanes = DT / kPer;       // MXInt staging: sixteen elements per lane
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int i = lane & 31, h2 = lane >> 5;
@@ -519,7 +545,6 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
     const Request rq = request_of(a, b);
     const int rows = rq.n * a.group, r0 = tile.index * kTileRows;
     const int len = rq.len, dim = a.dim;
-    const int32_t* row_table = a.table + (int64_t)b * a.width;
 
     // the keys that some row of the tile sees, and this split's run of them in whole tiles
     const int all = max(0, len - rq.n + min(r0 + kTileRows - 1, rows - 1) / a.group + 1);
@@ -547,57 +572,97 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
         }
     }
 
-    // staging
-    v4u sk[kPasses], sv[kPasses];
-    int ek[kPasses], ev[kPasses];
-    const int srow = threadIdx.x / kLanes, schunk = threadIdx.x % kLanes;
-    const int srow0 = __builtin_amdgcn_readfirstlane(srow);               // the rows of a wave's pass lie in one page
-    const int sd = schunk * kPer;
-    auto load = [&](int kb) {
+    // Staging.  bfloat16: copies from memory straight to LDS, 1 KiB (whole rows) per wave and instruction, lane L's bytes at
+    // 16 L of it, so the placement of the chunks is done by what each lane reads.  MXInt: through registers.
+    const int last_run = (len - 1) & ~15;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
+    constexpr int kPieceRows = BLOCK == 0 ? 512 / DT : 64 / kLanes;       // rows of a wave's piece, within a run of sixteen
+    constexpr int kPieces = KT / (4 * kPieceRows) > 0 ? KT / (4 * kPieceRows) : 1;
+    const int rel = BLOCK == 0 ? lane / (DT / 8) : lane / kLanes;         // this lane's row of the piece
+    uint32_t k_from = 0, v_from = 0;                                      // and the place of what it reads in there
+    {
+        const int row = kPieceRows * wave + rel;                          // the pieces are 4 * kPieceRows rows apart: no matter here
+        if constexpr (BLOCK == 0) {
+            const int chunk = lane % (DT / 8);
+            const int kc = (k_place<DT>(row, chunk) - row * DT * 2) >> 4, vc = (v_place<DT>(row, chunk) - row * DT * 2) >> 4;
+            k_from = (rel * dim + (8 * kc < dim ? 8 * kc : 0)) * 2;
+            v_from = (rel * dim + (8 * vc < dim ? 8 * vc : 0)) * 2;
+        } else {
+            const int d = (lane % kLanes) * kPer;
+            k_from = v_from = rel * dim + (d < dim ? d : 0);
+        }
+    }
+    const uint32_t e_from = BLOCK == 0 ? 0 : rel * (dim / (BLOCK == 0 ? 1 : BLOCK)) + (k_from - rel * dim) / (BLOCK == 0 ? 1 : BLOCK);
+    v4u sk[BLOCK == 0 ? 1 : kPieces], sv[BLOCK == 0 ? 1 : kPieces];
+    int ek[BLOCK == 0 ? 1 : kPieces], ev[BLOCK == 0 ? 1 : kPieces];
+    PageWindow pages(a, b, len);
+    const bool stages = 4 * kPieceRows <= KT || wave < KT / kPieceRows;   // with few keys per tile some waves have none to bring
+    auto load = [&](uint32_t stage, int kb) __attribute__((always_inline)) {
+        if (!stages) return;
 #pragma unroll
-        for (int u = 0; u < kPasses; ++u) {
-            const int key0 = kb + u * kRows + srow0;
-            const int64_t row = pool_row(a, row_table, h, min(key0, len - 1)) - (min(key0, len - 1) & 15) + ((u * kRows + srow0) & 15);
-            const int rel = srow - srow0, d = sd < dim ? sd : 0;
-            sk[u] = *reinterpret_cast<const v4u*>(a.k + row * dim * EB + (rel * dim + d) * EB);
-            sv[u] = *reinterpret_cast<const v4u*>(a.v + row * dim * EB + (rel * dim + d) * EB);
-            if constexpr (BLOCK != 0) {
-                ek[u] = (a.k_exps + row * (dim / BLOCK))[rel * (dim / BLOCK) + d / BLOCK];
-                ev[u] = (a.v_exps + row * (dim / BLOCK))[rel * (dim / BLOCK) + d / BLOCK];
+        for (int u = 0; u < kPieces; ++u) {
+            const int key = kb + (4 * u + wave) * kPieceRows, run = min(key & ~15, last_run);
+            const int64_t row = pages.row(a, h, run) + (key & 15);
+            const uint8_t* kp = a.k + row * dim * EB;
+            const uint8_t* vp = a.v + row * dim * EB;
+            if constexpr (BLOCK == 0) {
+                const uint32_t to = lds0 + stage + (4 * u + wave) * 1024;
+                copy16_to_lds(kp, k_from, to);
+                copy16_to_lds(vp, v_from, to + kTensor);
+            } else {
+                sk[u] = *reinterpret_cast<const v4u*>(kp + k_from);
+                sv[u] = *reinterpret_cast<const v4u*>(vp + v_from);
+                ek[u] = (a.k_exps + row * (dim / BLOCK))[e_from];
+                ev[u] = (a.v_exps + row * (dim / BLOCK))[e_from];
             }
         }
     };
     auto widen = [&](const v4u& x, float sc, v4u (&y)[2]) {               // sixteen mantissas to bfloat16 numbers
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
-            const int t = (int)x[w >> 1];
+            int t = (int)x[w >> 1];
+            asm("" : "+v"(t));
             const float lo = (float)(int8_t)(t >> (16 * (w & 1))) * sc, hi = (float)(int8_t)(t >> (16 * (w & 1) + 8)) * sc;
             y[w >> 2][w & 3] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
         }
     };
-    auto store = [&](uint8_t* stage, int kb) {
-        if (kStagers < 256 && threadIdx.x >= kStagers) return;
+    // What lies past the request's end may be anything, NaN among it, and meets probabilities of zero: it becomes zeros.  (Past
+    // the head dimension lies a repetition; it meets zeros of q, or gives results that nobody reads.)
+    auto store = [&](uint8_t* stage, int kb) __attribute__((always_inline)) {
+        if constexpr (BLOCK != 0) {
+            if (!stages) return;
 #pragma unroll
-        for (int u = 0; u < kPasses; ++u) {
-            const int key = u * kRows + srow;
-            // what lies past the head dimension multiplies zeros of q, what lies past the request's end probabilities of zero:
-            // it must be finite
-            const bool in = sd < dim && kb + key < len;
-            if constexpr (BLOCK == 0) {
-                const v4u zero = {0, 0, 0, 0};
-                *reinterpret_cast<v4u*>(stage + k_place<DT>(key, schunk)) = in ? sk[u] : zero;
-                *reinterpret_cast<v4u*>(stage + kTensor + v_place<DT>(key, schunk)) = in ? sv[u] : zero;
-            } else {
+            for (int u = 0; u < kPieces; ++u) {
+                const int key = (4 * u + wave) * kPieceRows + rel, chunk = 2 * (lane % kLanes);
+                const bool in = kb + key < len;
                 v4u y[2];
                 widen(sk[u], in ? power2(ek[u] - a.exp_shift) : 0.f, y);
-                *reinterpret_cast<v4u*>(stage + k_place<DT>(key, 2 * schunk)) = y[0];
-                *reinterpret_cast<v4u*>(stage + k_place<DT>(key, 2 * schunk + 1)) = y[1];
+                *reinterpret_cast<v4u*>(stage + k_place<DT>(key, chunk)) = y[0];
+                *reinterpret_cast<v4u*>(stage + k_place<DT>(key, chunk + 1)) = y[1];
                 widen(sv[u], in ? power2(ev[u] - a.exp_shift) : 0.f, y);
-                *reinterpret_cast<v4u*>(stage + kTensor + v_place<DT>(key, 2 * schunk)) = y[0];
-                *reinterpret_cast<v4u*>(stage + kTensor + v_place<DT>(key, 2 * schunk + 1)) = y[1];
+                *reinterpret_cast<v4u*>(stage + kTensor + v_place<DT>(key, chunk)) = y[0];
+                *reinterpret_cast<v4u*>(stage + kTensor + v_place<DT>(key, chunk + 1)) = y[1];
             }
         }
     };
+    auto clear_past = [&](uint8_t* stage, int kb) __attribute__((always_inline)) {
+        if constexpr (BLOCK == 0) {
+            const int from = (len - kb) * DT * 2;                         // rows of the V tile lie one after another
+            const v4u zero = {0, 0, 0, 0};
+            for (int x = from + threadIdx.x * 16; x < kTensor; x += 4096) *reinterpret_cast<v4u*>(stage + kTensor + x) = zero;
+        }
+    };
+
+    // places of this lane's reads in a stage, without the multiples of eight keys that the instructions add
+    const uint8_t* k_at[NK];
+    const uint8_t* v_at[ND];
+#pragma unroll
+    for (int kk = 0; kk < NK; ++kk) k_at[kk] = smem + k_place<DT>(i, 2 * kk + h2);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt) {
+        const int d = 32 * dt + (lane & 16) + 4 * (lane & 3);
+        v_at[dt] = smem + kTensor + v_place<DT>(4 * h2 + ((lane & 15) >> 2), d >> 3) + (d & 7) * 2;
+    }
 
     float m = -__builtin_inff(), l = 0.f;
     v16f o[ND];
@@ -606,7 +671,8 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
 
-    auto compute = [&](const uint8_t* stage, int kb) {
+    auto compute = [&](auto stage_c, int kb) __attribute__((always_inline)) {
+        constexpr int stage = decltype(stage_c)::value * kStage;
         v16f s[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -614,13 +680,25 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
             for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
             for (int kk = 0; kk < NK; ++kk) {
-                const v4u kf = *reinterpret_cast<const v4u*>(stage + k_place<DT>(32 * t + i, 2 * kk + h2));
+                const v4u kf = *reinterpret_cast<const v4u*>(k_at[kk] + (stage + 32 * t * DT * 2));
 #pragma unroll
                 for (int p = QP - 1; p >= 0; --p)
                     s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, kf), __builtin_bit_cast(v8bf, qf[p][kk]), s[t],
                                                                    0, 0, 0);
             }
         }
+        v4u vf[2][ND];
+        auto read_v = [&](int step) __attribute__((always_inline)) {                                     // sixteen keys
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int jj = 0; jj < 2; ++jj) {
+                    const v2u x = read_transposed(v_at[dt] + (stage + (16 * step + 8 * jj) * DT * 2));
+                    vf[step & 1][dt][2 * jj] = x[0];
+                    vf[step & 1][dt][2 * jj + 1] = x[1];
+                }
+        };
+        read_v(0);
         // result register e of half t: key 32t + 8(e/4) + 4h2 + e%4
         if (kb + KT - 1 > min(first_last, wave_stop - 1)) {
 #pragma unroll
@@ -636,17 +714,19 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 16; ++e) top = __builtin_fmaxf(top, s[t][e]);
-        const float m_new = __builtin_fmaxf(m, max_across_32(top) * a.c);
-        const float m_use = m_new == -__builtin_inff() ? 0.f : m_new;
-        if (__any(m_new > m)) {
-            const float alpha = exp2_of(m - m_use);
+        top = max_across_32(top) * a.c;
+        // The sums are kept against a maximum that follows the rows' own within 2^8: the first tile sets it, few later ones move it.
+        if (__any(top > m + 8.f)) {
+            const float m_new = __builtin_fmaxf(m, top);
+            const float alpha = m_new == -__builtin_inff() ? 1.f : exp2_of(m - m_new);
+            m = m_new;
             l *= alpha;
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
         }
-        m = m_new;
+        const float m_use = m == -__builtin_inff() ? 0.f : m;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             float sum = 0.f;
@@ -657,7 +737,9 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
             }
             l += sum;
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {                        // sixteen keys
+            for (int half = 0; half < 2; ++half) {
+                const int step = 2 * t + half;
+                if (step + 1 < 2 * NT) read_v(step + 1);
                 v4u pf[P];
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -667,35 +749,37 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
                     for (int p = 0; p < P; ++p) pf[p][w] = x[p];
                 }
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt) {
-                    v4u vf;
+                for (int p = P - 1; p >= 0; --p)
 #pragma unroll
-                    for (int jj = 0; jj < 2; ++jj) {
-                        const int key = 32 * t + 16 * half + 8 * jj + 4 * h2 + ((lane & 15) >> 2);
-                        const int d = 32 * dt + (lane & 16) + 4 * (lane & 3);
-                        const v2u x = read_transposed(stage + kTensor + v_place<DT>(key, d >> 3) + (d & 7) * 2);
-                        vf[2 * jj] = x[0];
-                        vf[2 * jj + 1] = x[1];
-                    }
-#pragma unroll
-                    for (int p = P - 1; p >= 0; --p)
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, vf), __builtin_bit_cast(v8bf, pf[p]),
-                                                                        o[dt], 0, 0, 0);
-                }
+                    for (int dt = 0; dt < ND; ++dt)
+                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, vf[step & 1][dt]),
+                                                                        __builtin_bit_cast(v8bf, pf[p]), o[dt], 0, 0, 0);
             }
         }
     };
 
+    // A tile: its data is awaited and published, the next tile's is asked for, and, MXInt, put in place after the arithmetic.
+    auto step = [&](auto stage_c, int kb) __attribute__((always_inline)) {
+        constexpr int at = decltype(stage_c)::value * kStage, other = kStage - at;
+        if constexpr (BLOCK == 0) __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0): the copies
+        __syncthreads();                                                  // the tile is there, and the other stage has been read
+        if (BLOCK == 0 && kb + KT > len) {
+            clear_past(smem + at, kb);
+            __syncthreads();
+        }
+        const bool more = kb + KT < stop;
+        if (more) load(other, kb + KT);
+        if (kb < wave_stop) compute(stage_c, kb);
+        if (more) store(smem + other, kb + KT);
+    };
     if (begin < stop) {
-        load(begin);
+        load(0, begin);
         store(smem, begin);
-        int at = 0;
-        for (int kb = begin; kb < stop; kb += KT) {
-            __syncthreads();                          // the tile is there, and the other stage has been read
-            if (kb + KT < stop) load(kb + KT);
-            if (kb < wave_stop) compute(smem + at * kStage, kb);
-            if (kb + KT < stop) store(smem + (at ^ 1) * kStage, kb + KT);
-            at ^= 1;
+        for (int kb = begin;;) {
+            step(std::integral_constant<int, 0>{}, kb);
+            if ((kb += KT) >= stop) break;
+            step(std::integral_constant<int, 1>{}, kb);
+            if ((kb += KT) >= stop) break;
         }
     }
 
