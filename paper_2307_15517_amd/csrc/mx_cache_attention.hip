@@ -108,7 +108,7 @@ struct PageWindow {
     // length and the same for all lanes.  A page index outside the pool reads as page 0.
     __device__ __forceinline__ int64_t row(const CacheAttnArgs& a, int h, int key) {
         const int page = key >> a.page_log2;
-        if (page - base >= 64) {
+        if ((unsigned)(page - base) >= 64) {
             base = page;
             id = row_table[min(page + (int)(threadIdx.x & 63), last)];
             asm volatile("" : "+v"(id));       // awaited here, once in 64 pages, and not wherever it might just have been loaded
@@ -142,15 +142,26 @@ __device__ __forceinline__ void pieces_of(float a, float b, uint32_t (&w)[P]) {
     }
 }
 
+// The largest of three, or two; __builtin_fmaxf spends an instruction on every operand whose origin the compiler cannot see.
+__device__ __forceinline__ float max_of(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float max_of(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
 __device__ __forceinline__ float max_across_32(float v) {
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __builtin_fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    return max_of(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float max_across_16_32(float v) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __builtin_fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    v = max_of(__uint_as_float(a[0]), __uint_as_float(a[1]));
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return __builtin_fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+    return max_of(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 __device__ __forceinline__ float sum_across_16_32(float v) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -312,12 +323,12 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
                 }
             }
             if (kb + 31 > min(first_last, stop - 1)) {
+                const int seen = min(last, stop - 1) - kb - 4 * g;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int key = kb + 16 * t + 4 * g + e;
-                        s[t][e] = key <= last && key < stop ? s[t][e] : -__builtin_inff();
+                        s[t][e] = 16 * t + e <= seen ? s[t][e] : -__builtin_inff();
                     }
             }
             float top = -__builtin_inff();
@@ -443,14 +454,20 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
 
 // ---- many rows: chunks and prompts ----------------------------------------------------------------------
 // A workgroup takes 128 rows (token, head of the group) of one request and key/value head, a wave 32 of them, q in registers;
-// K and V pass through LDS in tiles of 64 (fp32: 32) keys as bfloat16 (MXInt elements become that on the way, exactly), two stages, so
-// that a tile's loads run under the arithmetic on the one before.  S^T = K Q^T puts a row in a lane's column, so that its
-// maximum and sum take one exchange between the lane halves, and hands the probabilities to O^T = V^T P^T in registers;
-// V is transposed by the LDS reads.
-constexpr int kTileRows = 128;
-// keys per tile: 32 with fp32 activations, whose q takes three times the registers
-template <int TYPE>
-constexpr int kTileKeys = TYPE == MX_F32 ? 32 : 64;
+// K and V pass through LDS in tiles of 64 keys.  S^T = K Q^T puts a row in a lane's column, so that its maximum and sum take one
+// exchange between the lane halves, and hands the probabilities to O^T = V^T P^T in registers; V is transposed by the LDS reads.
+//
+// Bound by the matrix instructions and, nearly as much, by the vector arithmetic of the softmax, which run under each other only
+// where the program has them side by side.  So the work goes in steps of 32 keys, and step u holds three things that do not
+// depend on each other: P V of step u-1, the scores of step u+1, and the softmax of step u, whose instructions stand between
+// those matrix instructions.  K's stages are therefore 32 keys ahead of V's.
+//
+// bfloat16 activations: one half-precision piece holds a probability to 11 bits, where bfloat16 would need two and twice the
+// matrix instructions.  V becomes half precision on its way to LDS, scaled by a power of two per run of sixteen keys so that its
+// largest number is near 2^12 (numbers 2^-26 of that and larger stay exact); that power goes into the exponent of the
+// probabilities, against a maximum over (score + exponent), and out of their sum again, which costs an addition per eight
+// keys.  fp32 activations: three bfloat16 pieces of q and of the probabilities, V as it is.
+constexpr int kTileRows = 128, kTileKeys = 64;
 
 // The request and its tile of rows that tile number `tile` is; b < 0: none.  Every wave looks for itself, 64 requests at a time.
 struct Tile {
@@ -509,18 +526,59 @@ __device__ __forceinline__ void copy16_to_lds(const uint8_t* uniform_src, uint32
 
 // Four keys (rows of V in LDS) of one column per lane: lane l of sixteen gives the place of row l/4, columns 4(l%4).. and
 // receives column l of the four rows.
-__device__ __forceinline__ v2u read_transposed(const uint8_t* p) {
-    const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)p);
+__device__ __forceinline__ v2u read_transposed(uint32_t lds) {
+    const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(uintptr_t)lds);
     return __builtin_bit_cast(v2u, r);
 }
+__device__ __forceinline__ v4u lds_read(uint32_t lds) { return *(__attribute__((address_space(3))) const v4u*)(uintptr_t)lds; }
+__device__ __forceinline__ void lds_write(uint32_t lds, v4u x) { *(__attribute__((address_space(3))) v4u*)(uintptr_t)lds = x; }
+// A register that the compiler may not look into: what is added to it stays in the instructions' offsets instead of becoming
+// a register of its own, one for every place in every stage.
+__device__ __forceinline__ void opaque(uint32_t& x) { asm("" : "+v"(x)); }
+
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+
+// Two bfloat16 numbers times a power of two as half-precision numbers
+__device__ __forceinline__ uint32_t bf16_to_half(uint32_t x, float scale) {
+    uint32_t r;
+    asm("v_fma_mixlo_f16 %0, %1, %3, 0\n\tv_fma_mixhi_f16 %0, %2, %3, 0" : "=&v"(r) : "v"(x << 16), "v"(x & 0xffff0000u), "v"(scale));
+    return r;
+}
+// Bytes 2i and 2i+1 of x (mantissas, the sign bit flipped: m + 128) times a power of two as half-precision numbers: the byte
+// goes under the exponent of 1024, and one multiply-add takes 1024 + 128 away again, exactly
+template <int I>
+__device__ __forceinline__ uint32_t bytes_to_half(uint32_t x, v2h scale, v2h minus) {
+    const v2h t = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, x, I == 0 ? 0x04010400u : 0x04030402u));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(t, scale, minus));
+}
+
+template <int CTRL>
+__device__ __forceinline__ float max_with(float v) {
+    return __builtin_fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true)));
+}
+__device__ __forceinline__ float max_across_wave(float v) {
+    v = max_with<0xB1>(v);             // lane ^ 1, ^ 2, 7 - lane in eight, 15 - lane in sixteen
+    v = max_with<0x4E>(v);
+    v = max_with<0x141>(v);
+    v = max_with<0x140>(v);
+    return max_across_16_32(v);
+}
+
+constexpr float kHalfShift = 6.f;      // probabilities are carried times 2^6: the largest is at most 2^14, what is flushed 2^-31 of it
+constexpr float kLag = 8.f;            // the maximum that they are taken against follows the rows' own within this power of two
+constexpr int kLeastExponent = -40;    // of a run of V
 
 template <int TYPE, int DT, int BLOCK>
-__global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
-    constexpr int QP = Pieces<TYPE>::Q, P = Pieces<TYPE>::P;
-    constexpr int KT = kTileKeys<TYPE>, NT = KT / 32, NK = DT / 16, ND = DT / 32;
+__global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kernel(CacheAttnArgs a) {
+    constexpr bool HALF = TYPE == MX_BF16;
+    constexpr int QP = Pieces<TYPE>::Q, P = HALF ? 1 : 3;
+    constexpr int NK = DT / 16, ND = DT / 32;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
-    constexpr int kTensor = KT * DT * 2, kStage = 2 * kTensor;
-    constexpr int kPer = 16, kLanes = DT / kPer;       // MXInt staging: sixteen elements per lane
+    constexpr int kTensor = kTileKeys * DT * 2;            // LDS: K stage 0, 1, V stage 0, 1, then the exponents of V's runs
+    constexpr int kVBase = 2 * kTensor, kExp = 4 * kTensor;
+    constexpr bool kCopyV = BLOCK == 0 && !HALF;           // V goes to LDS as it is
+    constexpr int kLoads = 16 * DT * EB / 1024;            // 16-byte loads per lane that bring a run of sixteen keys
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int i = lane & 31, h2 = lane >> 5;
@@ -548,15 +606,14 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
 
     // the keys that some row of the tile sees, and this split's run of them in whole tiles
     const int all = max(0, len - rq.n + min(r0 + kTileRows - 1, rows - 1) / a.group + 1);
-    const int per = (((all + KT - 1) / KT) + a.splits - 1) / a.splits * KT;
+    const int per = (((all + kTileKeys - 1) / kTileKeys) + a.splits - 1) / a.splits * kTileKeys;
     const int begin = min(split * per, all), stop = min(begin + per, all);
 
     // this wave's rows: q is the right operand of the scores, lane (i, h2) row i, elements 16kk + 8h2 ..
     const int r = min(r0 + 32 * wave + i, rows - 1);
     const int tok = r / a.group, head = h * a.group + (r - tok * a.group);
-    const int last = len - rq.n + tok;
-    const int first_last = len - rq.n + min(r0 + 32 * wave, rows - 1) / a.group;          // the last key all of its rows see
-    const int wave_stop = min(stop, len - rq.n + min(r0 + 32 * wave + 31, rows - 1) / a.group + 1);
+    const int last = min(len - rq.n + tok, stop - 1);                     // the last key of this split that the row sees
+    const int all_see = min(len - rq.n + min(r0 + 32 * wave, rows - 1) / a.group, stop - 1);   // the last one all of the wave's see
     v4u qf[QP][NK];
 #pragma unroll
     for (int kk = 0; kk < NK; ++kk) {
@@ -572,52 +629,68 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
         }
     }
 
-    // Staging.  bfloat16: copies from memory straight to LDS, 1 KiB (whole rows) per wave and instruction, lane L's bytes at
-    // 16 L of it, so the placement of the chunks is done by what each lane reads.  MXInt: through registers.
-    const int last_run = (len - 1) & ~15;
+    // ---- staging: a wave brings one run of sixteen keys of a stage, which lies in one page -------------------
+    // As it is (bfloat16 K, bfloat16 V for fp32 activations): copies from memory straight to LDS, 1 KiB each, lane L's bytes at
+    // 16 L of it, so the placement of the chunks is done by what each lane reads.  Else through registers.
+    constexpr int kLaneRows = 1024 / (DT * EB);                           // rows of a load
+    constexpr int kRowLanes = 64 / kLaneRows;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
-    constexpr int kPieceRows = BLOCK == 0 ? 512 / DT : 64 / kLanes;       // rows of a wave's piece, within a run of sixteen
-    constexpr int kPieces = KT / (4 * kPieceRows) > 0 ? KT / (4 * kPieceRows) : 1;
-    const int rel = BLOCK == 0 ? lane / (DT / 8) : lane / kLanes;         // this lane's row of the piece
-    uint32_t k_from = 0, v_from = 0;                                      // and the place of what it reads in there
-    {
-        const int row = kPieceRows * wave + rel;                          // the pieces are 4 * kPieceRows rows apart: no matter here
-        if constexpr (BLOCK == 0) {
-            const int chunk = lane % (DT / 8);
-            const int kc = (k_place<DT>(row, chunk) - row * DT * 2) >> 4, vc = (v_place<DT>(row, chunk) - row * DT * 2) >> 4;
-            k_from = (rel * dim + (8 * kc < dim ? 8 * kc : 0)) * 2;
-            v_from = (rel * dim + (8 * vc < dim ? 8 * vc : 0)) * 2;
-        } else {
-            const int d = (lane % kLanes) * kPer;
-            k_from = v_from = rel * dim + (d < dim ? d : 0);
+    const int last_run = (len - 1) & ~15;
+    const int rel = lane / kRowLanes;
+    const int lane_d = lane % kRowLanes * (16 / EB);                      // what lies past the head dimension reads its start again
+    uint32_t k_from[BLOCK == 0 ? kLoads : 1], v_from[kCopyV ? kLoads : 1];
+    const uint32_t from = (rel * dim + (lane_d < dim ? lane_d : 0)) * EB;
+    if constexpr (BLOCK == 0) {
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            const int row = u * kLaneRows + rel, chunk = lane % kRowLanes;
+            const int kc = 8 * ((k_place<DT>(row, chunk) - row * DT * 2) >> 4), vc = 8 * ((v_place<DT>(row, chunk) - row * DT * 2) >> 4);
+            k_from[u] = (row * dim + (kc < dim ? kc : 0)) * 2;
+            if constexpr (kCopyV) v_from[u] = (row * dim + (vc < dim ? vc : 0)) * 2;
         }
     }
-    const uint32_t e_from = BLOCK == 0 ? 0 : rel * (dim / (BLOCK == 0 ? 1 : BLOCK)) + (k_from - rel * dim) / (BLOCK == 0 ? 1 : BLOCK);
-    v4u sk[BLOCK == 0 ? 1 : kPieces], sv[BLOCK == 0 ? 1 : kPieces];
-    int ek[BLOCK == 0 ? 1 : kPieces], ev[BLOCK == 0 ? 1 : kPieces];
-    PageWindow pages(a, b, len);
-    const bool stages = 4 * kPieceRows <= KT || wave < KT / kPieceRows;   // with few keys per tile some waves have none to bring
-    auto load = [&](uint32_t stage, int kb) __attribute__((always_inline)) {
-        if (!stages) return;
+    const uint32_t e_from = BLOCK == 0 ? 0 : rel * (dim / (BLOCK == 0 ? 1 : BLOCK)) + (lane_d < dim ? lane_d : 0) / (BLOCK == 0 ? 1 : BLOCK);
+    uint32_t k_to[kLoads][2], v_to[kLoads][2];                            // places of this lane's chunks in a stage
 #pragma unroll
-        for (int u = 0; u < kPieces; ++u) {
-            const int key = kb + (4 * u + wave) * kPieceRows, run = min(key & ~15, last_run);
-            const int64_t row = pages.row(a, h, run) + (key & 15);
-            const uint8_t* kp = a.k + row * dim * EB;
-            const uint8_t* vp = a.v + row * dim * EB;
+    for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int row = 16 * wave + u * kLaneRows + rel, chunk = lane % kRowLanes * (2 / EB) + x;
+            k_to[u][x] = lds0 + k_place<DT>(row, chunk);
+            v_to[u][x] = lds0 + kVBase + v_place<DT>(row, chunk);
+        }
+    v4u sk[BLOCK == 0 ? 1 : kLoads], sv[kCopyV ? 1 : kLoads];
+    int ek[kLoads], ev[kLoads];
+    PageWindow pages(a, b, len);
+    auto row_of = [&](int key) __attribute__((always_inline)) { return pages.row(a, h, max(min(key + 16 * wave, last_run), 0)); };
+    // K stage t: keys begin + 64t + 32 ..; V stage t: keys begin + 64t ..
+    auto load_k = [&](int slot, int key0) __attribute__((always_inline)) {
+        const int64_t row = row_of(key0);
+        const uint8_t* src = a.k + row * dim * EB;
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
             if constexpr (BLOCK == 0) {
-                const uint32_t to = lds0 + stage + (4 * u + wave) * 1024;
-                copy16_to_lds(kp, k_from, to);
-                copy16_to_lds(vp, v_from, to + kTensor);
+                copy16_to_lds(src, k_from[u], lds0 + slot + wave * (16 * DT * 2) + u * 1024);
             } else {
-                sk[u] = *reinterpret_cast<const v4u*>(kp + k_from);
-                sv[u] = *reinterpret_cast<const v4u*>(vp + v_from);
-                ek[u] = (a.k_exps + row * (dim / BLOCK))[e_from];
-                ev[u] = (a.v_exps + row * (dim / BLOCK))[e_from];
+                sk[u] = *reinterpret_cast<const v4u*>(src + u * kLaneRows * dim + from);
+                ek[u] = (a.k_exps + row * (dim / BLOCK) + u * kLaneRows * (dim / BLOCK))[e_from];
             }
         }
     };
-    auto widen = [&](const v4u& x, float sc, v4u (&y)[2]) {               // sixteen mantissas to bfloat16 numbers
+    auto load_v = [&](int slot, int key0) __attribute__((always_inline)) {
+        const int64_t row = row_of(key0);
+        const uint8_t* src = a.v + row * dim * EB;
+#pragma unroll
+        for (int u = 0; u < kLoads; ++u) {
+            if constexpr (kCopyV) {
+                copy16_to_lds(src, v_from[u], lds0 + kVBase + slot + wave * (16 * DT * 2) + u * 1024);
+            } else {
+                sv[u] = *reinterpret_cast<const v4u*>(src + u * kLaneRows * dim * EB + from);
+                if constexpr (BLOCK != 0) ev[u] = (a.v_exps + row * (dim / BLOCK) + u * kLaneRows * (dim / BLOCK))[e_from];
+            }
+        }
+    };
+    auto widen = [&](const v4u& x, float sc, v4u (&y)[2]) __attribute__((always_inline)) {     // sixteen mantissas to bfloat16 numbers
 #pragma unroll
         for (int w = 0; w < 8; ++w) {
             int t = (int)x[w >> 1];
@@ -626,42 +699,90 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
             y[w >> 2][w & 3] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
         }
     };
-    // What lies past the request's end may be anything, NaN among it, and meets probabilities of zero: it becomes zeros.  (Past
-    // the head dimension lies a repetition; it meets zeros of q, or gives results that nobody reads.)
-    auto store = [&](uint8_t* stage, int kb) __attribute__((always_inline)) {
+    auto put_k = [&](int slot) __attribute__((always_inline)) {
         if constexpr (BLOCK != 0) {
-            if (!stages) return;
 #pragma unroll
-            for (int u = 0; u < kPieces; ++u) {
-                const int key = (4 * u + wave) * kPieceRows + rel, chunk = 2 * (lane % kLanes);
-                const bool in = kb + key < len;
+            for (int u = 0; u < kLoads; ++u) {
                 v4u y[2];
-                widen(sk[u], in ? power2(ek[u] - a.exp_shift) : 0.f, y);
-                *reinterpret_cast<v4u*>(stage + k_place<DT>(key, chunk)) = y[0];
-                *reinterpret_cast<v4u*>(stage + k_place<DT>(key, chunk + 1)) = y[1];
-                widen(sv[u], in ? power2(ev[u] - a.exp_shift) : 0.f, y);
-                *reinterpret_cast<v4u*>(stage + kTensor + v_place<DT>(key, chunk)) = y[0];
-                *reinterpret_cast<v4u*>(stage + kTensor + v_place<DT>(key, chunk + 1)) = y[1];
+                widen(sk[u], power2(ek[u] - a.exp_shift), y);
+                lds_write(k_to[u][0] + slot, y[0]);
+                lds_write(k_to[u][1] + slot, y[1]);
             }
         }
     };
-    auto clear_past = [&](uint8_t* stage, int kb) __attribute__((always_inline)) {
-        if constexpr (BLOCK == 0) {
-            const int from = (len - kb) * DT * 2;                         // rows of the V tile lie one after another
-            const v4u zero = {0, 0, 0, 0};
-            for (int x = from + threadIdx.x * 16; x < kTensor; x += 4096) *reinterpret_cast<v4u*>(stage + kTensor + x) = zero;
+    // What lies past the request's end may be anything, NaN among it, and meets probabilities of zero: it becomes zeros.  (Past
+    // the head dimension lies a repetition; it meets zeros of q, or gives results that nobody reads.)
+    auto put_v = [&](int slot, int key0) __attribute__((always_inline)) {
+        if constexpr (kCopyV) return;
+        if (key0 + 16 * wave + 16 > len) {
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                const bool in = key0 + 16 * wave + u * kLaneRows + rel < len;
+                if constexpr (BLOCK == 0) sv[u] = in ? sv[u] : v4u{0, 0, 0, 0};
+                else sv[u] = in ? sv[u] : v4u{0, 0, 0, 0}, ev[u] = in ? ev[u] : 0;
+            }
+        }
+        if constexpr (!HALF) {
+            if constexpr (BLOCK != 0) {
+#pragma unroll
+                for (int u = 0; u < kLoads; ++u) {
+                    v4u y[2];
+                    widen(sv[u], power2(ev[u] - a.exp_shift), y);
+                    lds_write(v_to[u][0] + slot, y[0]);
+                    lds_write(v_to[u][1] + slot, y[1]);
+                }
+            }
+        } else if constexpr (BLOCK == 0) {
+            float top = 0.f;                                              // the low half of a dword does not reach its exponent
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u)
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(__uint_as_float(sv[u][w])), __builtin_fabsf(__uint_as_float(sv[u][w] << 16))), top);
+            top = max_across_wave(top);
+            const int e = max((int)(__float_as_uint(top) >> 23) - 127 - 11, kLeastExponent);
+            if (lane == 0) *reinterpret_cast<float*>(smem + kExp + (slot ? 16 : 0) + wave * 4) = (float)e;
+            const float scale = power2(-e);
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                v4u y;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) y[w] = bf16_to_half(sv[u][w], scale);
+                lds_write(v_to[u][0] + slot, y);
+            }
+        } else {
+            int et = ev[0];
+#pragma unroll
+            for (int u = 1; u < kLoads; ++u) et = max(et, ev[u]);
+            et = (int)max_across_wave((float)et);
+            const int e = max(et - a.exp_shift - 5, kLeastExponent);
+            if (lane == 0) *reinterpret_cast<float*>(smem + kExp + (slot ? 16 : 0) + wave * 4) = (float)e;
+#pragma unroll
+            for (int u = 0; u < kLoads; ++u) {
+                const float sc = power2(ev[u] - a.exp_shift - e);         // at most 2^5
+                const _Float16 s1 = (_Float16)sc, m1 = (_Float16)(sc * -1152.f);
+                const v2h scale = {s1, s1}, minus = {m1, m1};
+                v4u y[2];
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t x = sv[u][w] ^ 0x80808080u;
+                    y[w >> 1][2 * (w & 1)] = bytes_to_half<0>(x, scale, minus);
+                    y[w >> 1][2 * (w & 1) + 1] = bytes_to_half<1>(x, scale, minus);
+                }
+                lds_write(v_to[u][0] + slot, y[0]);
+                    lds_write(v_to[u][1] + slot, y[1]);
+            }
         }
     };
 
     // places of this lane's reads in a stage, without the multiples of eight keys that the instructions add
-    const uint8_t* k_at[NK];
-    const uint8_t* v_at[ND];
+    uint32_t k_at[NK], v_at[ND];
 #pragma unroll
-    for (int kk = 0; kk < NK; ++kk) k_at[kk] = smem + k_place<DT>(i, 2 * kk + h2);
+    for (int kk = 0; kk < NK; ++kk) k_at[kk] = lds0 + k_place<DT>(i, 2 * kk + h2);
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt) {
         const int d = 32 * dt + (lane & 16) + 4 * (lane & 3);
-        v_at[dt] = smem + kTensor + v_place<DT>(4 * h2 + ((lane & 15) >> 2), d >> 3) + (d & 7) * 2;
+        v_at[dt] = lds0 + kVBase + v_place<DT>(4 * h2 + ((lane & 15) >> 2), d >> 3) + (d & 7) * 2;
     }
 
     float m = -__builtin_inff(), l = 0.f;
@@ -670,53 +791,84 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[dt][e] = 0.f;
+    v16f s[2];                                  // scores of an even and an odd step; register e: key 8(e/4) + 4h2 + e%4
+    v4u kf[NK], vf[2][ND], pf[2][P];            // vf, pf: two runs of sixteen keys of the step before
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) vf[x][dt] = v4u{0, 0, 0, 0};
+#pragma unroll
+        for (int p = 0; p < P; ++p) pf[x][p] = v4u{0, 0, 0, 0};
+    }
+    auto read_k = [&](int first, int end_, int at) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kk = first; kk < end_; ++kk) {
+            opaque(k_at[kk]);
+            kf[kk] = lds_read(k_at[kk] + at);
+        }
+    };
+    auto read_v = [&](int x, int dt, int at) __attribute__((always_inline)) {
+        opaque(v_at[dt]);
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj) {
+            const v2u y = read_transposed(v_at[dt] + (at + (16 * x + 8 * jj) * DT * 2));
+            vf[x][dt][2 * jj] = y[0];
+            vf[x][dt][2 * jj + 1] = y[1];
+        }
+    };
+    auto score = [&](int n, auto set_c) __attribute__((always_inline)) {              // matrix instruction n of NK * QP
+        constexpr int set = decltype(set_c)::value;
+        const int kk = n / QP, p = QP - 1 - n % QP;
+        v16f zero;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+        s[set] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, kf[kk]), __builtin_bit_cast(v8bf, qf[p][kk]),
+                                                         n == 0 ? zero : s[set], 0, 0, 0);
+    };
+    auto out = [&](int n) __attribute__((always_inline)) {                            // matrix instruction n of 2 * P * ND
+        const int x = n / (P * ND), p = P - 1 - n / ND % P, dt = n % ND;
+        if constexpr (HALF)
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, vf[x][dt]), __builtin_bit_cast(v8h, pf[x][p]), o[dt], 0, 0, 0);
+        else
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, vf[x][dt]), __builtin_bit_cast(v8bf, pf[x][p]), o[dt], 0, 0, 0);
+    };
 
-    auto compute = [&](auto stage_c, int kb) __attribute__((always_inline)) {
-        constexpr int stage = decltype(stage_c)::value * kStage;
-        v16f s[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
-#pragma unroll
-            for (int kk = 0; kk < NK; ++kk) {
-                const v4u kf = *reinterpret_cast<const v4u*>(k_at[kk] + (stage + 32 * t * DT * 2));
-#pragma unroll
-                for (int p = QP - 1; p >= 0; --p)
-                    s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, kf), __builtin_bit_cast(v8bf, qf[p][kk]), s[t],
-                                                                   0, 0, 0);
-            }
-        }
-        v4u vf[2][ND];
-        auto read_v = [&](int step) __attribute__((always_inline)) {                                     // sixteen keys
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                for (int jj = 0; jj < 2; ++jj) {
-                    const v2u x = read_transposed(v_at[dt] + (stage + (16 * step + 8 * jj) * DT * 2));
-                    vf[step & 1][dt][2 * jj] = x[0];
-                    vf[step & 1][dt][2 * jj + 1] = x[1];
-                }
-        };
-        read_v(0);
-        // result register e of half t: key 32t + 8(e/4) + 4h2 + e%4
-        if (kb + KT - 1 > min(first_last, wave_stop - 1)) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int key = kb + 32 * t + 8 * (e >> 2) + 4 * h2 + (e & 3);
-                    s[t][e] = key <= last && key < stop ? s[t][e] : -__builtin_inff();
-                }
-        }
+    // One step of 32 keys from kb; k_next: place of the next step's keys in LDS, v_this: of this step's values, e0 and e1: the
+    // exponents of their two runs.
+    auto step = [&](auto set_c, int kb, auto k_next_c, auto v_this_c, float e0, float e1) __attribute__((always_inline)) {
+        constexpr int set = decltype(set_c)::value, k_next = decltype(k_next_c)::value, v_this = decltype(v_this_c)::value;
+        constexpr int NO = 2 * P * ND, NQ = NK * QP;
         float top = -__builtin_inff();
+        // P V of the step before, the maximum of this step's scores under it.  The operands of both products share registers: a
+        // half of one is read from LDS when a half of the other has been used.
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int n = 0; n < NO; ++n) {
+            out(n);
+            __builtin_amdgcn_sched_barrier(0);
+            if (n == NO / 2 - 1) read_k(0, NK / 2, k_next);
+            if (n == NO - 1) read_k(NK / 2, NK, k_next);
+            if (n == 0 && kb + 31 > all_see) {
+                const int most = last - kb - 4 * h2;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) top = __builtin_fmaxf(top, s[t][e]);
-        top = max_across_32(top) * a.c;
-        // The sums are kept against a maximum that follows the rows' own within 2^8: the first tile sets it, few later ones move it.
-        if (__any(top > m + 8.f)) {
+                for (int e = 0; e < 16; ++e) s[set][e] = 8 * (e >> 2) + (e & 3) <= most ? s[set][e] : -__builtin_inff();
+            }
+            if (n == NO / 2) {
+                float t[2];
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    t[x] = max_of(s[set][8 * x], s[set][8 * x + 1], s[set][8 * x + 2]);
+                    t[x] = max_of(t[x], s[set][8 * x + 3], s[set][8 * x + 4]);
+                    t[x] = max_of(t[x], s[set][8 * x + 5], s[set][8 * x + 6]);
+                    t[x] = max_of(t[x], s[set][8 * x + 7]);
+                }
+                if constexpr (HALF) top = max_of(__builtin_fmaf(t[0], a.c, e0), __builtin_fmaf(t[1], a.c, e1));
+                else top = max_of(t[0], t[1]) * a.c;
+                top = max_across_32(top);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // The sums are kept against a maximum that follows the rows' own within 2^8: the first step sets it, few later ones move it.
+        if (__any(top > m + kLag)) {
             const float m_new = __builtin_fmaxf(m, top);
             const float alpha = m_new == -__builtin_inff() ? 1.f : exp2_of(m - m_new);
             m = m_new;
@@ -727,60 +879,91 @@ __global__ __launch_bounds__(256, 2) void cache_chunk_kernel(CacheAttnArgs a) {
                 for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
         }
         const float m_use = m == -__builtin_inff() ? 0.f : m;
+        const float add[2] = {HALF ? e0 + kHalfShift - m_use : -m_use, HALF ? e1 + kHalfShift - m_use : -m_use};
+        __builtin_amdgcn_sched_barrier(0);
+        // the scores of the next step, this step's probabilities under it; its values are read for the step after
+        float sum = 0.f;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float sum = 0.f;
+        for (int n = 0; n < NQ; ++n) {
+            score(n, std::integral_constant<int, set ^ 1>{});
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                s[t][e] = exp2_of(__builtin_fmaf(s[t][e], a.c, -m_use));
-                sum += s[t][e];
-            }
-            l += sum;
+            for (int x = n * 8 / NQ; x < (n + 1) * 8 / NQ; ++x) {         // probabilities 2x and 2x + 1
+                float pr[2];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const int step = 2 * t + half;
-                if (step + 1 < 2 * NT) read_v(step + 1);
-                v4u pf[P];
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    uint32_t x[P];
-                    pieces_of<P>(s[t][8 * half + 2 * w], s[t][8 * half + 2 * w + 1], x);
-#pragma unroll
-                    for (int p = 0; p < P; ++p) pf[p][w] = x[p];
+                for (int y = 0; y < 2; ++y) {
+                    pr[y] = exp2_of(__builtin_fmaf(s[set][2 * x + y], a.c, add[x >> 2]));
+                    sum += pr[y];
                 }
+                if constexpr (HALF) {
+                    const v2h q2 = {(_Float16)pr[0], (_Float16)pr[1]};
+                    pf[x >> 2][0][x & 3] = __builtin_bit_cast(uint32_t, q2);
+                    if (x == 3) { l += __builtin_ldexpf(sum, -(int)e0); sum = 0.f; }
+                    if (x == 7) l += __builtin_ldexpf(sum, -(int)e1);
+                } else {
+                    uint32_t w[P];
+                    pieces_of<P>(pr[0], pr[1], w);
 #pragma unroll
-                for (int p = P - 1; p >= 0; --p)
+                    for (int p = 0; p < P; ++p) pf[x >> 2][p][x & 3] = w[p];
+                    if (x == 7) l += sum;
+                }
+            }
+            if (n == NQ / 2 - 1 || n == NQ - 1) {
 #pragma unroll
-                    for (int dt = 0; dt < ND; ++dt)
-                        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, vf[step & 1][dt]),
-                                                                        __builtin_bit_cast(v8bf, pf[p]), o[dt], 0, 0, 0);
+                for (int dt = 0; dt < ND; ++dt) read_v(n == NQ - 1, dt, v_this);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // A tile of 64 keys in the stages at `slot` (0 or kTensor): its data is awaited and published, the next one's is asked for and,
+    // where it passes through registers, put in place after the arithmetic.  One body for both stages: with two, the compiler
+    // keeps the accumulators in two places.
+    if (begin < stop) {
+        // before the loop: the first 32 keys' scores, from what would be K's stage before the first, and the first stages
+        load_k(kTensor, begin - 32);
+        put_k(kTensor);
+        load_v(0, begin);
+        load_k(0, begin + 32);
+        put_k(0);
+        put_v(0, begin);
+        if constexpr (BLOCK == 0) __builtin_amdgcn_s_waitcnt(0x0F70);
+        __syncthreads();
+        read_k(0, NK, kTensor + 32 * DT * 2);
+#pragma unroll
+        for (int n = 0; n < NK * QP; ++n) score(n, std::integral_constant<int, 0>{});
+        int slot = 0;
+        for (int kb = begin; kb < stop; kb += kTileKeys) {
+            if constexpr (BLOCK == 0) __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0): the copies
+            __syncthreads();
+            if (kCopyV && kb + kTileKeys > len) {
+                const v4u zero = {0, 0, 0, 0};                                // rows of the stage lie one after another
+                for (int x = (len - kb) * DT * 2 + threadIdx.x * 16; x < kTensor; x += 4096) lds_write(lds0 + kVBase + slot + x, zero);
+                __syncthreads();
+            }
+            const bool more = kb + kTileKeys < stop;
+            if (more) {
+                load_v(slot ^ kTensor, kb + kTileKeys);
+                load_k(slot ^ kTensor, kb + kTileKeys + 32);
+            }
+            float4 e = make_float4(0.f, 0.f, 0.f, 0.f);
+            if constexpr (HALF) e = *reinterpret_cast<const float4*>(smem + kExp + (slot ? 16 : 0));
+            constexpr auto first = std::integral_constant<int, 0>{};
+            constexpr auto second = std::integral_constant<int, 32 * DT * 2>{};
+            step(std::integral_constant<int, 0>{}, kb, first, first, e.x, e.y);
+            step(std::integral_constant<int, 1>{}, kb + 32, second, second, e.z, e.w);
+            const int to_other = slot ? -kTensor : kTensor;
+            slot ^= kTensor;
+#pragma unroll
+            for (int kk = 0; kk < NK; ++kk) k_at[kk] += to_other;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) v_at[dt] += to_other;
+            if (more) {
+                put_k(slot);
+                put_v(slot, kb + kTileKeys);
             }
         }
-    };
-
-    // A tile: its data is awaited and published, the next tile's is asked for, and, MXInt, put in place after the arithmetic.
-    auto step = [&](auto stage_c, int kb) __attribute__((always_inline)) {
-        constexpr int at = decltype(stage_c)::value * kStage, other = kStage - at;
-        if constexpr (BLOCK == 0) __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0): the copies
-        __syncthreads();                                                  // the tile is there, and the other stage has been read
-        if (BLOCK == 0 && kb + KT > len) {
-            clear_past(smem + at, kb);
-            __syncthreads();
-        }
-        const bool more = kb + KT < stop;
-        if (more) load(other, kb + KT);
-        if (kb < wave_stop) compute(stage_c, kb);
-        if (more) store(smem + other, kb + KT);
-    };
-    if (begin < stop) {
-        load(0, begin);
-        store(smem, begin);
-        for (int kb = begin;;) {
-            step(std::integral_constant<int, 0>{}, kb);
-            if ((kb += KT) >= stop) break;
-            step(std::integral_constant<int, 1>{}, kb);
-            if ((kb += KT) >= stop) break;
-        }
+#pragma unroll
+        for (int n = 0; n < 2 * P * ND; ++n) out(n);
     }
 
     // lane (i, h2) holds row i, elements 32dt + 8(e/4) + 4h2 + e%4
@@ -945,7 +1128,7 @@ mx_status launch_kernels(CacheAttnArgs a, const Plan& p, uint8_t* workspace, hip
         const int64_t rows = (int64_t)p.tiles * a.heads * kTileRows;
         a.part_o = (float*)(workspace + kCounterBytes);
         a.part_ml = (float2*)(a.part_o + rows * p.chunk_splits * a.dim);
-        constexpr int lds = 4 * kTileKeys<TYPE> * DT * 2;
+        constexpr int lds = 4 * kTileKeys * DT * 2 + 32;
         static std::atomic<uint64_t> raised{0};
         if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_chunk_kernel<TYPE, DT, BLOCK>, lds, raised)) return MX_ERR_DEVICE;
         cache_chunk_kernel<TYPE, DT, BLOCK><<<(unsigned)((int64_t)p.tiles * a.heads * p.chunk_splits), 256, lds, stream>>>(a);
