@@ -532,6 +532,10 @@ __device__ __forceinline__ v2u read_transposed(uint32_t lds) {
 }
 __device__ __forceinline__ v4u lds_read(uint32_t lds) { return *(__attribute__((address_space(3))) const v4u*)(uintptr_t)lds; }
 __device__ __forceinline__ void lds_write(uint32_t lds, v4u x) { *(__attribute__((address_space(3))) v4u*)(uintptr_t)lds = x; }
+// The value is computed before this point: an empty volatile statement is ordered with the scheduling fences, and so, through it,
+// is the (otherwise freely movable) arithmetic that gives x.
+__device__ __forceinline__ void pin(float x) { asm volatile("" ::"v"(x)); }
+__device__ __forceinline__ void pin(uint32_t x) { asm volatile("" ::"v"(x)); }
 // A register that the compiler may not look into: what is added to it stays in the instructions' offsets instead of becoming
 // a register of its own, one for every place in every stage.
 __device__ __forceinline__ void opaque(uint32_t& x) { asm("" : "+v"(x)); }
@@ -895,16 +899,21 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kerne
                     pr[y] = exp2_of(__builtin_fmaf(s[set][2 * x + y], a.c, add[x >> 2]));
                     sum += pr[y];
                 }
+                pin(sum);
                 if constexpr (HALF) {
                     const v2h q2 = {(_Float16)pr[0], (_Float16)pr[1]};
                     pf[x >> 2][0][x & 3] = __builtin_bit_cast(uint32_t, q2);
+                    pin(pf[x >> 2][0][x & 3]);
                     if (x == 3) { l += __builtin_ldexpf(sum, -(int)e0); sum = 0.f; }
                     if (x == 7) l += __builtin_ldexpf(sum, -(int)e1);
                 } else {
                     uint32_t w[P];
                     pieces_of<P>(pr[0], pr[1], w);
 #pragma unroll
-                    for (int p = 0; p < P; ++p) pf[x >> 2][p][x & 3] = w[p];
+                    for (int p = 0; p < P; ++p) {
+                        pf[x >> 2][p][x & 3] = w[p];
+                        pin(w[p]);
+                    }
                     if (x == 7) l += sum;
                 }
             }
@@ -991,67 +1000,82 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kerne
 }
 
 // ---- joining the splits ---------------------------------------------------------------------------------
-// o = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), in the order of the splits whatever order they ended in.  A workgroup takes
-// a row, each wave a quarter of its splits: the loads of a wave do not wait for each other.
+// o = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), in an order that the number of splits gives, whatever order they ended in.
+// 32 lanes take a row, four elements each; with many splits the eight groups of a workgroup share a row (GROUPS 8), with few they
+// take eight rows.
 constexpr int kMaxSplits = 64;
 
-template <int TYPE, bool CHUNK>
+template <int TYPE, bool CHUNK, int GROUPS>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
-    __shared__ float lds[4][128];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t prow = blockIdx.x;
+    __shared__ float4 lds[GROUPS == 8 ? 8 : 1][32];
+    const int group = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t prow = GROUPS == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + group;
     const int unit = (int)(prow / a.part_rows), row = (int)(prow - (int64_t)unit * a.part_rows);
     const int h = unit % a.heads;
     int b = unit / a.heads, r = row;
-    if constexpr (CHUNK) {
+    if constexpr (CHUNK) {                            // part_rows is 128, so the rows of a workgroup are of one unit
         const Tile t = find_tile(a, b);
         if (t.b < 0) return;
         b = t.b;
         r += t.index * kTileRows;
+    } else if (b >= a.requests) {
+        return;
     }
     const Request rq = request_of(a, b);
     const int64_t rows = (int64_t)rq.n * a.group;
     if (r >= rows || rows < a.least || rows > a.most || (!CHUNK && rows > a.part_rows)) return;
     const int tok = r / a.group, head = h * a.group + (r - tok * a.group);
 
-    const float2 ml = lane < a.splits ? a.part_ml[prow * a.splits + lane] : make_float2(-__builtin_inff(), 0.f);
-    float mm = ml.x;
+    float2 ml[2];
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) mm = __builtin_fmaxf(mm, __shfl_xor(mm, d, 64));
-    const float f = ml.x == -__builtin_inff() ? 0.f : exp2_of(ml.x - mm);
-    float ll = ml.y * f;
+    for (int x = 0; x < 2; ++x) ml[x] = lane + 32 * x < a.splits ? a.part_ml[prow * a.splits + lane + 32 * x] : make_float2(-__builtin_inff(), 0.f);
+    float mm = __builtin_fmaxf(ml[0].x, ml[1].x);
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) ll += __shfl_xor(ll, d, 64);
-    const float* p = a.part_o + prow * a.splits * a.dim;
-    float x0 = 0.f, x1 = 0.f;
-    const bool two = lane + 64 < a.dim, one = lane < a.dim;
-    for (int s0 = wave; s0 < a.splits; s0 += 32) {
-        float y0[8], y1[8];
+    for (int d = 1; d < 32; d *= 2) mm = __builtin_fmaxf(mm, __shfl_xor(mm, d, 32));
+    const float f0 = ml[0].x == -__builtin_inff() ? 0.f : exp2_of(ml[0].x - mm);
+    const float f1 = ml[1].x == -__builtin_inff() ? 0.f : exp2_of(ml[1].x - mm);
+    float ll = ml[0].y * f0 + ml[1].y * f1;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) ll += __shfl_xor(ll, d, 32);
+
+    const int d = 4 * lane;
+    const float4* p = reinterpret_cast<const float4*>(a.part_o + prow * a.splits * a.dim + (d < a.dim ? d : 0));
+    const int stride = a.dim / 4;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = GROUPS == 8 ? group : 0; s0 < a.splits; s0 += 8 * GROUPS) {
+        float4 y[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) y[u] = p[(int64_t)min(s0 + u * GROUPS, a.splits - 1) * stride];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const int64_t at = (int64_t)min(s0 + 4 * u, a.splits - 1) * a.dim + lane;
-            y0[u] = one ? p[at] : 0.f;
-            y1[u] = two ? p[at + 64] : 0.f;
-        }
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int s = s0 + 4 * u;
-            const float w = s < a.splits ? __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(f), s & 63)) : 0.f;
-            x0 += y0[u] * w;
-            x1 += y1[u] * w;
+            const int s = s0 + u * GROUPS;
+            const float w0 = __shfl(s < 32 ? f0 : f1, s & 31, 32), w = s < a.splits ? w0 : 0.f;
+            x.x += y[u].x * w; x.y += y[u].y * w; x.z += y[u].z * w; x.w += y[u].w * w;
         }
     }
-    lds[wave][lane] = x0;
-    lds[wave][lane + 64] = x1;
-    __syncthreads();
-    const int d = threadIdx.x * 4;
+    if constexpr (GROUPS == 8) {
+        lds[group][lane] = x;
+        __syncthreads();
+        if (group != 0) return;
+#pragma unroll
+        for (int g = 1; g < 8; ++g) {
+            const float4 y = lds[g][lane];
+            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+        }
+    }
     if (d < a.dim) {
         const float inv = ll > 0.f ? 1.f / ll : 0.f;
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = (lds[0][d + e] + lds[1][d + e] + lds[2][d + e] + lds[3][d + e]) * inv;
-        store_out<TYPE, 4>(a, (int64_t)(rq.t0 + tok) * a.ldo + (int64_t)head * a.dim + d, x);
+        const float o[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+        store_out<TYPE, 4>(a, (int64_t)(rq.t0 + tok) * a.ldo + (int64_t)head * a.dim + d, o);
     }
+}
+
+template <int TYPE, bool CHUNK>
+mx_status launch_join(const CacheAttnArgs& a, int64_t rows, hipStream_t stream) {
+    if (a.splits > 8) cache_join_kernel<TYPE, CHUNK, 8><<<(unsigned)rows, 256, 0, stream>>>(a);
+    else cache_join_kernel<TYPE, CHUNK, 1><<<(unsigned)ceil_div(rows, 8), 256, 0, stream>>>(a);
+    MX_HIP_LAUNCH_CHECK();
+    return MX_OK;
 }
 
 template <int TYPE>
@@ -1076,7 +1100,21 @@ struct Plan {
     size_t bytes;
 };
 
-Plan plan_of(const mx_cache& c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len) {
+// Splits of the keys for `groups` workgroups that have `tiles` tiles of 64 keys each to go through, `slots` of which the GPU holds at
+// once: the fewest rounds times tiles, a workgroup's start and end counting as kStart tiles.  (Two sides, chunk of 300 rows of fp32
+// on 2000 keys, 96 groups: see the table of the design notes.)
+int chunk_splits(int64_t groups, int64_t tiles, int64_t slots) {
+    constexpr int kStart = 5;
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int s = 1; s <= kMaxSplits && s <= tiles; ++s) {
+        const int64_t cost = ceil_div(groups * s, slots) * (ceil_div(tiles, s) + kStart + (s > 1 ? 2 : 0));
+        if (cost < least) { least = cost; best = s; }
+    }
+    return best;
+}
+
+Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len) {
     Plan p{};
     const int64_t group = heads_q / c.heads;
     const int64_t most = (max_new < tokens ? max_new : tokens) * group;
@@ -1090,8 +1128,7 @@ Plan plan_of(const mx_cache& c, int64_t tokens, int64_t requests, int32_t heads_
     const int64_t rows = tokens * group;
     const int64_t big = p.decode ? (rows / (kFewRows + 1) < requests ? rows / (kFewRows + 1) : requests) : 1;   // requests with more rows
     p.tiles = p.chunk ? clamp(p.decode ? rows / kTileRows + big : ceil_div(rows, kTileRows), INT32_MAX) : 0;
-    p.chunk_splits = p.chunk ? clamp(512 / ((int64_t)p.tiles * c.heads), ceil_div(max_len, 512)) : 1;
-    p.chunk_splits = p.chunk_splits > kMaxSplits ? kMaxSplits : p.chunk_splits;
+    p.chunk_splits = p.chunk ? chunk_splits((rows / kTileRows + 1) * c.heads, ceil_div(max_len, kTileKeys), type == MX_F32 ? 256 : 512) : 1;
     const size_t part = (size_t)c.dim * 4 + 8;
     const size_t few = p.decode && p.splits > 1 ? (size_t)units * p.part_rows * p.splits * part : 0;
     const size_t many = p.chunk && p.chunk_splits > 1 ? (size_t)p.tiles * c.heads * kTileRows * p.chunk_splits * part : 0;
@@ -1115,8 +1152,8 @@ mx_status launch_kernels(CacheAttnArgs a, const Plan& p, uint8_t* workspace, hip
         MX_HIP_LAUNCH_CHECK();
         a.fill = 0;
         if (p.splits > 1) {
-            cache_join_kernel<TYPE, false><<<(unsigned)rows, 256, 0, stream>>>(a);
-            MX_HIP_LAUNCH_CHECK();
+            const mx_status st = launch_join<TYPE, false>(a, rows, stream);
+            if (st != MX_OK) return st;
         }
     }
     if (p.chunk) {
@@ -1133,10 +1170,7 @@ mx_status launch_kernels(CacheAttnArgs a, const Plan& p, uint8_t* workspace, hip
         if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_chunk_kernel<TYPE, DT, BLOCK>, lds, raised)) return MX_ERR_DEVICE;
         cache_chunk_kernel<TYPE, DT, BLOCK><<<(unsigned)((int64_t)p.tiles * a.heads * p.chunk_splits), 256, lds, stream>>>(a);
         MX_HIP_LAUNCH_CHECK();
-        if (p.chunk_splits > 1) {
-            cache_join_kernel<TYPE, true><<<(unsigned)rows, 256, 0, stream>>>(a);
-            MX_HIP_LAUNCH_CHECK();
-        }
+        if (p.chunk_splits > 1) return launch_join<TYPE, true>(a, rows, stream);
     }
     return MX_OK;
 }
@@ -1172,7 +1206,9 @@ extern "C" size_t mx_cache_attention_workspace_bytes(mx_cache c, int64_t tokens,
     if (cache_status(c) != MX_OK || !attention_args_ok(c, tokens, requests, heads_q, max_new, max_len) ||
         !attention_supported(c, tokens, requests, heads_q))
         return 0;
-    return plan_of(c, tokens, requests, heads_q, max_new, max_len).bytes;
+    const size_t a = plan_of(c, MX_F32, tokens, requests, heads_q, max_new, max_len).bytes;
+    const size_t b = plan_of(c, MX_BF16, tokens, requests, heads_q, max_new, max_len).bytes;
+    return a > b ? a : b;                             // the same buffer serves calls of either type
 }
 
 extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32_t heads_q, mx_cache c,
@@ -1200,7 +1236,7 @@ extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tok
     if (st != MX_OK) return st;
     if (!attention_supported(c, tokens, requests, heads_q) || width > INT32_MAX / c.page) return MX_ERR_UNSUPPORTED;
     if (tokens == 0) return MX_OK;
-    const Plan p = plan_of(c, tokens, requests, heads_q, max_new, max_len);
+    const Plan p = plan_of(c, type, tokens, requests, heads_q, max_new, max_len);
     if ((int64_t)p.tiles * c.heads * (p.chunk_splits > 1 ? kTileRows : 1) > INT32_MAX) return MX_ERR_UNSUPPORTED;
     CacheAttnArgs a{};
     a.q = q; a.out = out; a.ldq = ldq; a.ldo = ldo;
