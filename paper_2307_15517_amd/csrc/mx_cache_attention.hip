@@ -27,6 +27,7 @@ struct CacheAttnArgs {
     const int32_t* kv_len;
     float* part_o;             // [part row][split][dim], unnormalised
     float2* part_ml;           // [part row][split]: row maximum (exp2 domain), row sum
+    uint32_t* counters;        // of the workgroups of a unit that have stored their part; zero between calls
     int64_t tokens;
     int64_t max_keys;          // width * page
     uint32_t pages;
@@ -37,6 +38,7 @@ struct CacheAttnArgs {
     int32_t least, most;       // this launch takes the requests that have least .. most rows (token, head of a group)
     int32_t part_rows;         // part rows per unit; a request with more rows is not split
     int32_t tiles;             // cache_chunk_kernel: row tiles of all requests, at most
+    int32_t join;              // the workgroup of a unit that comes last joins its parts; else a launch of its own does
     int32_t fill;              // this launch writes the zeros of tokens outside every request
     int32_t vec_q, vec_o;      // rows of q / out allow 16-byte (bfloat16 out: 8-byte) accesses
     float c;                   // |scale| * log2(e)
@@ -187,6 +189,90 @@ struct Pieces {
     static constexpr int Q = TYPE == MX_F32 ? 3 : 1, P = TYPE == MX_F32 ? 3 : 2;
 };
 
+// Parts of a row's result pass between workgroups that may sit behind different L2 caches: they are written through to and read
+// from the level that all compute units share (device scope), so that no cache has to be written back or invalidated as a whole.
+constexpr int kDeviceScope = 0x10;
+constexpr int kMaxSplits = 64;
+
+// The parts of `rows` rows (16 or, with 32 lanes a row, eight at a time), `splits` each, of a unit whose workgroups have all
+// stored theirs: o = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m).  Called by the 256 threads of the workgroup that came last; the
+// order of the additions is given by the sizes, not by the order of arrival.  32 lanes take four elements each of a row; the eight
+// groups of 32 share a row's splits when there are fewer rows than groups.
+template <typename Store>
+__device__ __forceinline__ void join_parts(const CacheAttnArgs& a, int64_t part_row, int rows, float4 (*lds)[32], Store store) {
+    const int group = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int share = 8;                                                        // groups per row
+    while (share > 1 && rows * share > 8) share >>= 1;
+    const BufRsrc ro = make_rsrc(a.part_o + part_row * a.splits * a.dim, (uint32_t)(rows * a.splits * a.dim * 4));
+    const BufRsrc rm = make_rsrc(a.part_ml + part_row * a.splits, (uint32_t)(rows * a.splits * 8));
+    const int d = 4 * lane < a.dim ? 4 * lane : 0;
+    for (int r0 = 0; r0 < rows; r0 += 8 / share) {
+        const int row = min(r0 + group / share, rows - 1), first = group & (share - 1);
+        float m[2], l[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const int s = lane + 32 * x;
+            const auto t = __builtin_amdgcn_raw_buffer_load_b64(rm, (row * a.splits + min(s, a.splits - 1)) * 8, 0, kDeviceScope);
+            m[x] = s < a.splits ? __uint_as_float(t[0]) : -__builtin_inff();
+            l[x] = __uint_as_float(t[1]);
+        }
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        float top = __builtin_fmaxf(m[0], m[1]);
+#pragma unroll
+        for (int e = 1; e < 32; e *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, e, 32));
+        const float f0 = m[0] == -__builtin_inff() ? 0.f : exp2_of(m[0] - top), f1 = m[1] == -__builtin_inff() ? 0.f : exp2_of(m[1] - top);
+        float sum = (m[0] == -__builtin_inff() ? 0.f : l[0] * f0) + (m[1] == -__builtin_inff() ? 0.f : l[1] * f1);
+#pragma unroll
+        for (int e = 1; e < 32; e *= 2) sum += __shfl_xor(sum, e, 32);
+        for (int s0 = first; s0 < a.splits; s0 += 8 * share) {
+            v4u y[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                y[u] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(ro, ((row * a.splits + min(s0 + u * share, a.splits - 1)) * a.dim + d) * 4, 0, kDeviceScope));
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int s = s0 + u * share;
+                const float w0 = __shfl(s < 32 ? f0 : f1, s & 31, 32);
+                if (s < a.splits) {
+                    x.x += __uint_as_float(y[u][0]) * w0; x.y += __uint_as_float(y[u][1]) * w0;
+                    x.z += __uint_as_float(y[u][2]) * w0; x.w += __uint_as_float(y[u][3]) * w0;
+                }
+            }
+        }
+        if (share > 1) {
+            __syncthreads();
+            lds[group][lane] = x;
+            __syncthreads();
+            if (first == 0)
+                for (int g = 1; g < share; ++g) {
+                    const float4 y = lds[group + g][lane];
+                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                }
+        }
+        if (first == 0 && r0 + group / share < rows && 4 * lane < a.dim) {
+            const float inv = sum > 0.f ? 1.f / sum : 0.f;
+            const float o[4] = {x.x * inv, x.y * inv, x.z * inv, x.w * inv};
+            store(row, 4 * lane, o);
+        }
+    }
+}
+
+// Counts this workgroup in after its parts are stored; true in the one that comes last, which also clears the counter.
+__device__ __forceinline__ bool came_last(uint32_t* counter, int splits, uint32_t* flag) {
+    // this thread's parts have been written through (the wait), then every thread's (the barrier), then the arrival is counted
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const uint32_t old = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *flag = old == (uint32_t)(splits - 1);
+        if (*flag) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+    return *flag != 0;
+}
+
 template <int DT, int BLOCK>
 struct KeyBlock {
     static constexpr int KC = DT / 64;                            // MXInt: 16-byte chunks of a key per lane
@@ -203,8 +289,9 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
     constexpr int EB = BLOCK == 0 ? 2 : 1;
     constexpr int QP = Pieces<TYPE>::Q, P = Pieces<TYPE>::P;
     using Block = KeyBlock<DT, BLOCK>;
-    __shared__ float lds_o[4][16][DT + 4];
+    __shared__ __attribute__((aligned(16))) float lds_o[4][16][DT + 4];
     __shared__ float2 lds_ml[4][16];
+    __shared__ uint32_t flag;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int n = lane & 15, g = lane >> 4;
     if (a.fill) fill_padding<TYPE>(a);
@@ -252,7 +339,6 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
         for (int j = 0; j < NJ; ++j) o[j] = v4f{0.f, 0.f, 0.f, 0.f};
 
         // The two runs of sixteen keys of a block lie in one page each; a run past the end reads the last one again (masked).
-        // A block's loads are issued while the one before is computed on; there is one past the end, so that no load is conditional.
         const int last_run = (len - 1) & ~15;
         PageWindow pages(a, b, len);
         auto load = [&](Block& f, int kb) __attribute__((always_inline)) {
@@ -396,18 +482,10 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
                 if constexpr (BLOCK != 0) __builtin_amdgcn_sched_barrier(0);
             }
         };
-        int kb = begin + 32 * wave;
-        if (kb < stop) {
-            Block f0, f1;
-            load(f0, kb);
-            for (;;) {
-                load(f1, kb + 128);
-                compute(f0, kb);
-                if ((kb += 128) >= stop) break;
-                load(f0, kb + 128);
-                compute(f1, kb);
-                if ((kb += 128) >= stop) break;
-            }
+        for (int kb = begin + 32 * wave; kb < stop; kb += 128) {
+            Block f;
+            load(f, kb);
+            compute(f, kb);
         }
 
         // the four waves join: lane (n, g) holds row n, elements VE*(4g + e) + j
@@ -442,14 +520,24 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
                 for (int j = 0; j < VE; ++j) acc[j] *= inv;
                 store_out<TYPE, VE>(a, (int64_t)(rq.t0 + tk) * a.ldo + (int64_t)hd * dim + VE * part, acc);
             } else {
-                const int64_t at = ((int64_t)unit * a.part_rows + row) * a.splits + split;
-                if (part == 0) a.part_ml[at] = make_float2(mm, ll);
+                const int at = row * splits + split;
+                const int64_t rows0 = (int64_t)unit * a.part_rows * splits;
+                const BufRsrc ro = make_rsrc(a.part_o + rows0 * dim, (uint32_t)(rows * splits * dim * 4));
+                const BufRsrc rm = make_rsrc(a.part_ml + rows0, (uint32_t)(rows * splits * 8));
+                if (part == 0) __builtin_amdgcn_raw_buffer_store_b64(v2u{__float_as_uint(mm), __float_as_uint(ll)}, rm, at * 8, 0, kDeviceScope);
 #pragma unroll
                 for (int j = 0; j < VE; j += 4)
-                    *reinterpret_cast<float4*>(a.part_o + at * dim + VE * part + j) = make_float4(acc[j], acc[j + 1], acc[j + 2], acc[j + 3]);
+                    __builtin_amdgcn_raw_buffer_store_b128(v4u{__float_as_uint(acc[j]), __float_as_uint(acc[j + 1]), __float_as_uint(acc[j + 2]), __float_as_uint(acc[j + 3])},
+                                                           ro, (at * dim + VE * part + j) * 4, 0, kDeviceScope);
             }
         }
     }
+    if (splits == 1 || !a.join) return;
+    if (!came_last(a.counters + unit, splits, &flag)) return;
+    join_parts(a, (int64_t)unit * a.part_rows, rows, reinterpret_cast<float4(*)[32]>(&lds_o[0][0][0]), [&](int row, int d, const float (&x)[4]) {
+        const int tk = row / a.group, hd = h * a.group + (row - tk * a.group);
+        store_out<TYPE, 4>(a, (int64_t)(rq.t0 + tk) * a.ldo + (int64_t)hd * dim + d, x);
+    });
 }
 
 // ---- many rows: chunks and prompts ----------------------------------------------------------------------
@@ -1003,8 +1091,6 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kerne
 // o = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), in an order that the number of splits gives, whatever order they ended in.
 // 32 lanes take a row, four elements each; with many splits the eight groups of a workgroup share a row (GROUPS 8), with few they
 // take eight rows.
-constexpr int kMaxSplits = 64;
-
 template <int TYPE, bool CHUNK, int GROUPS>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
     __shared__ float4 lds[GROUPS == 8 ? 8 : 1][32];
@@ -1140,6 +1226,7 @@ template <int TYPE, int DT, int BLOCK>
 mx_status launch_kernels(CacheAttnArgs a, const Plan& p, uint8_t* workspace, hipStream_t stream) {
     const int64_t units = (int64_t)a.requests * a.heads;
     a.fill = 1;
+    a.counters = (uint32_t*)workspace;
     if (p.decode) {
         a.least = 1;
         a.most = p.chunk ? kFewRows : INT32_MAX;
@@ -1148,13 +1235,15 @@ mx_status launch_kernels(CacheAttnArgs a, const Plan& p, uint8_t* workspace, hip
         const int64_t rows = units * p.part_rows;
         a.part_o = (float*)(workspace + kCounterBytes);
         a.part_ml = (float2*)(a.part_o + rows * p.splits * a.dim);
+        a.join = p.part_rows * p.splits <= 128;
         cache_decode_kernel<TYPE, DT, BLOCK><<<(unsigned)(units * p.splits), 256, 0, stream>>>(a);
         MX_HIP_LAUNCH_CHECK();
         a.fill = 0;
-        if (p.splits > 1) {
+        if (p.splits > 1 && !a.join) {
             const mx_status st = launch_join<TYPE, false>(a, rows, stream);
             if (st != MX_OK) return st;
         }
+
     }
     if (p.chunk) {
         a.least = p.decode ? kFewRows + 1 : 1;
