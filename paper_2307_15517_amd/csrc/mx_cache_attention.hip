@@ -38,6 +38,7 @@ struct CacheAttnArgs {
     int32_t least, most;       // this launch takes the requests that have least .. most rows (token, head of a group)
     int32_t part_rows;         // part rows per unit; a request with more rows is not split
     int32_t tiles;             // cache_chunk_kernel: row tiles of all requests, at most
+    int32_t sorted;            // cache_decode_kernel: the longest requests go first
     int32_t join;              // the workgroup of a unit that comes last joins its parts; else a launch of its own does
     int32_t fill;              // this launch writes the zeros of tokens outside every request
     int32_t vec_q, vec_o;      // rows of q / out allow 16-byte (bfloat16 out: 8-byte) accesses
@@ -283,6 +284,18 @@ struct KeyBlock {
     int ve[8];
 };
 
+// The request that is number n by length (at most 64 of them; equal lengths in their order).
+__device__ __forceinline__ int nth_longest(const CacheAttnArgs& a, int n) {
+    const int lane = threadIdx.x & 63;
+    const int len = lane < a.requests ? a.kv_len[lane] : INT_MIN;
+    int rank = 0;
+    for (int j = 0; j < a.requests; ++j) {
+        const int other = __builtin_amdgcn_readlane(len, j);
+        rank += other > len || (other == len && j < lane);
+    }
+    return __builtin_ctzll(__ballot(rank == n && lane < a.requests));
+}
+
 template <int TYPE, int DT, int BLOCK>
 __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
     constexpr int NS = DT / 32, NJ = DT / 16, VE = DT / 16;
@@ -298,7 +311,9 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
 
     const int split = blockIdx.x % a.splits;
     const int unit = blockIdx.x / a.splits;
-    const int h = unit % a.heads, b = unit / a.heads;
+    const int h = unit % a.heads;
+    int b = unit / a.heads;
+    if (a.sorted) b = nth_longest(a, b);
     const Request rq = request_of(a, b);
     const int rows = rq.n * a.group;
     if (rows < a.least || rows > a.most) return;
@@ -1104,8 +1119,9 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
         if (t.b < 0) return;
         b = t.b;
         r += t.index * kTileRows;
-    } else if (b >= a.requests) {
-        return;
+    } else {
+        if (b >= a.requests) return;
+        if (a.sorted) b = nth_longest(a, b);
     }
     const Request rq = request_of(a, b);
     const int64_t rows = (int64_t)rq.n * a.group;
@@ -1209,7 +1225,9 @@ Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, 
     p.part_rows = (int)(most < kFewRows ? most : kFewRows);
     auto clamp = [](int64_t v, int64_t hi) { return (int)(v > hi ? (hi < 1 ? 1 : hi) : v < 1 ? 1 : v); };
     const int64_t units = requests * c.heads;
-    p.splits = units > 0 ? clamp(1024 / units, ceil_div(max_len, 256)) : 1;
+    // as many workgroups as the GPU holds at once, but no run of keys over 4096, which would leave the last ones alone at the end
+    const int64_t slots = type == MX_F32 ? 512 : 768, even = units > 0 ? slots / units : 1, fine = ceil_div(max_len, 4096);
+    p.splits = units <= kCounterBytes / 4 ? clamp(even > fine ? even : fine, ceil_div(max_len, 256)) : 1;
     p.splits = p.splits > kMaxSplits ? kMaxSplits : p.splits;
     const int64_t rows = tokens * group;
     const int64_t big = p.decode ? (rows / (kFewRows + 1) < requests ? rows / (kFewRows + 1) : requests) : 1;   // requests with more rows
@@ -1236,6 +1254,7 @@ mx_status launch_kernels(CacheAttnArgs a, const Plan& p, uint8_t* workspace, hip
         a.part_o = (float*)(workspace + kCounterBytes);
         a.part_ml = (float2*)(a.part_o + rows * p.splits * a.dim);
         a.join = p.part_rows * p.splits <= 128;
+        a.sorted = a.requests > 1 && a.requests <= 64 && units * p.splits > 512;
         cache_decode_kernel<TYPE, DT, BLOCK><<<(unsigned)(units * p.splits), 256, 0, stream>>>(a);
         MX_HIP_LAUNCH_CHECK();
         a.fill = 0;
