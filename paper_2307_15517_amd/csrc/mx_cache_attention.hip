@@ -297,7 +297,7 @@ __device__ __forceinline__ int nth_longest(const CacheAttnArgs& a, int n) {
 }
 
 template <int TYPE, int DT, int BLOCK>
-__global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
+__device__ __forceinline__ void decode(const CacheAttnArgs& a) {
     constexpr int NS = DT / 32, NJ = DT / 16, VE = DT / 16;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
     constexpr int QP = Pieces<TYPE>::Q, P = Pieces<TYPE>::P;
@@ -307,7 +307,6 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
     __shared__ uint32_t flag;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int n = lane & 15, g = lane >> 4;
-    if (a.fill) fill_padding<TYPE>(a);
 
     const int split = blockIdx.x % a.splits;
     const int unit = blockIdx.x / a.splits;
@@ -555,6 +554,12 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
     });
 }
 
+template <int TYPE, int DT, int BLOCK>
+__global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
+    decode<TYPE, DT, BLOCK>(a);
+    if (a.fill) fill_padding<TYPE>(a);     // last: its loads would hold up everything else
+}
+
 // ---- many rows: chunks and prompts ----------------------------------------------------------------------
 // A workgroup takes 128 rows (token, head of the group) of one request and key/value head, a wave 32 of them, q in registers;
 // K and V pass through LDS in tiles of 64 keys.  S^T = K Q^T puts a row in a lane's column, so that its maximum and sum take one
@@ -572,17 +577,20 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
 // keys.  fp32 activations: three bfloat16 pieces of q and of the probabilities, V as it is.
 constexpr int kTileRows = 128, kTileKeys = 64;
 
-// The request and its tile of rows that tile number `tile` is; b < 0: none.  Every wave looks for itself, 64 requests at a time.
+// The request that tile number `tile` belongs to, and which of its tiles of rows it is; b < 0: none.  Every wave looks for itself, 64
+// requests at a time.
 struct Tile {
     int b, index;
+    Request rq;
 };
 __device__ __forceinline__ Tile find_tile(const CacheAttnArgs& a, int tile) {
     const int lane = threadIdx.x & 63;
     int before = 0;
     for (int base = 0; base < a.requests; base += 64) {
         int count = 0;
+        Request r{0, 0, 0};
         if (base + lane < a.requests) {
-            const Request r = request_of(a, base + lane);
+            r = request_of(a, base + lane);
             const int64_t rows = (int64_t)r.n * a.group;
             if (rows >= a.least && rows <= a.most) count = (int)((rows + kTileRows - 1) / kTileRows);
         }
@@ -595,11 +603,12 @@ __device__ __forceinline__ Tile find_tile(const CacheAttnArgs& a, int tile) {
         const uint64_t past = __ballot(before + upto > tile);
         if (past != 0) {
             const int at = __builtin_ctzll(past);
-            return Tile{base + at, tile - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(count, at))};
+            const int index = tile - before - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(count, at));
+            return Tile{base + at, index, Request{__builtin_amdgcn_readlane(r.t0, at), __builtin_amdgcn_readlane(r.n, at), __builtin_amdgcn_readlane(r.len, at)}};
         }
         before += __builtin_amdgcn_readlane(upto, 63);
     }
-    return Tile{-1, 0};
+    return Tile{-1, 0, Request{0, 0, 0}};
 }
 
 // LDS tile of keys by DT elements, rows without padding, 16-byte chunks placed so that neither the reads of K (32 keys, one
@@ -677,7 +686,7 @@ constexpr float kLag = 8.f;            // the maximum that they are taken agains
 constexpr int kLeastExponent = -40;    // of a run of V
 
 template <int TYPE, int DT, int BLOCK>
-__global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kernel(CacheAttnArgs a) {
+__device__ __forceinline__ void chunk(const CacheAttnArgs& a) {
     constexpr bool HALF = TYPE == MX_BF16;
     constexpr int QP = Pieces<TYPE>::Q, P = HALF ? 1 : 3;
     constexpr int NK = DT / 16, ND = DT / 32;
@@ -689,7 +698,6 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kerne
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int i = lane & 31, h2 = lane >> 5;
-    if (a.fill) fill_padding<TYPE>(a);
 
     // Workgroup u runs on XCD u % 8: with a multiple of eight heads an XCD takes whole heads, so that its L2 holds few of them.
     // The tiles with the most keys go first.
@@ -707,7 +715,7 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kerne
     const Tile tile = find_tile(a, tile_id);
     if (tile.b < 0) return;
     const int b = tile.b;
-    const Request rq = request_of(a, b);
+    const Request rq = tile.rq;
     const int rows = rq.n * a.group, r0 = tile.index * kTileRows;
     const int len = rq.len, dim = a.dim;
 
@@ -1100,6 +1108,12 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kerne
                 }
             }
     }
+}
+
+template <int TYPE, int DT, int BLOCK>
+__global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kernel(CacheAttnArgs a) {
+    chunk<TYPE, DT, BLOCK>(a);
+    if (a.fill) fill_padding<TYPE>(a);
 }
 
 // ---- joining the splits ---------------------------------------------------------------------------------

@@ -127,20 +127,18 @@ def status_string(status: int) -> str:
     return load().mx_status_string(int(status)).decode()
 
 
-def _stream(stream) -> ctypes.c_void_p:
+# Handles and pointers go to ctypes as plain integers (the declared argument types make pointers of them): an object per pointer
+# costs a third of a microsecond, and a call of a serving step has a dozen.
+def _stream(stream) -> int:
     if stream is None:                    # the raw handle: a torch.cuda.Stream object costs 2.8 us per call to make
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, torch.cuda.Stream):
-        return ctypes.c_void_p(stream.cuda_stream)
-    return ctypes.c_void_p(int(stream))
+        return stream.cuda_stream
+    return int(stream)
 
 
-def _p(t) -> ctypes.c_void_p:
-    if t is None:
-        return ctypes.c_void_p(0)
-    if isinstance(t, int):
-        return ctypes.c_void_p(t)
-    return ctypes.c_void_p(t.data_ptr())
+def _p(t) -> Optional[int]:
+    return t.data_ptr() if isinstance(t, torch.Tensor) else t
 
 
 def _raise(status: int, what: str):
@@ -295,16 +293,6 @@ def mx_linear_static_workspace_max() -> int:
     return int(load().mx_linear_static_workspace_max())
 
 
-# The calls of a serving step run many times a second on few tokens, so their pointers go to ctypes as plain integers: an
-# object per pointer costs as much as a small kernel runs.
-def _at(t):
-    return t.data_ptr() if isinstance(t, torch.Tensor) else t
-
-
-def _raw_stream(stream):
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else _stream(stream)
-
-
 def mx_cache_data_bytes(c: mx_cache) -> int:
     return int(load().mx_cache_data_bytes(c))
 
@@ -313,10 +301,17 @@ def mx_cache_exps_bytes(c: mx_cache) -> int:
     return int(load().mx_cache_exps_bytes(c))
 
 
+# The three calls of a serving step: with tensors for all arrays (no integers or None among them) nothing is asked about them.
 def mx_cache_plan(ctx_len, new_len, requests, page, free_pages, n_free, table, width, tokens, q_start, kv_len, slots,
                   positions, counts, stream=None, check: bool = True) -> int:
-    s = load().mx_cache_plan(_at(ctx_len), _at(new_len), requests, page, _at(free_pages), n_free, _at(table), width, tokens,
-                             _at(q_start), _at(kv_len), _at(slots), _at(positions), _at(counts), _raw_stream(stream))
+    h = _stream(stream)
+    try:
+        s = _lib.mx_cache_plan(ctx_len.data_ptr(), new_len.data_ptr(), requests, page, free_pages.data_ptr(), n_free,
+                               table.data_ptr(), width, tokens, q_start.data_ptr(), kv_len.data_ptr(), slots.data_ptr(),
+                               positions.data_ptr(), counts.data_ptr(), h)
+    except AttributeError:
+        s = load().mx_cache_plan(_p(ctx_len), _p(new_len), requests, page, _p(free_pages), n_free, _p(table), width, tokens,
+                                 _p(q_start), _p(kv_len), _p(slots), _p(positions), _p(counts), h)
     if check:
         _raise(s, "mx_cache_plan")
     return s
@@ -324,8 +319,13 @@ def mx_cache_plan(ctx_len, new_len, requests, page, free_pages, n_free, table, w
 
 def mx_cache_append(k, v, type, tokens, ldk, ldv, c, k_data, k_exps, v_data, v_exps, slots, stream=None,
                     check: bool = True) -> int:
-    s = load().mx_cache_append(_at(k), _at(v), type, tokens, ldk, ldv, c, _at(k_data), _at(k_exps), _at(v_data), _at(v_exps),
-                               _at(slots), _raw_stream(stream))
+    h = _stream(stream)
+    try:
+        s = _lib.mx_cache_append(k.data_ptr(), v.data_ptr(), type, tokens, ldk, ldv, c, k_data.data_ptr(), k_exps.data_ptr(),
+                                 v_data.data_ptr(), v_exps.data_ptr(), slots.data_ptr(), h)
+    except AttributeError:
+        s = load().mx_cache_append(_p(k), _p(v), type, tokens, ldk, ldv, c, _p(k_data), _p(k_exps), _p(v_data), _p(v_exps),
+                                   _p(slots), h)
     if check:
         _raise(s, "mx_cache_append")
     return s
@@ -338,9 +338,16 @@ def mx_cache_attention_workspace_bytes(c: mx_cache, tokens: int, requests: int, 
 
 def mx_cache_attention(q, type, tokens, ldq, heads_q, c, k_data, k_exps, v_data, v_exps, table, width, q_start, kv_len,
                        requests, max_new, max_len, scale, workspace, out, ldo, stream=None, check: bool = True) -> int:
-    s = load().mx_cache_attention(_at(q), type, tokens, ldq, heads_q, c, _at(k_data), _at(k_exps), _at(v_data), _at(v_exps),
-                                  _at(table), width, _at(q_start), _at(kv_len), requests, max_new, max_len, scale,
-                                  _at(workspace), _at(out), ldo, _raw_stream(stream))
+    h = _stream(stream)
+    try:
+        s = _lib.mx_cache_attention(q.data_ptr(), type, tokens, ldq, heads_q, c, k_data.data_ptr(), k_exps.data_ptr(),
+                                    v_data.data_ptr(), v_exps.data_ptr(), table.data_ptr(), width, q_start.data_ptr(),
+                                    kv_len.data_ptr(), requests, max_new, max_len, scale, workspace.data_ptr(), out.data_ptr(),
+                                    ldo, h)
+    except AttributeError:
+        s = load().mx_cache_attention(_p(q), type, tokens, ldq, heads_q, c, _p(k_data), _p(k_exps), _p(v_data), _p(v_exps),
+                                      _p(table), width, _p(q_start), _p(kv_len), requests, max_new, max_len, scale,
+                                      _p(workspace), _p(out), ldo, h)
     if check:
         _raise(s, "mx_cache_attention")
     return s
