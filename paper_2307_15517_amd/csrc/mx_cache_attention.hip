@@ -40,7 +40,6 @@ struct CacheAttnArgs {
     int32_t tiles;             // cache_chunk_kernel: row tiles of all requests, at most
     int32_t sorted;            // cache_decode_kernel: the longest requests go first
     int32_t join;              // the workgroup of a unit that comes last joins its parts; else a launch of its own does
-    int32_t fill;              // this launch writes the zeros of tokens outside every request
     int32_t vec_q, vec_o;      // rows of q / out allow 16-byte (bfloat16 out: 8-byte) accesses
     float c;                   // |scale| * log2(e)
     uint32_t flip;             // sign bit of the scale: carried by q
@@ -296,20 +295,24 @@ __device__ __forceinline__ int nth_longest(const CacheAttnArgs& a, int n) {
     return __builtin_ctzll(__ballot(rank == n && lane < a.requests));
 }
 
+template <int DT>
+struct DecodeLds {
+    float o[4][16][DT + 4];
+    float2 ml[4][16];
+    uint32_t flag;
+};
+
 template <int TYPE, int DT, int BLOCK>
-__device__ __forceinline__ void decode(const CacheAttnArgs& a) {
+__device__ __forceinline__ void decode(const CacheAttnArgs& a, int index, DecodeLds<DT>& lds) {
     constexpr int NS = DT / 32, NJ = DT / 16, VE = DT / 16;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
     constexpr int QP = Pieces<TYPE>::Q, P = Pieces<TYPE>::P;
     using Block = KeyBlock<DT, BLOCK>;
-    __shared__ __attribute__((aligned(16))) float lds_o[4][16][DT + 4];
-    __shared__ float2 lds_ml[4][16];
-    __shared__ uint32_t flag;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int n = lane & 15, g = lane >> 4;
 
-    const int split = blockIdx.x % a.splits;
-    const int unit = blockIdx.x / a.splits;
+    const int split = index % a.splits;
+    const int unit = index / a.splits;
     const int h = unit % a.heads;
     int b = unit / a.heads;
     if (a.sorted) b = nth_longest(a, b);
@@ -505,27 +508,27 @@ __device__ __forceinline__ void decode(const CacheAttnArgs& a) {
         // the four waves join: lane (n, g) holds row n, elements VE*(4g + e) + j
         l = sum_across_16_32(l);
         __syncthreads();                                                  // the tile before has been read
-        if (g == 0) lds_ml[wave][n] = make_float2(m, l);
+        if (g == 0) lds.ml[wave][n] = make_float2(m, l);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) lds_o[wave][n][VE * (4 * g + e) + j] = o[j][e];
+            for (int j = 0; j < NJ; ++j) lds.o[wave][n][VE * (4 * g + e) + j] = o[j][e];
         __syncthreads();
         const int row = threadIdx.x >> 4, part = threadIdx.x & 15;
         if (r0 + row < rows && VE * part < dim) {
             float mm = -__builtin_inff();
 #pragma unroll
-            for (int w = 0; w < 4; ++w) mm = __builtin_fmaxf(mm, lds_ml[w][row].x);
+            for (int w = 0; w < 4; ++w) mm = __builtin_fmaxf(mm, lds.ml[w][row].x);
             float ll = 0.f, acc[VE];
 #pragma unroll
             for (int j = 0; j < VE; ++j) acc[j] = 0.f;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float2 ml = lds_ml[w][row];
+                const float2 ml = lds.ml[w][row];
                 const float f = ml.x == -__builtin_inff() ? 0.f : exp2_of(ml.x - mm);
                 ll += ml.y * f;
 #pragma unroll
-                for (int j = 0; j < VE; ++j) acc[j] += lds_o[w][row][VE * part + j] * f;
+                for (int j = 0; j < VE; ++j) acc[j] += lds.o[w][row][VE * part + j] * f;
             }
             if (splits == 1) {
                 const int tk = (r0 + row) / a.group, hd = h * a.group + (r0 + row - tk * a.group);
@@ -547,8 +550,8 @@ __device__ __forceinline__ void decode(const CacheAttnArgs& a) {
         }
     }
     if (splits == 1 || !a.join) return;
-    if (!came_last(a.counters + unit, splits, &flag)) return;
-    join_parts(a, (int64_t)unit * a.part_rows, rows, reinterpret_cast<float4(*)[32]>(&lds_o[0][0][0]), [&](int row, int d, const float (&x)[4]) {
+    if (!came_last(a.counters + unit, splits, &lds.flag)) return;
+    join_parts(a, (int64_t)unit * a.part_rows, rows, reinterpret_cast<float4(*)[32]>(&lds.o[0][0][0]), [&](int row, int d, const float (&x)[4]) {
         const int tk = row / a.group, hd = h * a.group + (row - tk * a.group);
         store_out<TYPE, 4>(a, (int64_t)(rq.t0 + tk) * a.ldo + (int64_t)hd * dim + d, x);
     });
@@ -556,8 +559,9 @@ __device__ __forceinline__ void decode(const CacheAttnArgs& a) {
 
 template <int TYPE, int DT, int BLOCK>
 __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
-    decode<TYPE, DT, BLOCK>(a);
-    if (a.fill) fill_padding<TYPE>(a);     // last: its loads would hold up everything else
+    __shared__ __attribute__((aligned(16))) DecodeLds<DT> lds;
+    decode<TYPE, DT, BLOCK>(a, blockIdx.x, lds);
+    fill_padding<TYPE>(a);     // last: its loads would hold up everything else
 }
 
 // ---- many rows: chunks and prompts ----------------------------------------------------------------------
@@ -686,7 +690,7 @@ constexpr float kLag = 8.f;            // the maximum that they are taken agains
 constexpr int kLeastExponent = -40;    // of a run of V
 
 template <int TYPE, int DT, int BLOCK>
-__device__ __forceinline__ void chunk(const CacheAttnArgs& a) {
+__device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t* smem) {
     constexpr bool HALF = TYPE == MX_BF16;
     constexpr int QP = Pieces<TYPE>::Q, P = HALF ? 1 : 3;
     constexpr int NK = DT / 16, ND = DT / 32;
@@ -695,7 +699,6 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a) {
     constexpr int kVBase = 2 * kTensor, kExp = 4 * kTensor;
     constexpr bool kCopyV = BLOCK == 0 && !HALF;           // V goes to LDS as it is
     constexpr int kLoads = 16 * DT * EB / 1024;            // 16-byte loads per lane that bring a run of sixteen keys
-    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int i = lane & 31, h2 = lane >> 5;
 
@@ -704,12 +707,12 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a) {
     const int per_head = a.tiles * a.splits;
     int h, rest;
     if (a.heads % 8 == 0) {
-        const int j = blockIdx.x / 8;
-        h = blockIdx.x % 8 + 8 * (j / per_head);
+        const int j = index / 8;
+        h = index % 8 + 8 * (j / per_head);
         rest = j % per_head;
     } else {
-        h = blockIdx.x % a.heads;
-        rest = blockIdx.x / a.heads;
+        h = index % a.heads;
+        rest = index / a.heads;
     }
     const int split = rest % a.splits, tile_id = a.tiles - 1 - rest / a.splits;
     const Tile tile = find_tile(a, tile_id);
@@ -1110,10 +1113,13 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a) {
     }
 }
 
+// Requests of many rows and, in the workgroups after `chunks`, of few: in a batch that has both they run side by side.
 template <int TYPE, int DT, int BLOCK>
-__global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_chunk_kernel(CacheAttnArgs a) {
-    chunk<TYPE, DT, BLOCK>(a);
-    if (a.fill) fill_padding<TYPE>(a);
+__global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_mixed_kernel(CacheAttnArgs many, CacheAttnArgs few, int chunks) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    if ((int)blockIdx.x < chunks) chunk<TYPE, DT, BLOCK>(many, blockIdx.x, smem);
+    else decode<TYPE, DT, BLOCK>(few, blockIdx.x - chunks, *reinterpret_cast<DecodeLds<DT>*>(smem));
+    fill_padding<TYPE>(many);
 }
 
 // ---- joining the splits ---------------------------------------------------------------------------------
@@ -1213,7 +1219,7 @@ struct Plan {
     bool decode, chunk;
     int part_rows, splits;         // of cache_decode_kernel
     int tiles, chunk_splits;
-    size_t bytes;
+    size_t few_bytes, bytes;
 };
 
 // Splits of the keys for `groups` workgroups that have `tiles` tiles of 64 keys each to go through, `slots` of which the GPU holds at
@@ -1247,54 +1253,55 @@ Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, 
     const int64_t big = p.decode ? (rows / (kFewRows + 1) < requests ? rows / (kFewRows + 1) : requests) : 1;   // requests with more rows
     p.tiles = p.chunk ? clamp(p.decode ? rows / kTileRows + big : ceil_div(rows, kTileRows), INT32_MAX) : 0;
     p.chunk_splits = p.chunk ? chunk_splits((rows / kTileRows + 1) * c.heads, ceil_div(max_len, kTileKeys), type == MX_F32 ? 256 : 512) : 1;
-    const size_t part = (size_t)c.dim * 4 + 8;
-    const size_t few = p.decode && p.splits > 1 ? (size_t)units * p.part_rows * p.splits * part : 0;
-    const size_t many = p.chunk && p.chunk_splits > 1 ? (size_t)p.tiles * c.heads * kTileRows * p.chunk_splits * part : 0;
-    p.bytes = ((few > many ? few : many) + 255) / 256 * 256 + kCounterBytes;
+    auto part_bytes = [&](size_t rows, int splits) { return splits > 1 ? (rows * splits * ((size_t)c.dim * 4 + 8) + 255) / 256 * 256 : 0; };
+    p.few_bytes = p.decode ? part_bytes((size_t)units * p.part_rows, p.splits) : 0;
+    p.bytes = kCounterBytes + p.few_bytes + (p.chunk ? part_bytes((size_t)p.tiles * c.heads * kTileRows, p.chunk_splits) : 0);
     return p;
 }
 
 template <int TYPE, int DT, int BLOCK>
-mx_status launch_kernels(CacheAttnArgs a, const Plan& p, uint8_t* workspace, hipStream_t stream) {
-    const int64_t units = (int64_t)a.requests * a.heads;
-    a.fill = 1;
-    a.counters = (uint32_t*)workspace;
+mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* workspace, hipStream_t stream) {
+    CacheAttnArgs few = base, many = base;
+    uint8_t* parts = workspace + kCounterBytes;
+    const int64_t units = (int64_t)base.requests * base.heads;
+    int64_t few_rows = 0, many_rows = 0;
     if (p.decode) {
-        a.least = 1;
-        a.most = p.chunk ? kFewRows : INT32_MAX;
-        a.splits = p.splits;
-        a.part_rows = p.part_rows;
-        const int64_t rows = units * p.part_rows;
-        a.part_o = (float*)(workspace + kCounterBytes);
-        a.part_ml = (float2*)(a.part_o + rows * p.splits * a.dim);
-        a.join = p.part_rows * p.splits <= 128;
-        a.sorted = a.requests > 1 && a.requests <= 64 && units * p.splits > 512;
-        cache_decode_kernel<TYPE, DT, BLOCK><<<(unsigned)(units * p.splits), 256, 0, stream>>>(a);
-        MX_HIP_LAUNCH_CHECK();
-        a.fill = 0;
-        if (p.splits > 1 && !a.join) {
-            const mx_status st = launch_join<TYPE, false>(a, rows, stream);
-            if (st != MX_OK) return st;
-        }
-
+        few.least = 1;
+        few.most = p.chunk ? kFewRows : INT32_MAX;
+        few.splits = p.splits;
+        few.part_rows = p.part_rows;
+        few.counters = (uint32_t*)workspace;
+        few_rows = units * p.part_rows;
+        few.part_o = (float*)parts;
+        few.part_ml = (float2*)(few.part_o + few_rows * p.splits * base.dim);
+        few.join = p.part_rows * p.splits <= 128;
+        few.sorted = base.requests > 1 && base.requests <= 64 && units * p.splits > 512;
+        parts += p.few_bytes;
     }
     if (p.chunk) {
-        a.least = p.decode ? kFewRows + 1 : 1;
-        a.most = INT32_MAX;
-        a.splits = p.chunk_splits;
-        a.tiles = p.tiles;
-        a.part_rows = kTileRows;
-        const int64_t rows = (int64_t)p.tiles * a.heads * kTileRows;
-        a.part_o = (float*)(workspace + kCounterBytes);
-        a.part_ml = (float2*)(a.part_o + rows * p.chunk_splits * a.dim);
+        many.least = p.decode ? kFewRows + 1 : 1;
+        many.most = INT32_MAX;
+        many.splits = p.chunk_splits;
+        many.tiles = p.tiles;
+        many.part_rows = kTileRows;
+        many_rows = (int64_t)p.tiles * base.heads * kTileRows;
+        many.part_o = (float*)parts;
+        many.part_ml = (float2*)(many.part_o + many_rows * p.chunk_splits * base.dim);
         constexpr int lds = 4 * kTileKeys * DT * 2 + 32;
+        static_assert(sizeof(DecodeLds<DT>) <= lds, "both share the workgroup's LDS");
         static std::atomic<uint64_t> raised{0};
-        if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_chunk_kernel<TYPE, DT, BLOCK>, lds, raised)) return MX_ERR_DEVICE;
-        cache_chunk_kernel<TYPE, DT, BLOCK><<<(unsigned)((int64_t)p.tiles * a.heads * p.chunk_splits), 256, lds, stream>>>(a);
-        MX_HIP_LAUNCH_CHECK();
-        if (p.chunk_splits > 1) return launch_join<TYPE, true>(a, rows, stream);
+        if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_mixed_kernel<TYPE, DT, BLOCK>, lds, raised)) return MX_ERR_DEVICE;
+        const int64_t chunks = (int64_t)p.tiles * base.heads * p.chunk_splits;
+        cache_mixed_kernel<TYPE, DT, BLOCK><<<(unsigned)(chunks + (p.decode ? units * p.splits : 0)), 256, lds, stream>>>(many, few, (int)chunks);
+    } else {
+        cache_decode_kernel<TYPE, DT, BLOCK><<<(unsigned)(units * p.splits), 256, 0, stream>>>(few);
     }
-    return MX_OK;
+    MX_HIP_LAUNCH_CHECK();
+    if (p.decode && p.splits > 1 && !few.join) {
+        const mx_status st = launch_join<TYPE, false>(few, few_rows, stream);
+        if (st != MX_OK) return st;
+    }
+    return p.chunk && p.chunk_splits > 1 ? launch_join<TYPE, true>(many, many_rows, stream) : MX_OK;
 }
 
 template <int TYPE>
