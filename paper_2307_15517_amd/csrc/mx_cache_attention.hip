@@ -1124,17 +1124,18 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_mixed_kerne
 
 // ---- joining the splits ---------------------------------------------------------------------------------
 // o = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), in an order that the number of splits gives, whatever order they ended in.
-// 32 lanes take a row, four elements each; with many splits the eight groups of a workgroup share a row (GROUPS 8), with few they
-// take eight rows.
-template <int TYPE, bool CHUNK, int GROUPS>
+// 32 lanes take a row, four elements each.  Many splits: a workgroup a row, its eight groups of 32 sharing the splits.  Few splits of a
+// tile: a workgroup 32 rows, a group four of them at a time (eight rows, one a group, took 3 us longer for 44 tiles of 8 heads,
+// most of it finding the tile; the last workgroup to arrive joining a tile, 8).
+template <int TYPE, bool CHUNK>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
-    __shared__ float4 lds[GROUPS == 8 ? 8 : 1][32];
+    __shared__ float4 lds[8][32];
     const int group = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t prow = GROUPS == 8 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 8 + group;
+    const int64_t prow = blockIdx.x;
     const int unit = (int)(prow / a.part_rows), row = (int)(prow - (int64_t)unit * a.part_rows);
     const int h = unit % a.heads;
     int b = unit / a.heads, r = row;
-    if constexpr (CHUNK) {                            // part_rows is 128, so the rows of a workgroup are of one unit
+    if constexpr (CHUNK) {
         const Tile t = find_tile(a, b);
         if (t.b < 0) return;
         b = t.b;
@@ -1164,26 +1165,24 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
     const float4* p = reinterpret_cast<const float4*>(a.part_o + prow * a.splits * a.dim + (d < a.dim ? d : 0));
     const int stride = a.dim / 4;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = GROUPS == 8 ? group : 0; s0 < a.splits; s0 += 8 * GROUPS) {
+    for (int s0 = group; s0 < a.splits; s0 += 64) {
         float4 y[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) y[u] = p[(int64_t)min(s0 + u * GROUPS, a.splits - 1) * stride];
+        for (int u = 0; u < 8; ++u) y[u] = p[(int64_t)min(s0 + u * 8, a.splits - 1) * stride];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            const int s = s0 + u * GROUPS;
+            const int s = s0 + u * 8;
             const float w0 = __shfl(s < 32 ? f0 : f1, s & 31, 32), w = s < a.splits ? w0 : 0.f;
             x.x += y[u].x * w; x.y += y[u].y * w; x.z += y[u].z * w; x.w += y[u].w * w;
         }
     }
-    if constexpr (GROUPS == 8) {
-        lds[group][lane] = x;
-        __syncthreads();
-        if (group != 0) return;
+    lds[group][lane] = x;
+    __syncthreads();
+    if (group != 0) return;
 #pragma unroll
-        for (int g = 1; g < 8; ++g) {
-            const float4 y = lds[g][lane];
-            x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-        }
+    for (int g = 1; g < 8; ++g) {
+        const float4 y = lds[g][lane];
+        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
     }
     if (d < a.dim) {
         const float inv = ll > 0.f ? 1.f / ll : 0.f;
@@ -1192,10 +1191,63 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
     }
 }
 
+template <int TYPE>
+__global__ __launch_bounds__(256) void cache_join_tiles_kernel(CacheAttnArgs a) {
+    const int group = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int unit = blockIdx.x / (kTileRows / 32), base = blockIdx.x % (kTileRows / 32) * 32;
+    const int h = unit % a.heads;
+    const Tile t = find_tile(a, unit / a.heads);
+    if (t.b < 0) return;
+    const int first = t.index * kTileRows, rows = min(kTileRows, t.rq.n * a.group - first);
+    const int d = 4 * lane < a.dim ? 4 * lane : 0;
+    const int64_t part_row = (int64_t)unit * kTileRows;
+    if (base >= rows) return;
+    float x[4][4], m[4], l[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        m[u] = -__builtin_inff();
+        l[u] = x[u][0] = x[u][1] = x[u][2] = x[u][3] = 0.f;
+    }
+    for (int s0 = 0; s0 < a.splits; s0 += 4) {
+        float4 y[4][4];
+        float2 ml[4][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int64_t at = (part_row + min(base + group + 8 * u, rows - 1)) * a.splits + min(s0 + s, a.splits - 1);
+                ml[u][s] = a.part_ml[at];
+                y[u][s] = *reinterpret_cast<const float4*>(a.part_o + at * a.dim + d);
+            }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if (s0 + s >= a.splits || ml[u][s].x == -__builtin_inff()) continue;      // a split that the row saw nothing of
+                const float top = __builtin_fmaxf(m[u], ml[u][s].x), f = exp2_of(m[u] - top), w = exp2_of(ml[u][s].x - top);
+                m[u] = top;
+                l[u] = l[u] * f + ml[u][s].y * w;
+                x[u][0] = x[u][0] * f + y[u][s].x * w;
+                x[u][1] = x[u][1] * f + y[u][s].y * w;
+                x[u][2] = x[u][2] * f + y[u][s].z * w;
+                x[u][3] = x[u][3] * f + y[u][s].w * w;
+            }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int row = base + group + 8 * u;
+        if (row >= rows || 4 * lane >= a.dim) continue;
+        const int tok = (first + row) / a.group, head = h * a.group + (first + row - tok * a.group);
+        const float inv = l[u] > 0.f ? 1.f / l[u] : 0.f;
+        const float o[4] = {x[u][0] * inv, x[u][1] * inv, x[u][2] * inv, x[u][3] * inv};
+        store_out<TYPE, 4>(a, (int64_t)(t.rq.t0 + tok) * a.ldo + (int64_t)head * a.dim + d, o);
+    }
+}
+
 template <int TYPE, bool CHUNK>
 mx_status launch_join(const CacheAttnArgs& a, int64_t rows, hipStream_t stream) {
-    if (a.splits > 8) cache_join_kernel<TYPE, CHUNK, 8><<<(unsigned)rows, 256, 0, stream>>>(a);
-    else cache_join_kernel<TYPE, CHUNK, 1><<<(unsigned)ceil_div(rows, 8), 256, 0, stream>>>(a);
+    if (CHUNK && a.splits <= 16) cache_join_tiles_kernel<TYPE><<<(unsigned)(rows / 32), 256, 0, stream>>>(a);
+    else cache_join_kernel<TYPE, CHUNK><<<(unsigned)rows, 256, 0, stream>>>(a);
     MX_HIP_LAUNCH_CHECK();
     return MX_OK;
 }
@@ -1274,7 +1326,7 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         few_rows = units * p.part_rows;
         few.part_o = (float*)parts;
         few.part_ml = (float2*)(few.part_o + few_rows * p.splits * base.dim);
-        few.join = p.part_rows * p.splits <= 128;
+        few.join = p.chunk || p.part_rows * p.splits <= 128;      // next to chunks the bound of sixteen rows says little
         few.sorted = base.requests > 1 && base.requests <= 64 && units * p.splits > 512;
         parts += p.few_bytes;
     }
