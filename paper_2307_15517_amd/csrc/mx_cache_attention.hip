@@ -104,8 +104,14 @@ struct PageWindow {
     const int32_t* row_table;
     int base, last, id;        // id: of page `base` + lane, no further than `last`
 
-    __device__ __forceinline__ PageWindow(const CacheAttnArgs& a, int b, int len)
-        : row_table(a.table + (int64_t)b * a.width), base(-64), last((len - 1) >> a.page_log2), id(0) {}
+    // The first window is asked for at once, before the request's length is known (what lies past its pages is not looked at).
+    __device__ __forceinline__ PageWindow(const CacheAttnArgs& a, int b) : row_table(a.table + (int64_t)b * a.width), base(0), last(0), id(0) {
+        if (a.width > 0) id = row_table[min((int)(threadIdx.x & 63), (int)a.width - 1)];
+    }
+    __device__ __forceinline__ void set_length(const CacheAttnArgs& a, int len) {
+        last = (len - 1) >> a.page_log2;
+        asm volatile("" : "+v"(id));               // awaited here, not in the loop
+    }
     // The row of the pool that holds key `key` of the request (and those after it in its run of sixteen): `key` is below its
     // length and the same for all lanes.  A page index outside the pool reads as page 0.
     __device__ __forceinline__ int64_t row(const CacheAttnArgs& a, int h, int key) {
@@ -121,25 +127,46 @@ struct PageWindow {
     }
 };
 
-template <int TYPE>
-__device__ __forceinline__ void load_q(const CacheAttnArgs& a, int64_t at, float (&v)[8]) {
-    if (a.vec_q) load8<TYPE, true>(a.q, at, v);
-    else load8<TYPE, false>(a.q, at, v);
-}
-
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The leading bfloat16 pieces (8 bits, cut) of two floats, which keep the rest
+__device__ __forceinline__ uint32_t cut_piece(float& a, float& b) {
+    const uint32_t w = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+    b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+    return w;
+}
 
 // bfloat16 pieces of a float whose sum is the float's leading 8, 16 or 24 bits; each piece is cut, not rounded, but the last
 template <int P>
 __device__ __forceinline__ void pieces_of(float a, float b, uint32_t (&w)[P]) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        if (p == P - 1) {
-            w[p] = pack_bf16(a, b);
-        } else {
-            w[p] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
-            a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
-            b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+        w[p] = p == P - 1 ? pack_bf16(a, b) : cut_piece(a, b);
+    }
+}
+
+// q of one row as the pieces that a lane holds: N runs of eight elements, run n from element at(n) on (zeros past the head
+// dimension).  The loads of all runs go out together: one branch on the alignment around them, none inside.
+template <int TYPE, int QP, int N, typename At>
+__device__ __forceinline__ void load_q(const CacheAttnArgs& a, int64_t row, At at, v4u (&qf)[QP][N]) {
+    float v[N][8];
+    if (a.vec_q) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) load8<TYPE, true>(a.q, row + (at(n) < a.dim ? at(n) : 0), v[n]);
+    } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n) load8<TYPE, false>(a.q, row + (at(n) < a.dim ? at(n) : 0), v[n]);
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const uint32_t keep = at(n) < a.dim ? 0xffffffffu : 0u;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t w[QP];
+            pieces_of<QP>(__uint_as_float(__float_as_uint(v[n][2 * e]) ^ a.flip), __uint_as_float(__float_as_uint(v[n][2 * e + 1]) ^ a.flip), w);
+#pragma unroll
+            for (int p = 0; p < QP; ++p) qf[p][n][e] = w[p] & keep;
         }
     }
 }
@@ -316,12 +343,14 @@ __device__ __forceinline__ void decode(const CacheAttnArgs& a, int index, Decode
     const int h = unit % a.heads;
     int b = unit / a.heads;
     if (a.sorted) b = nth_longest(a, b);
+    PageWindow pages(a, b);
     const Request rq = request_of(a, b);
     const int rows = rq.n * a.group;
     if (rows < a.least || rows > a.most) return;
     const int splits = rows <= a.part_rows ? a.splits : 1;
     if (split >= splits) return;
     const int len = rq.len;
+    pages.set_length(a, len);
     // this split's run of keys, in whole blocks of 128
     const int per = (((len + 127) >> 7) + splits - 1) / splits;
     const int begin = min(split * per * 128, len), end = min(begin + per * 128, len);
@@ -333,19 +362,6 @@ __device__ __forceinline__ void decode(const CacheAttnArgs& a, int index, Decode
         const int tok = r / a.group, head = h * a.group + (r - tok * a.group);
         const int last = len - rq.n + tok;                                // the last key this row sees
         v4u qf[QP][NS];
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const int d = BLOCK == 0 ? 32 * s + 8 * g : 64 * (s >> 1) + 16 * g + 8 * (s & 1);
-            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (d < dim) load_q<TYPE>(a, (int64_t)(rq.t0 + tok) * a.ldq + (int64_t)head * dim + d, v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t w[QP];
-                pieces_of<QP>(__uint_as_float(__float_as_uint(v[2 * i]) ^ a.flip), __uint_as_float(__float_as_uint(v[2 * i + 1]) ^ a.flip), w);
-#pragma unroll
-                for (int p = 0; p < QP; ++p) qf[p][s][i] = w[p];
-            }
-        }
         // keys past the last one any row of this tile sees are left out
         const int first_last = len - rq.n + r0 / a.group;                 // the last key that all its rows see
         const int stop = min(end, len - rq.n + min(r0 + 15, rows - 1) / a.group + 1);
@@ -357,7 +373,6 @@ __device__ __forceinline__ void decode(const CacheAttnArgs& a, int index, Decode
 
         // The two runs of sixteen keys of a block lie in one page each; a run past the end reads the last one again (masked).
         const int last_run = (len - 1) & ~15;
-        PageWindow pages(a, b, len);
         auto load = [&](Block& f, int kb) __attribute__((always_inline)) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -499,6 +514,9 @@ __device__ __forceinline__ void decode(const CacheAttnArgs& a, int index, Decode
                 if constexpr (BLOCK != 0) __builtin_amdgcn_sched_barrier(0);
             }
         };
+        load_q<TYPE, QP, NS>(a, (int64_t)(rq.t0 + tok) * a.ldq + (int64_t)head * dim,
+                             [&](int n) { return BLOCK == 0 ? 32 * n + 8 * g : 64 * (n >> 1) + 16 * g + 8 * (n & 1); }, qf);
+        // One block in flight per wave: a second one costs a third wave per SIMD (32 ragged sequences 79 us, 84 with it).
         for (int kb = begin + 32 * wave; kb < stop; kb += 128) {
             Block f;
             load(f, kb);
@@ -718,6 +736,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
     const Tile tile = find_tile(a, tile_id);
     if (tile.b < 0) return;
     const int b = tile.b;
+    PageWindow pages(a, b);
     const Request rq = tile.rq;
     const int rows = rq.n * a.group, r0 = tile.index * kTileRows;
     const int len = rq.len, dim = a.dim;
@@ -733,19 +752,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
     const int last = min(len - rq.n + tok, stop - 1);                     // the last key of this split that the row sees
     const int all_see = min(len - rq.n + min(r0 + 32 * wave, rows - 1) / a.group, stop - 1);   // the last one all of the wave's see
     v4u qf[QP][NK];
-#pragma unroll
-    for (int kk = 0; kk < NK; ++kk) {
-        const int d = 16 * kk + 8 * h2;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (d < dim) load_q<TYPE>(a, (int64_t)(rq.t0 + tok) * a.ldq + (int64_t)head * dim + d, v);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t w[QP];
-            pieces_of<QP>(__uint_as_float(__float_as_uint(v[2 * e]) ^ a.flip), __uint_as_float(__float_as_uint(v[2 * e + 1]) ^ a.flip), w);
-#pragma unroll
-            for (int p = 0; p < QP; ++p) qf[p][kk][e] = w[p];
-        }
-    }
+    load_q<TYPE, QP, NK>(a, (int64_t)(rq.t0 + tok) * a.ldq + (int64_t)head * dim, [&](int n) { return 16 * n + 8 * h2; }, qf);
 
     // ---- staging: a wave brings one run of sixteen keys of a stage, which lies in one page -------------------
     // As it is (bfloat16 K, bfloat16 V for fp32 activations): copies from memory straight to LDS, 1 KiB each, lane L's bytes at
@@ -779,7 +786,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
         }
     v4u sk[BLOCK == 0 ? 1 : kLoads], sv[kCopyV ? 1 : kLoads];
     int ek[kLoads], ev[kLoads];
-    PageWindow pages(a, b, len);
+    pages.set_length(a, len);
     auto row_of = [&](int key) __attribute__((always_inline)) { return pages.row(a, h, max(min(key + 16 * wave, last_run), 0)); };
     // K stage t: keys begin + 64t + 32 ..; V stage t: keys begin + 64t ..
     auto load_k = [&](int slot, int key0) __attribute__((always_inline)) {
@@ -1276,7 +1283,7 @@ struct Plan {
 
 // Splits of the keys for `groups` workgroups that have `tiles` tiles of 64 keys each to go through, `slots` of which the GPU holds at
 // once: the fewest rounds times tiles, a workgroup's start and end counting as kStart tiles.  (Two sides, chunk of 300 rows of fp32
-// on 2000 keys, 96 groups: see the table of the design notes.)
+// on 2000 keys, 96 groups.)
 int chunk_splits(int64_t groups, int64_t tiles, int64_t slots) {
     constexpr int kStart = 5;
     int best = 1;
