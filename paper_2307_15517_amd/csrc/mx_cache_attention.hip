@@ -34,7 +34,8 @@ struct CacheAttnArgs {
     int32_t requests, heads, group, heads_q, dim;
     int32_t page_log2;
     int32_t exp_shift;         // an exponent byte e stands for 2^(e - exp_shift) per mantissa unit
-    int32_t splits;            // of this launch
+    int32_t splits;            // of this launch, at most
+    int32_t run;               // cache_chunk_kernel: tiles of keys that a split is given
     int32_t least, most;       // this launch takes the requests that have least .. most rows (token, head of a group)
     int32_t part_rows;         // part rows per unit; a request with more rows is not split
     int32_t tiles;             // cache_chunk_kernel: row tiles of all requests, at most
@@ -633,6 +634,14 @@ __device__ __forceinline__ Tile find_tile(const CacheAttnArgs& a, int tile) {
     return Tile{-1, 0, Request{0, 0, 0}};
 }
 
+// The keys of the request that some row of the tile sees, and the splits that they are given: as many as there are runs of them.
+__device__ __forceinline__ int keys_seen(const CacheAttnArgs& a, const Tile& t) {
+    return max(0, t.rq.len - t.rq.n + min(t.index * kTileRows + kTileRows - 1, t.rq.n * a.group - 1) / a.group + 1);
+}
+__device__ __forceinline__ int splits_of(const CacheAttnArgs& a, int keys) {
+    return max(1, min(((keys + kTileKeys - 1) / kTileKeys + a.run - 1) / a.run, a.splits));
+}
+
 // LDS tile of keys by DT elements, rows without padding, 16-byte chunks placed so that neither the reads of K (32 keys, one
 // chunk each) nor the transposing reads of V (8 keys, 64 bytes each) meet on a bank more often than they must.
 template <int DT>
@@ -742,8 +751,9 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
     const int len = rq.len, dim = a.dim;
 
     // the keys that some row of the tile sees, and this split's run of them in whole tiles
-    const int all = max(0, len - rq.n + min(r0 + kTileRows - 1, rows - 1) / a.group + 1);
-    const int per = (((all + kTileKeys - 1) / kTileKeys) + a.splits - 1) / a.splits * kTileKeys;
+    const int all = keys_seen(a, tile), splits = splits_of(a, all);
+    if (split >= splits) return;
+    const int per = (((all + kTileKeys - 1) / kTileKeys) + splits - 1) / splits * kTileKeys;
     const int begin = min(split * per, all), stop = min(begin + per, all);
 
     // this wave's rows: q is the right operand of the scores, lane (i, h2) row i, elements 16kk + 8h2 ..
@@ -1100,9 +1110,9 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
     if (r0 + 32 * wave + i < rows) {
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
         const float ll = __uint_as_float(both[0]) + __uint_as_float(both[1]);
-        const float inv = a.splits > 1 ? 1.f : ll > 0.f ? 1.f / ll : 0.f;
+        const float inv = splits > 1 ? 1.f : ll > 0.f ? 1.f / ll : 0.f;
         const int64_t prow = (((int64_t)tile_id * a.heads + h) * kTileRows + 32 * wave + i) * a.splits + split;
-        if (a.splits > 1 && h2 == 0) a.part_ml[prow] = make_float2(m, ll);
+        if (splits > 1 && h2 == 0) a.part_ml[prow] = make_float2(m, ll);
         const int64_t to = (int64_t)(rq.t0 + tok) * a.ldo + (int64_t)head * dim;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)
@@ -1113,7 +1123,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[e] = o[dt][4 * q4 + e] * inv;
                 if (d < dim) {
-                    if (a.splits == 1) store_out<TYPE, 4>(a, to + d, x);
+                    if (splits == 1) store_out<TYPE, 4>(a, to + d, x);
                     else *reinterpret_cast<float4*>(a.part_o + prow * dim + d) = make_float4(x[0], x[1], x[2], x[3]);
                 }
             }
@@ -1141,11 +1151,13 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
     const int64_t prow = blockIdx.x;
     const int unit = (int)(prow / a.part_rows), row = (int)(prow - (int64_t)unit * a.part_rows);
     const int h = unit % a.heads;
-    int b = unit / a.heads, r = row;
+    int b = unit / a.heads, r = row, splits = a.splits;
     if constexpr (CHUNK) {
         const Tile t = find_tile(a, b);
         if (t.b < 0) return;
         b = t.b;
+        splits = splits_of(a, keys_seen(a, t));
+        if (splits == 1) return;
         r += t.index * kTileRows;
     } else {
         if (b >= a.requests) return;
@@ -1158,7 +1170,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
 
     float2 ml[2];
 #pragma unroll
-    for (int x = 0; x < 2; ++x) ml[x] = lane + 32 * x < a.splits ? a.part_ml[prow * a.splits + lane + 32 * x] : make_float2(-__builtin_inff(), 0.f);
+    for (int x = 0; x < 2; ++x) ml[x] = lane + 32 * x < splits ? a.part_ml[prow * a.splits + lane + 32 * x] : make_float2(-__builtin_inff(), 0.f);
     float mm = __builtin_fmaxf(ml[0].x, ml[1].x);
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) mm = __builtin_fmaxf(mm, __shfl_xor(mm, d, 32));
@@ -1172,14 +1184,14 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
     const float4* p = reinterpret_cast<const float4*>(a.part_o + prow * a.splits * a.dim + (d < a.dim ? d : 0));
     const int stride = a.dim / 4;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = group; s0 < a.splits; s0 += 64) {
+    for (int s0 = group; s0 < splits; s0 += 64) {
         float4 y[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) y[u] = p[(int64_t)min(s0 + u * 8, a.splits - 1) * stride];
+        for (int u = 0; u < 8; ++u) y[u] = p[(int64_t)min(s0 + u * 8, splits - 1) * stride];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
             const int s = s0 + u * 8;
-            const float w0 = __shfl(s < 32 ? f0 : f1, s & 31, 32), w = s < a.splits ? w0 : 0.f;
+            const float w0 = __shfl(s < 32 ? f0 : f1, s & 31, 32), w = s < splits ? w0 : 0.f;
             x.x += y[u].x * w; x.y += y[u].y * w; x.z += y[u].z * w; x.w += y[u].w * w;
         }
     }
@@ -1208,21 +1220,22 @@ __global__ __launch_bounds__(256) void cache_join_tiles_kernel(CacheAttnArgs a) 
     const int first = t.index * kTileRows, rows = min(kTileRows, t.rq.n * a.group - first);
     const int d = 4 * lane < a.dim ? 4 * lane : 0;
     const int64_t part_row = (int64_t)unit * kTileRows;
-    if (base >= rows) return;
+    const int splits = splits_of(a, keys_seen(a, t));
+    if (base >= rows || splits == 1) return;                               // (of a single split the rows are there)
     float x[4][4], m[4], l[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         m[u] = -__builtin_inff();
         l[u] = x[u][0] = x[u][1] = x[u][2] = x[u][3] = 0.f;
     }
-    for (int s0 = 0; s0 < a.splits; s0 += 4) {
+    for (int s0 = 0; s0 < splits; s0 += 4) {
         float4 y[4][4];
         float2 ml[4][4];
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const int64_t at = (part_row + min(base + group + 8 * u, rows - 1)) * a.splits + min(s0 + s, a.splits - 1);
+                const int64_t at = (part_row + min(base + group + 8 * u, rows - 1)) * a.splits + min(s0 + s, splits - 1);
                 ml[u][s] = a.part_ml[at];
                 y[u][s] = *reinterpret_cast<const float4*>(a.part_o + at * a.dim + d);
             }
@@ -1230,7 +1243,7 @@ __global__ __launch_bounds__(256) void cache_join_tiles_kernel(CacheAttnArgs a) 
         for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                if (s0 + s >= a.splits || ml[u][s].x == -__builtin_inff()) continue;      // a split that the row saw nothing of
+                if (s0 + s >= splits || ml[u][s].x == -__builtin_inff()) continue;      // a split that the row saw nothing of
                 const float top = __builtin_fmaxf(m[u], ml[u][s].x), f = exp2_of(m[u] - top), w = exp2_of(ml[u][s].x - top);
                 m[u] = top;
                 l[u] = l[u] * f + ml[u][s].y * w;
@@ -1277,19 +1290,27 @@ constexpr int kFewRows = 16;
 struct Plan {
     bool decode, chunk;
     int part_rows, splits;         // of cache_decode_kernel
-    int tiles, chunk_splits;
+    int tiles, chunk_splits, run;
     size_t few_bytes, bytes;
 };
 
-// Splits of the keys for `groups` workgroups that have `tiles` tiles of 64 keys each to go through, `slots` of which the GPU holds at
-// once: the fewest rounds times tiles, a workgroup's start and end counting as kStart tiles.  (Two sides, chunk of 300 rows of fp32
-// on 2000 keys, 96 groups.)
-int chunk_splits(int64_t groups, int64_t tiles, int64_t slots) {
+// Splits of the longest tiles' keys, `tiles` tiles of 64 each, for `groups` workgroups, `slots` of which the GPU holds at once, and
+// `other` tiles' time of work beside them.  A workgroup's start and end count as kStart tiles, a part's store and its join as two.
+// One request: all have as many keys, so the fewest rounds times tiles.  Several: half as many keys on average (the host knows the
+// longest only), so the longest workgroup or the work over the slots, whichever takes longer.  Measured on 168 groups of 47 tiles at
+// most beside 21 requests of one token: 1 split 97 us, 2 73, 3 (taken) 67, 4 79; 80 groups of 32 tiles of one request: 1 64 us, 3 38,
+// 6 (taken) 39, 8 48.
+int chunk_splits(int64_t groups, int64_t tiles, int64_t slots, int64_t other, bool one) {
     constexpr int kStart = 5;
     int best = 1;
-    int64_t least = INT64_MAX;
+    double least = 1e300;
     for (int s = 1; s <= kMaxSplits && s <= tiles; ++s) {
-        const int64_t cost = ceil_div(groups * s, slots) * (ceil_div(tiles, s) + kStart + (s > 1 ? 2 : 0));
+        const int64_t fixed = kStart + (s > 1 ? 2 : 0), longest = ceil_div(tiles, s) + fixed, rounds = ceil_div(groups * s, slots);
+        double cost = (double)(rounds * longest);
+        if (!one) {
+            const double even = (groups * (0.5 * tiles + fixed * s) + other) / slots + (rounds > 1 ? 0.5 * longest : 0);
+            cost = even > longest ? even : longest;
+        }
         if (cost < least) { least = cost; best = s; }
     }
     return best;
@@ -1311,7 +1332,10 @@ Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, 
     const int64_t rows = tokens * group;
     const int64_t big = p.decode ? (rows / (kFewRows + 1) < requests ? rows / (kFewRows + 1) : requests) : 1;   // requests with more rows
     p.tiles = p.chunk ? clamp(p.decode ? rows / kTileRows + big : ceil_div(rows, kTileRows), INT32_MAX) : 0;
-    p.chunk_splits = p.chunk ? chunk_splits((rows / kTileRows + 1) * c.heads, ceil_div(max_len, kTileKeys), type == MX_F32 ? 256 : 512) : 1;
+    // (128 keys of a request of one token take about as long as a tile)
+    p.chunk_splits = p.chunk ? chunk_splits((rows / kTileRows + 1) * c.heads, ceil_div(max_len, kTileKeys), type == MX_F32 ? 256 : 512,
+                                            p.decode ? units * (max_len / 128) : 0, requests == 1) : 1;
+    p.run = clamp(ceil_div(ceil_div(max_len, kTileKeys), p.chunk_splits), 1 << 24);
     auto part_bytes = [&](size_t rows, int splits) { return splits > 1 ? (rows * splits * ((size_t)c.dim * 4 + 8) + 255) / 256 * 256 : 0; };
     p.few_bytes = p.decode ? part_bytes((size_t)units * p.part_rows, p.splits) : 0;
     p.bytes = kCounterBytes + p.few_bytes + (p.chunk ? part_bytes((size_t)p.tiles * c.heads * kTileRows, p.chunk_splits) : 0);
@@ -1341,6 +1365,7 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         many.least = p.decode ? kFewRows + 1 : 1;
         many.most = INT32_MAX;
         many.splits = p.chunk_splits;
+        many.run = p.run;
         many.tiles = p.tiles;
         many.part_rows = kTileRows;
         many_rows = (int64_t)p.tiles * base.heads * kTileRows;
