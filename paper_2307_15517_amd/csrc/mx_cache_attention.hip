@@ -35,10 +35,10 @@ struct CacheAttnArgs {
     int32_t page_log2;
     int32_t exp_shift;         // an exponent byte e stands for 2^(e - exp_shift) per mantissa unit
     int32_t splits;            // of this launch, at most
-    int32_t run;               // cache_chunk_kernel: tiles of keys that a split is given
+    int32_t run;               // chunk(): tiles of keys that a split is given
     int32_t least, most;       // this launch takes the requests that have least .. most rows (token, head of a group)
     int32_t part_rows;         // part rows per unit; a request with more rows is not split
-    int32_t tiles;             // cache_chunk_kernel: row tiles of all requests, at most
+    int32_t tiles;             // chunk(): row tiles of all requests, at most
     int32_t sorted;            // cache_decode_kernel: the longest requests go first
     int32_t join;              // the workgroup of a unit that comes last joins its parts; else a launch of its own does
     int32_t vec_q, vec_o;      // rows of q / out allow 16-byte (bfloat16 out: 8-byte) accesses
@@ -598,6 +598,9 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
 // largest number is near 2^12 (numbers 2^-26 of that and larger stay exact); that power goes into the exponent of the
 // probabilities, against a maximum over (score + exponent), and out of their sum again, which costs an addition per eight
 // keys.  fp32 activations: three bfloat16 pieces of q and of the probabilities, V as it is.
+//
+// DT is the head dimension that LDS is laid out for, 64 or 128, DC the one that is computed with: up to 96 of 128 the matrix
+// instructions leave the last quarter out (3 prompts of 1000 tokens, 8 heads x 4 of 96: 58.6 us with 128, 53.4 with 96).
 constexpr int kTileRows = 128, kTileKeys = 64;
 
 // The request that tile number `tile` belongs to, and which of its tiles of rows it is; b < 0: none.  Every wave looks for itself, 64
@@ -716,11 +719,11 @@ constexpr float kHalfShift = 6.f;      // probabilities are carried times 2^6: t
 constexpr float kLag = 8.f;            // the maximum that they are taken against follows the rows' own within this power of two
 constexpr int kLeastExponent = -40;    // of a run of V
 
-template <int TYPE, int DT, int BLOCK>
+template <int TYPE, int DT, int BLOCK, int DC>
 __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t* smem) {
     constexpr bool HALF = TYPE == MX_BF16;
     constexpr int QP = Pieces<TYPE>::Q, P = HALF ? 1 : 3;
-    constexpr int NK = DT / 16, ND = DT / 32;
+    constexpr int NK = DC / 16, ND = DC / 32;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
     constexpr int kTensor = kTileKeys * DT * 2;            // LDS: K stage 0, 1, V stage 0, 1, then the exponents of V's runs
     constexpr int kVBase = 2 * kTensor, kExp = 4 * kTensor;
@@ -1131,10 +1134,10 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
 }
 
 // Requests of many rows and, in the workgroups after `chunks`, of few: in a batch that has both they run side by side.
-template <int TYPE, int DT, int BLOCK>
+template <int TYPE, int DT, int BLOCK, int DC>
 __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_mixed_kernel(CacheAttnArgs many, CacheAttnArgs few, int chunks) {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    if ((int)blockIdx.x < chunks) chunk<TYPE, DT, BLOCK>(many, blockIdx.x, smem);
+    if ((int)blockIdx.x < chunks) chunk<TYPE, DT, BLOCK, DC>(many, blockIdx.x, smem);
     else decode<TYPE, DT, BLOCK>(few, blockIdx.x - chunks, *reinterpret_cast<DecodeLds<DT>*>(smem));
     fill_padding<TYPE>(many);
 }
@@ -1282,9 +1285,10 @@ __global__ __launch_bounds__(256) void cache_zero_kernel(CacheAttnArgs a) {
 }
 
 // ---- what a call launches -------------------------------------------------------------------------------
-// Requests with at most sixteen rows go to cache_decode_kernel, the others to cache_chunk_kernel.  The host knows bounds only:
-// when no request can have more rows by them, the first takes all (any number of rows is right there, sixteen at a time), a
-// single request goes to the one or the other, else both are launched and each leaves the other's requests alone.
+// Requests with at most sixteen rows are the work of decode(), the others of chunk().  The host knows bounds only: when no request can
+// have more rows by them, cache_decode_kernel takes all (any number of rows is right there, sixteen at a time), else
+// cache_mixed_kernel has workgroups of both, each of which leaves the other's requests alone; a single request needs those of
+// the one or the other only.  (24 mixed requests: 66 us in one launch, 80 in two.)
 constexpr int kFewRows = 16;
 
 struct Plan {
@@ -1342,7 +1346,7 @@ Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, 
     return p;
 }
 
-template <int TYPE, int DT, int BLOCK>
+template <int TYPE, int DT, int BLOCK, int DC>
 mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* workspace, hipStream_t stream) {
     CacheAttnArgs few = base, many = base;
     uint8_t* parts = workspace + kCounterBytes;
@@ -1374,9 +1378,9 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         constexpr int lds = 4 * kTileKeys * DT * 2 + 32;
         static_assert(sizeof(DecodeLds<DT>) <= lds, "both share the workgroup's LDS");
         static std::atomic<uint64_t> raised{0};
-        if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_mixed_kernel<TYPE, DT, BLOCK>, lds, raised)) return MX_ERR_DEVICE;
+        if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_mixed_kernel<TYPE, DT, BLOCK, DC>, lds, raised)) return MX_ERR_DEVICE;
         const int64_t chunks = (int64_t)p.tiles * base.heads * p.chunk_splits;
-        cache_mixed_kernel<TYPE, DT, BLOCK><<<(unsigned)(chunks + (p.decode ? units * p.splits : 0)), 256, lds, stream>>>(many, few, (int)chunks);
+        cache_mixed_kernel<TYPE, DT, BLOCK, DC><<<(unsigned)(chunks + (p.decode ? units * p.splits : 0)), 256, lds, stream>>>(many, few, (int)chunks);
     } else {
         cache_decode_kernel<TYPE, DT, BLOCK><<<(unsigned)(units * p.splits), 256, 0, stream>>>(few);
     }
@@ -1388,6 +1392,12 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
     return p.chunk && p.chunk_splits > 1 ? launch_join<TYPE, true>(many, many_rows, stream) : MX_OK;
 }
 
+template <int TYPE, int DT, int DC>
+mx_status launch_block(const CacheAttnArgs& a, const Plan& p, int block, uint8_t* workspace, hipStream_t stream) {
+    return block == 0 ? launch_kernels<TYPE, DT, 0, DC>(a, p, workspace, stream)
+           : block == 16 ? launch_kernels<TYPE, DT, 16, DC>(a, p, workspace, stream) : launch_kernels<TYPE, DT, 32, DC>(a, p, workspace, stream);
+}
+
 template <int TYPE>
 mx_status launch(const CacheAttnArgs& a, const Plan& p, int block, uint8_t* workspace, hipStream_t stream) {
     if (a.requests == 0) {
@@ -1395,11 +1405,8 @@ mx_status launch(const CacheAttnArgs& a, const Plan& p, int block, uint8_t* work
         MX_HIP_LAUNCH_CHECK();
         return MX_OK;
     }
-    if (a.dim <= 64)
-        return block == 0 ? launch_kernels<TYPE, 64, 0>(a, p, workspace, stream)
-               : block == 16 ? launch_kernels<TYPE, 64, 16>(a, p, workspace, stream) : launch_kernels<TYPE, 64, 32>(a, p, workspace, stream);
-    return block == 0 ? launch_kernels<TYPE, 128, 0>(a, p, workspace, stream)
-           : block == 16 ? launch_kernels<TYPE, 128, 16>(a, p, workspace, stream) : launch_kernels<TYPE, 128, 32>(a, p, workspace, stream);
+    if (a.dim <= 64) return launch_block<TYPE, 64, 64>(a, p, block, workspace, stream);
+    return a.dim <= 96 ? launch_block<TYPE, 128, 96>(a, p, block, workspace, stream) : launch_block<TYPE, 128, 128>(a, p, block, workspace, stream);
 }
 
 bool attention_args_ok(const mx_cache& c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len) {

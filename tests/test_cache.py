@@ -503,3 +503,26 @@ def test_step_in_a_graph():
         step()
         torch.cuda.synchronize()
         assert torch.equal(got, out) and got.isfinite().all()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "mx16"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attention_batches_whose_tiles_are_split_unevenly(dtype, kind):
+    """Row tiles of one run next to tiles of many, and requests of a few rows beside both; more than sixteen runs of a tile; a
+    tile whose first rows see nothing."""
+    Step([(300, 3000), (1, 2000), (300, 310), (20, 60), (3, 900)], 2, 2, 96, 16, FORMATS[kind], dtype, seed=16).check()
+    Step([(1, 4), (40, 9000), (1, 5000), (25, 64)], 1, 2, 64, 32, FORMATS[kind], dtype, seed=17).check()
+    Step([(90, 4000), (1, 3000), (70, 40), (200, 7)], 1, 1, 80, 16, FORMATS[kind], dtype, seed=18).check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("requests,heads,group,most_new,longest", [(40, 8, 4, 1, 4000), (40, 8, 4, 4, 41000), (64, 12, 1, 2, 600),
+                                                                 (65, 8, 1, 1, 700), (300, 4, 1, 1, 200), (150, 2, 1, 30, 90)])
+def test_attention_many_requests(dtype, requests, heads, group, most_new, longest):
+    """The longest requests first, however they stand; parts joined by a launch of their own; more requests than a wave has lanes."""
+    r = np.random.default_rng(requests + longest)
+    lens = [(int(r.integers(0, most_new + 1)), int(r.integers(1, min(longest, 400) + 1))) for _ in range(requests)]
+    lens[requests // 2], lens[requests // 3] = (most_new, longest), (1, longest)
+    Step(lens, heads, group, 64, 16, FORMATS["mx32"], dtype, seed=requests).check()
