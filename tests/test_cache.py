@@ -526,3 +526,48 @@ def test_attention_many_requests(dtype, requests, heads, group, most_new, longes
     lens = [(int(r.integers(0, most_new + 1)), int(r.integers(1, min(longest, 400) + 1))) for _ in range(requests)]
     lens[requests // 2], lens[requests // 3] = (most_new, longest), (1, longest)
     Step(lens, heads, group, 64, 16, FORMATS["mx32"], dtype, seed=requests).check()
+
+
+@gpu
+@pytest.mark.parametrize("f", [None, FORMATS["mx32"]])
+def test_serving_example(f):
+    """The example's steps against attention in float64 over the keys and values that its cache holds."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "examples", "paged_serving.py")
+    spec = importlib.util.spec_from_file_location("paged_serving", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    r = np.random.default_rng(5)
+    waiting = [ex.Request(r.integers(0, ex.VOCAB, n), m) for n, m in ((100, 4), (1, 9), (49, 2), (16, 3), (30, 1), (7, 5), (64, 2))]
+    lengths = sorted(x.stop + 1 for x in waiting)
+    server = ex.Server(batch=4, pages=64, page=16, max_len=160, chunk=48, f=f)
+    finished = []
+    for _ in range(40):
+        server.admit(waiting)
+        if all(x is None for x in server.places):
+            break
+        finished += server.step()
+        q, o, q_start, kv_len = server.last
+        c, found = server.cache.c, []
+        for data, exps in ((server.cache.k, server.cache.k_exps), (server.cache.v, server.cache.v_exps)):
+            x = data.view(torch.bfloat16) if f is None else mx.dequantize(data, exps, 1, c.pages * c.heads * c.page, c.dim, f)
+            found.append(x.reshape(c.pages, c.heads, c.page, c.dim).double().cpu())
+        table, q, o, q_start, kv_len = (t.cpu() for t in (server.table, q.double(), o.double(), q_start, kv_len))
+        for b in range(4):
+            n, m = int(q_start[b + 1] - q_start[b]), int(kv_len[b])
+            if n == 0:
+                continue
+            pages = table[b, :-(-m // 16)].long()
+            k, v = (x[pages].transpose(0, 1).reshape(c.heads, -1, c.dim)[:, :m] for x in found)
+            rows = slice(int(q_start[b]), int(q_start[b + 1]))
+            for a in range(ex.HEADS_Q):
+                x, h = q[rows, a * 64:(a + 1) * 64], a // (ex.HEADS_Q // ex.HEADS)
+                s = (x @ k[h].T) / 8.0
+                s = s.masked_fill(torch.arange(m)[None, :] > (m - n + torch.arange(n))[:, None], -np.inf)
+                # fp32 throughout: as in Step.reference, with |s| <= |q||k|/8
+                mag = (x.abs() @ k[h].abs().T).max() / 8.0
+                eps = 2 * 2.0 ** -24 * (64 + 12) * mag + 2 * (m + 64) * 2.0 ** -24
+                p = torch.softmax(s, -1)
+                assert ((o[rows, a * 64:(a + 1) * 64] - p @ v[h]).abs() <= eps * (p @ v[h].abs()) + 2.0 ** -120).all()
+    assert sorted(len(x.tokens) for x in finished) == lengths and sorted(server.free) == list(range(64))
