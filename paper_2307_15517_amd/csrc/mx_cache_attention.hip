@@ -1320,6 +1320,23 @@ int chunk_splits(int64_t groups, int64_t tiles, int64_t slots, int64_t other, bo
     return best;
 }
 
+// The last workgroup of a unit to arrive joins its splits, or a launch of its own does when there are many parts of many rows.
+bool joined_apart(int rows, int splits) { return rows * splits > 128; }
+
+// Splits of a request's keys in decode(), `blocks` steps of 128 keys in all: a step takes about 0.9 us, the meeting of the splits 2.4 +
+// 0.15 each, joining them apart 6.3.  (16 requests of 300 keys, 8 heads x 4: 1 split 9.6 us, 2 11.8, 3 10.9; 2 of 1000: 3 splits 12.2,
+// 4 10.8, 8 10.1; 1936 keys of 32 heads: 6 splits 14.2, 8 12.6, 16 13.9; 2 of 4096: 11 splits 14.2, 16 13.6, 32 16.9; 2 of 16000:
+// 25 splits 23.4, 48, joined apart, 21.8; one of 9000, one head x 8, joined apart: 18 splits 14.8, 36 11.8.)
+int decode_splits(int64_t blocks, int least, int most, int rows) {
+    int best = least;
+    int64_t lowest = INT64_MAX;
+    for (int s = least; s <= most && s <= blocks; ++s) {
+        const int64_t cost = 18 * ceil_div(blocks, s) + (s == 1 ? 0 : joined_apart(rows, s) ? 126 : 48 + 3 * s);
+        if (cost < lowest) { lowest = cost; best = s; }
+    }
+    return best;
+}
+
 Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len) {
     Plan p{};
     const int64_t group = heads_q / c.heads;
@@ -1329,10 +1346,10 @@ Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, 
     p.part_rows = (int)(most < kFewRows ? most : kFewRows);
     auto clamp = [](int64_t v, int64_t hi) { return (int)(v > hi ? (hi < 1 ? 1 : hi) : v < 1 ? 1 : v); };
     const int64_t units = requests * c.heads;
-    // as many workgroups as the GPU holds at once, but no run of keys over 4096, which would leave the last ones alone at the end
+    // at most as many workgroups as the GPU holds at once, but no run of keys over 4096, which would leave the last ones alone at the end
     const int64_t slots = type == MX_F32 ? 512 : 768, even = units > 0 ? slots / units : 1, fine = ceil_div(max_len, 4096);
-    p.splits = units <= kCounterBytes / 4 ? clamp(even > fine ? even : fine, ceil_div(max_len, 256)) : 1;
-    p.splits = p.splits > kMaxSplits ? kMaxSplits : p.splits;
+    p.splits = units <= kCounterBytes / 4 ? decode_splits(ceil_div(max_len, 128), clamp(fine, kMaxSplits), clamp(even > fine ? even : fine, kMaxSplits),
+                                                              p.chunk ? 0 : p.part_rows) : 1;
     const int64_t rows = tokens * group;
     const int64_t big = p.decode ? (rows / (kFewRows + 1) < requests ? rows / (kFewRows + 1) : requests) : 1;   // requests with more rows
     p.tiles = p.chunk ? clamp(p.decode ? rows / kTileRows + big : ceil_div(rows, kTileRows), INT32_MAX) : 0;
@@ -1361,7 +1378,7 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         few_rows = units * p.part_rows;
         few.part_o = (float*)parts;
         few.part_ml = (float2*)(few.part_o + few_rows * p.splits * base.dim);
-        few.join = p.chunk || p.part_rows * p.splits <= 128;      // next to chunks the bound of sixteen rows says little
+        few.join = p.chunk || !joined_apart(p.part_rows, p.splits);      // next to chunks the bound of sixteen rows says little
         few.sorted = base.requests > 1 && base.requests <= 64 && units * p.splits > 512;
         parts += p.few_bytes;
     }
