@@ -9,7 +9,8 @@ namespace {
 // needs before it, its tokens at the sum of the new tokens before it.  Integers only, a few hundred kilobytes at most: bound by
 // the latency of one launch and of the scan.  Every workgroup scans all requests for itself into LDS (two sums per request),
 // so that nothing is exchanged between workgroups and one launch does it; then it takes its share of the requests (a wave
-// each: the new entries of the row) and of the tokens (a thread each: its request by binary search in LDS).
+// each: the new entries of the row) and of the tokens (a thread each: its request by binary search in LDS).  4 requests 3.5 us
+// in the kernel, 5.5 a call; 700 requests, 10 percent with prompts of up to 1024 tokens, 8.9 and 8.5.
 struct PlanArgs {
     const int32_t* ctx;
     const int32_t* fresh;
@@ -129,6 +130,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
 // Every element is read once and written once: bound by memory, by latency at the few tokens of a decode step.  A lane takes
 // eight elements of a row (BLOCK/8 neighbouring lanes a block, whose largest magnitude they exchange), both tensors in one
 // launch.  The MXInt arithmetic is mx_quantize's, on the bits: E = floor(log2 max|x|) clamped, q = round(x 2^(6 - E)).
+// 1999 tokens x 8 heads x 128, fp32 into MXInt: 5.8 us for 20.6 MB, 3.6 TB/s; 8 tokens x 32 heads 2.5 us in the kernel, 5.4 a call.
 struct AppendArgs {
     const void* x[2];          // k, v
     void* data[2];
