@@ -1347,6 +1347,7 @@ int decode_splits(int64_t blocks, int least, int most, int rows) {
 
 Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len) {
     Plan p{};
+    if (max_len > INT32_MAX) max_len = INT32_MAX;      // no sum or product below leaves 64 bits
     const int64_t group = heads_q / c.heads;
     const int64_t most = (max_new < tokens ? max_new : tokens) * group;
     p.chunk = most > kFewRows;

@@ -571,3 +571,13 @@ def test_serving_example(f):
                 p = torch.softmax(s, -1)
                 assert ((o[rows, a * 64:(a + 1) * 64] - p @ v[h]).abs() <= eps * (p @ v[h].abs()) + 2.0 ** -120).all()
     assert sorted(len(x.tokens) for x in finished) == lengths and sorted(server.free) == list(range(64))
+
+
+@gpu
+@pytest.mark.parametrize("lens", [RAGGED, CHUNKS, [(300, 2000)]])
+def test_attention_takes_any_bounds(lens):
+    """Bounds as large as the type holds: no sum or product of the host's arithmetic may leave its range."""
+    for dtype in (torch.float32, torch.bfloat16):
+        s = Step(lens, 2, 2, 64, 16, FORMATS["mx32"], dtype, seed=19)
+        for bound in (2 ** 31 - 1, 2 ** 40, 2 ** 63 - 1):
+            s.check(max_new=bound, max_len=bound)
