@@ -10,7 +10,8 @@ namespace {
 // the latency of one launch and of the scan.  Every workgroup scans all requests for itself into LDS (two sums per request),
 // so that nothing is exchanged between workgroups and one launch does it; then it takes its share of the requests (a wave
 // each: the new entries of the row) and of the tokens (a thread each: its request by binary search in LDS).  4 requests 3.5 us
-// in the kernel, 5.5 a call; 700 requests, 10 percent with prompts of up to 1024 tokens, 8.9 and 8.5.
+// in the kernel, 5.5 a call; 700 requests, 10 percent with prompts of up to 1024 tokens, 7.6 a call (8.6 with a request a thread
+// and three scans; 4000 requests of one token 9.8 against 17).
 struct PlanArgs {
     const int32_t* ctx;
     const int32_t* fresh;
@@ -38,6 +39,8 @@ __device__ __forceinline__ int64_t wave_scan(int64_t v) {
     return v;
 }
 
+// RUN: neighbouring requests a thread takes of the scan, whose lengths it asks for together
+template <int RUN>
 __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
     extern __shared__ int32_t plan_lds[];
     int32_t* start = plan_lds;                        // [requests + 1]: first packed token of a request
@@ -51,33 +54,45 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
 
     if (tid < 2) served[tid] = 0;
     int64_t page_sum = 0, token_sum = 0, taken = 0, refused = 0;
-    for (int base = 0; base < a.requests; base += kPlanThreads) {
-        const int b = base + tid;
-        int64_t n = 0, need = 0;
-        bool wide = false;
-        if (b < a.requests) {
-            const int64_t c = length(a.ctx[b]);
-            n = length(a.fresh[b]);
-            const int64_t want = pages_of(c + n);
-            wide = want > a.width;
-            need = wide ? 0 : want - pages_of(c);
+    for (int base = 0; base < a.requests; base += kPlanThreads * RUN) {
+        const int b0 = base + tid * RUN;
+        int64_t n[RUN], need[RUN], c[RUN], sum_need = 0, sum_n = 0;
+        bool wide[RUN];
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            const int b = min(b0 + i, a.requests - 1);
+            c[i] = length(a.ctx[b]);
+            n[i] = length(a.fresh[b]);
         }
-        const int64_t up = wave_scan(need), ut = wave_scan(n);
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            if (b0 + i >= a.requests) c[i] = n[i] = 0;
+            const int64_t want = pages_of(c[i] + n[i]);
+            wide[i] = want > a.width;
+            need[i] = wide[i] ? 0 : want - pages_of(c[i]);
+            sum_need += need[i];
+            sum_n += n[i];
+        }
+        const int64_t up = wave_scan(sum_need), ut = wave_scan(sum_n);
         __syncthreads();                              // the tile before has read part
         if (lane == 63) { part[0][wave] = up; part[1][wave] = ut; }
         __syncthreads();
-        int64_t p = page_sum + up, t = token_sum + ut;
+        int64_t p = page_sum + up - sum_need, t = token_sum + ut - sum_n;
 #pragma unroll
         for (int w = 0; w < kPlanThreads / 64; ++w) {
             if (w < wave) { p += part[0][w]; t += part[1][w]; }
             page_sum += part[0][w];
             token_sum += part[1][w];
         }
-        if (b < a.requests) {
-            const bool no = wide || (need > 0 && p > a.n_free);
-            start[b + 1] = (int32_t)(t < INT32_MAX ? t : INT32_MAX);
-            at[b] = no ? -1 : need > 0 ? (int32_t)(p - need) : 0;     // served: p <= n_free < 2^31
-            taken += no ? 0 : need;
+#pragma unroll
+        for (int i = 0; i < RUN; ++i) {
+            p += need[i];
+            t += n[i];
+            if (b0 + i >= a.requests) break;
+            const bool no = wide[i] || (need[i] > 0 && p > a.n_free);
+            start[b0 + i + 1] = (int32_t)(t < INT32_MAX ? t : INT32_MAX);
+            at[b0 + i] = no ? -1 : need[i] > 0 ? (int32_t)(p - need[i]) : 0;     // served: p <= n_free < 2^31
+            taken += no ? 0 : need[i];
             refused += no;
         }
     }
@@ -231,12 +246,15 @@ extern "C" mx_status mx_cache_plan(const int32_t* ctx_len, const int32_t* new_le
                (int32_t)requests, log2_of(page)};
     const int lds = (int)(2 * requests + 1) * 4;
     static std::atomic<uint64_t> raised{0};
-    if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_plan_kernel, (2 * kCacheMaxRequests + 1) * 4, raised))
+    if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_plan_kernel<4>, (2 * kCacheMaxRequests + 1) * 4, raised))
         return MX_ERR_DEVICE;
     // a workgroup per 1024 tokens or 16 requests: the scan, which all repeat, costs as much as that
     int64_t groups = max(ceil_div(tokens, 1024), ceil_div(requests, 16));
     groups = groups < 1 ? 1 : groups > 512 ? 512 : groups;
-    cache_plan_kernel<<<(unsigned)groups, kPlanThreads, lds, (hipStream_t)stream>>>(a);
+    // one round of the scan with a request a thread is enough (60 prompts 6.2 us, four a thread 6.6), or several with four (700
+    // requests 7.6 us, one a thread 8.5)
+    if (requests <= kPlanThreads) cache_plan_kernel<1><<<(unsigned)groups, kPlanThreads, lds, (hipStream_t)stream>>>(a);
+    else cache_plan_kernel<4><<<(unsigned)groups, kPlanThreads, lds, (hipStream_t)stream>>>(a);
     MX_HIP_LAUNCH_CHECK();
     return MX_OK;
 }
