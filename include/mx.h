@@ -443,11 +443,10 @@ MX_API mx_status mx_cache_append(const void* k, const void* v, int32_t type, int
  * as width * page; q_start is clamped to [0, tokens].
  * max_new, max_len: bounds on the requests' new tokens and lengths as the host knows them.  They only shape the launch: the
  * result is right for any positive values.
- * Numerics: products of the exact inputs, scores, softmax statistics and sums in fp32.  MX_F32: q and the probabilities enter the
- * products with 24 bits.  MX_BF16: the probabilities enter the second product with 16 bits (requests of few rows) or with 11,
- * scaled so that those of a row's largest terms are normal half-precision numbers.  Same inputs, same bits.  Cached values and
- * probabilities below 2^-126 may count as zero; in MX_BF16 calls cached values below 2^-64 may, and cached values must stay below
- * 2^80 in size.
+ * Numerics: products of the exact inputs, scores, softmax statistics and sums in fp32.  q enters the products with all its bits,
+ * the probabilities with 24; in MX_BF16 calls those of requests with more than sixteen rows (token, head of a group) enter as two
+ * bfloat16 numbers, which leave 2^-16 of a probability at most.  Same inputs, same bits.  Cached values and probabilities below
+ * 2^-126 may count as zero.  Of the cached values a token does not see none has a part in its result.
  * workspace: mx_cache_attention_workspace_bytes(...) bytes for the same arguments, 256-byte aligned, caller-owned; its first
  *   65536 bytes must be zero when the call starts and are zero again afterwards, the rest needs no initial value.  Calls that
  *   may overlap in time need a workspace each.

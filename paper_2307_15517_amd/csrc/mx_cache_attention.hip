@@ -138,12 +138,22 @@ __device__ __forceinline__ uint32_t cut_piece(float& a, float& b) {
     return w;
 }
 
-// bfloat16 pieces of a float whose sum is the float's leading 8, 16 or 24 bits; each piece is cut, not rounded, but the last
+// The nearest bfloat16 numbers of two floats, which keep the rest (not for floats that would round to infinity)
+__device__ __forceinline__ uint32_t near_piece(float& a, float& b) {
+    const uint32_t w = pack_bf16(a, b);
+    a -= __uint_as_float(w << 16);
+    b -= __uint_as_float(w & 0xffff0000u);
+    return w;
+}
+
+// A float as one, two or three bfloat16 pieces.  One is the nearest bfloat16 number, which of a bfloat16 activation is all of it.
+// Three are all 24 bits: each is cut, and what the last one gets fits it.  Two are rounded each, which leaves 2^-16 of the float at
+// most (2^-15 if the first were cut) in as many instructions.
 template <int P>
 __device__ __forceinline__ void pieces_of(float a, float b, uint32_t (&w)[P]) {
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-        w[p] = p == P - 1 ? pack_bf16(a, b) : cut_piece(a, b);
+        w[p] = p == P - 1 ? pack_bf16(a, b) : P == 2 ? near_piece(a, b) : cut_piece(a, b);
     }
 }
 
@@ -209,17 +219,15 @@ __device__ __forceinline__ float power2(int n) { return __builtin_ldexpf(1.f, n)
 // keys of either half block in its registers, which is the right operand of O^T = V^T P^T as it stands; K and V go from memory
 // to registers without LDS, each lane a run of one key's row, and V's rows are transposed in registers.
 // DT: head dimension padded to 64 or 128 (in registers only).  BLOCK: 0 bfloat16, else MXInt.
-// Pieces: K and V are bfloat16 numbers as they are (an MXInt element has 7 bits and a sign).  bfloat16 q is one piece and its
-// probabilities are two, 16 bits, so that what is rounded is the result; float q and its probabilities are three, 24 bits.
-// The matrix instructions are idle most of the time here, so the pieces cost nothing.
+// Pieces: K and V are bfloat16 numbers as they are (an MXInt element has 7 bits and a sign).  bfloat16 q is one piece, float q
+// three, and the probabilities are three, so that nothing but the result is rounded to fewer than 24 bits.  The matrix instructions
+// are idle most of the time here: the third piece takes 1 % (32 ragged sequences, bfloat16: 75.0 us with two, 75.9).
 // Bound by the reads of K and V: one sequence of 100003 keys (8 heads x 5, bfloat16) 77 us = 5.3 TB/s of the 5.6 that a bare read
 // reaches; 32 of up to 8191 (8 heads x 4, MXInt 32) 74 us = 4.3 TB/s, the vector arithmetic of the MXInt conversion taking as long as
 // the reads and the last requests ending alone.  Short calls by the chain of loads (lengths, table, K and V), about 0.9 us a step, and
 // the meeting of the splits: 1936 keys of 32 heads 12.4 us, one sequence of 61 keys 6.1.
 template <int TYPE>
-struct Pieces {
-    static constexpr int Q = TYPE == MX_F32 ? 3 : 1, P = TYPE == MX_F32 ? 3 : 2;
-};
+constexpr int kQueryPieces = TYPE == MX_F32 ? 3 : 1;
 
 // Parts of a row's result pass between workgroups that may sit behind different L2 caches: they are written through to and read
 // from the level that all compute units share (device scope), so that no cache has to be written back or invalidated as a whole.
@@ -338,7 +346,7 @@ template <int TYPE, int DT, int BLOCK>
 __device__ __forceinline__ void decode(const CacheAttnArgs& a, int index, DecodeLds<DT>& lds) {
     constexpr int NS = DT / 32, NJ = DT / 16, VE = DT / 16;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
-    constexpr int QP = Pieces<TYPE>::Q, P = Pieces<TYPE>::P;
+    constexpr int QP = kQueryPieces<TYPE>, P = 3;
     using Block = KeyBlock<DT, BLOCK>;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int n = lane & 15, g = lane >> 4;
@@ -597,18 +605,18 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
 // depend on each other: P V of step u-1, the scores of step u+1, and the softmax of step u, whose instructions stand between
 // those matrix instructions.  K's stages are therefore 32 keys ahead of V's.
 //
-// bfloat16 activations: one half-precision piece holds a probability to 11 bits, where bfloat16 would need two and twice the
-// matrix instructions.  V becomes half precision on its way to LDS, scaled by a power of two per run of sixteen keys so that its
-// largest number is near 2^12 (numbers 2^-26 of that and larger stay exact); that power goes into the exponent of the
-// probabilities, against a maximum over (score + exponent), and out of their sum again, which costs an addition per eight
-// keys.  fp32 activations: three bfloat16 pieces of q and of the probabilities, V as it is.
+// K and V are bfloat16 numbers as they are, so nothing bounds their sizes.  fp32 activations: three bfloat16 pieces of q and of the
+// probabilities, all their bits.  bfloat16 activations: q as it is and two pieces of the probabilities, what is left out being 2^-16
+// of one, 2^-8 of what the rounding of the result leaves out.  (Three: 648 us for the five prompts below.  One half-precision
+// piece: 485, with 11 bits and V scaled to half precision's range by the largest of sixteen keys, which loses small values next to
+// large ones, also to those of tokens that a row must not see.)
 //
-// Measured: five prompts of 1687 .. 4096 tokens (8 heads x 4 of 128, bfloat16) 490 us = 750 TFLOP/s, vector ALUs active about 60 % and
-// matrix cores busy 36 % of the cycles; 300 tokens on 2000 keys (32 heads, fp32: three times the matrix instructions, one wave per
-// SIMD) 68 us, of which 8 join the splits.  Two half-precision pieces of q, K and P for fp32: 66 us, and probabilities below 2^-36 lost.
+// Measured: five prompts of 1687 .. 4096 tokens (8 heads x 4 of 128, bfloat16) 526 us = 704 TFLOP/s; 300 tokens on 2000 keys (32
+// heads, fp32: three times the matrix instructions, one wave per SIMD) 68 us, of which 8 join the splits.
 //
 // DT is the head dimension that LDS is laid out for, 64 or 128, DC the one that is computed with: up to 96 of 128 the matrix
-// instructions leave the last quarter out (3 prompts of 1000 tokens, 8 heads x 4 of 96: 58.6 us with 128, 53.4 with 96).
+// instructions leave the last quarter out (3 prompts of 1000 tokens, 8 heads x 4 of 96: 58.6 us with 128, 53.4 with 96, in half
+// precision).
 constexpr int kTileRows = 128, kTileKeys = 64;
 
 // The request that tile number `tile` belongs to, and which of its tiles of rows it is; b < 0: none.  Every wave looks for itself, 64
@@ -694,48 +702,15 @@ __device__ __forceinline__ void pin(uint32_t x) { asm volatile("" ::"v"(x)); }
 // a register of its own, one for every place in every stage.
 __device__ __forceinline__ void opaque(uint32_t& x) { asm("" : "+v"(x)); }
 
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-
-// Two bfloat16 numbers times a power of two as half-precision numbers
-__device__ __forceinline__ uint32_t bf16_to_half(uint32_t x, float scale) {
-    uint32_t r;
-    asm("v_fma_mixlo_f16 %0, %1, %3, 0\n\tv_fma_mixhi_f16 %0, %2, %3, 0" : "=&v"(r) : "v"(x << 16), "v"(x & 0xffff0000u), "v"(scale));
-    return r;
-}
-// Bytes 2i and 2i+1 of x (mantissas, the sign bit flipped: m + 128) times a power of two as half-precision numbers: the byte
-// goes under the exponent of 1024, and one multiply-add takes 1024 + 128 away again, exactly
-template <int I>
-__device__ __forceinline__ uint32_t bytes_to_half(uint32_t x, v2h scale, v2h minus) {
-    const v2h t = __builtin_bit_cast(v2h, __builtin_amdgcn_perm(0x64646464u, x, I == 0 ? 0x04010400u : 0x04030402u));
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(t, scale, minus));
-}
-
-template <int CTRL>
-__device__ __forceinline__ float max_with(float v) {
-    return __builtin_fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true)));
-}
-__device__ __forceinline__ float max_across_wave(float v) {
-    v = max_with<0xB1>(v);             // lane ^ 1, ^ 2, 7 - lane in eight, 15 - lane in sixteen
-    v = max_with<0x4E>(v);
-    v = max_with<0x141>(v);
-    v = max_with<0x140>(v);
-    return max_across_16_32(v);
-}
-
-constexpr float kHalfShift = 6.f;      // probabilities are carried times 2^6: the largest is at most 2^14, what is flushed 2^-31 of it
-constexpr float kLag = 8.f;            // the maximum that they are taken against follows the rows' own within this power of two
-constexpr int kLeastExponent = -40;    // of a run of V
+constexpr float kLag = 8.f;            // the maximum that probabilities are taken against follows the rows' own within this power of two
 
 template <int TYPE, int DT, int BLOCK, int DC>
 __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t* smem) {
-    constexpr bool HALF = TYPE == MX_BF16;
-    constexpr int QP = Pieces<TYPE>::Q, P = HALF ? 1 : 3;
+    constexpr int QP = kQueryPieces<TYPE>, P = TYPE == MX_F32 ? 3 : 2;
     constexpr int NK = DC / 16, ND = DC / 32;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
-    constexpr int kTensor = kTileKeys * DT * 2;            // LDS: K stage 0, 1, V stage 0, 1, then the exponents of V's runs
-    constexpr int kVBase = 2 * kTensor, kExp = 4 * kTensor;
-    constexpr bool kCopyV = BLOCK == 0 && !HALF;           // V goes to LDS as it is
+    constexpr int kTensor = kTileKeys * DT * 2;            // LDS: K stage 0, 1, V stage 0, 1
+    constexpr int kVBase = 2 * kTensor;
     constexpr int kLoads = 16 * DT * EB / 1024;            // 16-byte loads per lane that bring a run of sixteen keys
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int i = lane & 31, h2 = lane >> 5;
@@ -776,15 +751,15 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
     load_q<TYPE, QP, NK>(a, (int64_t)(rq.t0 + tok) * a.ldq + (int64_t)head * dim, [&](int n) { return 16 * n + 8 * h2; }, qf);
 
     // ---- staging: a wave brings one run of sixteen keys of a stage, which lies in one page -------------------
-    // As it is (bfloat16 K, bfloat16 V for fp32 activations): copies from memory straight to LDS, 1 KiB each, lane L's bytes at
-    // 16 L of it, so the placement of the chunks is done by what each lane reads.  Else through registers.
+    // bfloat16: copies from memory straight to LDS, 1 KiB each, lane L's bytes at 16 L of it, so the placement of the chunks is done
+    // by what each lane reads.  MXInt: through registers.
     constexpr int kLaneRows = 1024 / (DT * EB);                           // rows of a load
     constexpr int kRowLanes = 64 / kLaneRows;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem;
     const int last_run = (len - 1) & ~15;
     const int rel = lane / kRowLanes;
     const int lane_d = lane % kRowLanes * (16 / EB);                      // what lies past the head dimension reads its start again
-    uint32_t k_from[BLOCK == 0 ? kLoads : 1], v_from[kCopyV ? kLoads : 1];
+    uint32_t k_from[BLOCK == 0 ? kLoads : 1], v_from[BLOCK == 0 ? kLoads : 1];
     const uint32_t from = (rel * dim + (lane_d < dim ? lane_d : 0)) * EB;
     if constexpr (BLOCK == 0) {
 #pragma unroll
@@ -792,7 +767,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
             const int row = u * kLaneRows + rel, chunk = lane % kRowLanes;
             const int kc = 8 * ((k_place<DT>(row, chunk) - row * DT * 2) >> 4), vc = 8 * ((v_place<DT>(row, chunk) - row * DT * 2) >> 4);
             k_from[u] = (row * dim + (kc < dim ? kc : 0)) * 2;
-            if constexpr (kCopyV) v_from[u] = (row * dim + (vc < dim ? vc : 0)) * 2;
+            v_from[u] = (row * dim + (vc < dim ? vc : 0)) * 2;
         }
     }
     const uint32_t e_from = BLOCK == 0 ? 0 : rel * (dim / (BLOCK == 0 ? 1 : BLOCK)) + (lane_d < dim ? lane_d : 0) / (BLOCK == 0 ? 1 : BLOCK);
@@ -805,7 +780,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
             k_to[u][x] = lds0 + k_place<DT>(row, chunk);
             v_to[u][x] = lds0 + kVBase + v_place<DT>(row, chunk);
         }
-    v4u sk[BLOCK == 0 ? 1 : kLoads], sv[kCopyV ? 1 : kLoads];
+    v4u sk[BLOCK == 0 ? 1 : kLoads], sv[BLOCK == 0 ? 1 : kLoads];
     int ek[kLoads], ev[kLoads];
     pages.set_length(a, len);
     auto row_of = [&](int key) __attribute__((always_inline)) { return pages.row(a, h, max(min(key + 16 * wave, last_run), 0)); };
@@ -828,11 +803,11 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
         const uint8_t* src = a.v + row * dim * EB;
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
-            if constexpr (kCopyV) {
+            if constexpr (BLOCK == 0) {
                 copy16_to_lds(src, v_from[u], lds0 + kVBase + slot + wave * (16 * DT * 2) + u * 1024);
             } else {
-                sv[u] = *reinterpret_cast<const v4u*>(src + u * kLaneRows * dim * EB + from);
-                if constexpr (BLOCK != 0) ev[u] = (a.v_exps + row * (dim / BLOCK) + u * kLaneRows * (dim / BLOCK))[e_from];
+                sv[u] = *reinterpret_cast<const v4u*>(src + u * kLaneRows * dim + from);
+                ev[u] = (a.v_exps + row * (dim / BLOCK) + u * kLaneRows * (dim / BLOCK))[e_from];
             }
         }
     };
@@ -856,67 +831,19 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
             }
         }
     };
-    // What lies past the request's end may be anything, NaN among it, and meets probabilities of zero: it becomes zeros.  (Past
-    // the head dimension lies a repetition; it meets zeros of q, or gives results that nobody reads.)
+    // What lies past the request's end may be anything, NaN among it, and meets probabilities of zero: it becomes zeros
+    // (of bfloat16 V in LDS, before the stage is read).  Past the head dimension lies a repetition, which meets zeros of q or gives
+    // results that nobody reads.
     auto put_v = [&](int slot, int key0) __attribute__((always_inline)) {
-        if constexpr (kCopyV) return;
-        if (key0 + 16 * wave + 16 > len) {
+        if constexpr (BLOCK != 0) {
+            const bool whole = key0 + 16 * wave + 16 <= len;
 #pragma unroll
             for (int u = 0; u < kLoads; ++u) {
-                const bool in = key0 + 16 * wave + u * kLaneRows + rel < len;
-                if constexpr (BLOCK == 0) sv[u] = in ? sv[u] : v4u{0, 0, 0, 0};
-                else sv[u] = in ? sv[u] : v4u{0, 0, 0, 0}, ev[u] = in ? ev[u] : 0;
-            }
-        }
-        if constexpr (!HALF) {
-            if constexpr (BLOCK != 0) {
-#pragma unroll
-                for (int u = 0; u < kLoads; ++u) {
-                    v4u y[2];
-                    widen(sv[u], power2(ev[u] - a.exp_shift), y);
-                    lds_write(v_to[u][0] + slot, y[0]);
-                    lds_write(v_to[u][1] + slot, y[1]);
-                }
-            }
-        } else if constexpr (BLOCK == 0) {
-            float top = 0.f;                                              // the low half of a dword does not reach its exponent
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u)
-#pragma unroll
-                for (int w = 0; w < 4; ++w)
-                    top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(__uint_as_float(sv[u][w])), __builtin_fabsf(__uint_as_float(sv[u][w] << 16))), top);
-            top = max_across_wave(top);
-            const int e = max((int)(__float_as_uint(top) >> 23) - 127 - 11, kLeastExponent);
-            if (lane == 0) *reinterpret_cast<float*>(smem + kExp + (slot ? 16 : 0) + wave * 4) = (float)e;
-            const float scale = power2(-e);
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                v4u y;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) y[w] = bf16_to_half(sv[u][w], scale);
-                lds_write(v_to[u][0] + slot, y);
-            }
-        } else {
-            int et = ev[0];
-#pragma unroll
-            for (int u = 1; u < kLoads; ++u) et = max(et, ev[u]);
-            et = (int)max_across_wave((float)et);
-            const int e = max(et - a.exp_shift - 5, kLeastExponent);
-            if (lane == 0) *reinterpret_cast<float*>(smem + kExp + (slot ? 16 : 0) + wave * 4) = (float)e;
-#pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                const float sc = power2(ev[u] - a.exp_shift - e);         // at most 2^5
-                const _Float16 s1 = (_Float16)sc, m1 = (_Float16)(sc * -1152.f);
-                const v2h scale = {s1, s1}, minus = {m1, m1};
+                const bool in = whole || key0 + 16 * wave + u * kLaneRows + rel < len;
                 v4u y[2];
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t x = sv[u][w] ^ 0x80808080u;
-                    y[w >> 1][2 * (w & 1)] = bytes_to_half<0>(x, scale, minus);
-                    y[w >> 1][2 * (w & 1) + 1] = bytes_to_half<1>(x, scale, minus);
-                }
+                widen(in ? sv[u] : v4u{0, 0, 0, 0}, power2((in ? ev[u] : 0) - a.exp_shift), y);
                 lds_write(v_to[u][0] + slot, y[0]);
-                    lds_write(v_to[u][1] + slot, y[1]);
+                lds_write(v_to[u][1] + slot, y[1]);
             }
         }
     };
@@ -973,15 +900,11 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
     };
     auto out = [&](int n) __attribute__((always_inline)) {                            // matrix instruction n of 2 * P * ND
         const int x = n / (P * ND), p = P - 1 - n / ND % P, dt = n % ND;
-        if constexpr (HALF)
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, vf[x][dt]), __builtin_bit_cast(v8h, pf[x][p]), o[dt], 0, 0, 0);
-        else
-            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, vf[x][dt]), __builtin_bit_cast(v8bf, pf[x][p]), o[dt], 0, 0, 0);
+        o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, vf[x][dt]), __builtin_bit_cast(v8bf, pf[x][p]), o[dt], 0, 0, 0);
     };
 
-    // One step of 32 keys from kb; k_next: place of the next step's keys in LDS, v_this: of this step's values, e0 and e1: the
-    // exponents of their two runs.
-    auto step = [&](auto set_c, int kb, auto k_next_c, auto v_this_c, float e0, float e1) __attribute__((always_inline)) {
+    // One step of 32 keys from kb; k_next: place of the next step's keys in LDS, v_this: of this step's values.
+    auto step = [&](auto set_c, int kb, auto k_next_c, auto v_this_c) __attribute__((always_inline)) {
         constexpr int set = decltype(set_c)::value, k_next = decltype(k_next_c)::value, v_this = decltype(v_this_c)::value;
         constexpr int NO = 2 * P * ND, NQ = NK * QP;
         float top = -__builtin_inff();
@@ -1007,9 +930,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
                     t[x] = max_of(t[x], s[set][8 * x + 5], s[set][8 * x + 6]);
                     t[x] = max_of(t[x], s[set][8 * x + 7]);
                 }
-                if constexpr (HALF) top = max_of(__builtin_fmaf(t[0], a.c, e0), __builtin_fmaf(t[1], a.c, e1));
-                else top = max_of(t[0], t[1]) * a.c;
-                top = max_across_32(top);
+                top = max_across_32(max_of(t[0], t[1]) * a.c);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -1025,7 +946,6 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
                 for (int e = 0; e < 16; ++e) o[dt][e] *= alpha;
         }
         const float m_use = m == -__builtin_inff() ? 0.f : m;
-        const float add[2] = {HALF ? e0 + kHalfShift - m_use : -m_use, HALF ? e1 + kHalfShift - m_use : -m_use};
         __builtin_amdgcn_sched_barrier(0);
         // the scores of the next step, this step's probabilities under it; its values are read for the step after
         float sum = 0.f;
@@ -1038,26 +958,18 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
                 float pr[2];
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                    pr[y] = exp2_of(__builtin_fmaf(s[set][2 * x + y], a.c, add[x >> 2]));
+                    pr[y] = exp2_of(__builtin_fmaf(s[set][2 * x + y], a.c, -m_use));
                     sum += pr[y];
                 }
                 pin(sum);
-                if constexpr (HALF) {
-                    const v2h q2 = {(_Float16)pr[0], (_Float16)pr[1]};
-                    pf[x >> 2][0][x & 3] = __builtin_bit_cast(uint32_t, q2);
-                    pin(pf[x >> 2][0][x & 3]);
-                    if (x == 3) { l += __builtin_ldexpf(sum, -(int)e0); sum = 0.f; }
-                    if (x == 7) l += __builtin_ldexpf(sum, -(int)e1);
-                } else {
-                    uint32_t w[P];
-                    pieces_of<P>(pr[0], pr[1], w);
+                uint32_t w[P];
+                pieces_of<P>(pr[0], pr[1], w);
 #pragma unroll
-                    for (int p = 0; p < P; ++p) {
-                        pf[x >> 2][p][x & 3] = w[p];
-                        pin(w[p]);
-                    }
-                    if (x == 7) l += sum;
+                for (int p = 0; p < P; ++p) {
+                    pf[x >> 2][p][x & 3] = w[p];
+                    pin(w[p]);
                 }
+                if (x == 7) l += sum;
             }
             if (n == NQ / 2 - 1 || n == NQ - 1) {
 #pragma unroll
@@ -1086,7 +998,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
         for (int kb = begin; kb < stop; kb += kTileKeys) {
             if constexpr (BLOCK == 0) __builtin_amdgcn_s_waitcnt(0x0F70);     // vmcnt(0): the copies
             __syncthreads();
-            if (kCopyV && kb + kTileKeys > len) {
+            if (BLOCK == 0 && kb + kTileKeys > len) {
                 const v4u zero = {0, 0, 0, 0};                                // rows of the stage lie one after another
                 for (int x = (len - kb) * DT * 2 + threadIdx.x * 16; x < kTensor; x += 4096) lds_write(lds0 + kVBase + slot + x, zero);
                 __syncthreads();
@@ -1096,12 +1008,10 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
                 load_v(slot ^ kTensor, kb + kTileKeys);
                 load_k(slot ^ kTensor, kb + kTileKeys + 32);
             }
-            float4 e = make_float4(0.f, 0.f, 0.f, 0.f);
-            if constexpr (HALF) e = *reinterpret_cast<const float4*>(smem + kExp + (slot ? 16 : 0));
             constexpr auto first = std::integral_constant<int, 0>{};
             constexpr auto second = std::integral_constant<int, 32 * DT * 2>{};
-            step(std::integral_constant<int, 0>{}, kb, first, first, e.x, e.y);
-            step(std::integral_constant<int, 1>{}, kb + 32, second, second, e.z, e.w);
+            step(std::integral_constant<int, 0>{}, kb, first, first);
+            step(std::integral_constant<int, 1>{}, kb + 32, second, second);
             const int to_other = slot ? -kTensor : kTensor;
             slot ^= kTensor;
 #pragma unroll
@@ -1401,7 +1311,7 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         many_rows = (int64_t)p.tiles * base.heads * kTileRows;
         many.part_o = (float*)parts;
         many.part_ml = (float2*)(many.part_o + many_rows * p.chunk_splits * base.dim);
-        constexpr int lds = 4 * kTileKeys * DT * 2 + 32;
+        constexpr int lds = 4 * kTileKeys * DT * 2;
         static_assert(sizeof(DecodeLds<DT>) <= lds, "both share the workgroup's LDS");
         static std::atomic<uint64_t> raised{0};
         if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_mixed_kernel<TYPE, DT, BLOCK, DC>, lds, raised)) return MX_ERR_DEVICE;
