@@ -447,9 +447,10 @@ MX_API mx_status mx_cache_append(const void* k, const void* v, int32_t type, int
  * the probabilities with 24; in MX_BF16 calls those of requests with more than sixteen rows (token, head of a group) enter as two
  * bfloat16 numbers, which leave 2^-16 of a probability at most.  Same inputs, same bits.  Cached values and probabilities below
  * 2^-126 may count as zero.  Of the cached values a token does not see none has a part in its result.
- * workspace: mx_cache_attention_workspace_bytes(...) bytes for the same arguments, 256-byte aligned, caller-owned; its first
- *   65536 bytes must be zero when the call starts and are zero again afterwards, the rest needs no initial value.  Calls that
- *   may overlap in time need a workspace each.
+ * workspace: mx_cache_attention_workspace_bytes(...) bytes for the same arguments or larger ones (the size grows with each of
+ *   tokens, requests, max_new and max_len, to 0.55 GB at most: a workspace made for the largest batch serves all), 256-byte
+ *   aligned, caller-owned; its first 65536 bytes must be zero when the call starts and are zero again afterwards, the rest needs
+ *   no initial value.  Calls that may overlap in time need a workspace each.
  * heads_q a multiple of c.heads; requests <= 16384, else MX_ERR_UNSUPPORTED.
  */
 MX_API size_t mx_cache_attention_workspace_bytes(mx_cache c, int64_t tokens, int64_t requests, int32_t heads_q,

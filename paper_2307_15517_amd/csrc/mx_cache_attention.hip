@@ -25,7 +25,7 @@ struct CacheAttnArgs {
     int64_t width;
     const int32_t* q_start;
     const int32_t* kv_len;
-    float* part_o;             // [part row][split][dim], unnormalised
+    float* part_o;             // [part row][split][dim], unnormalised; part rows: of decode() [unit][part_rows], of chunk() [head][packed row]
     float2* part_ml;           // [part row][split]: row maximum (exp2 domain), row sum
     uint32_t* counters;        // of the workgroups of a unit that have stored their part; zero between calls
     int64_t tokens;
@@ -37,7 +37,7 @@ struct CacheAttnArgs {
     int32_t splits;            // of this launch, at most
     int32_t run;               // chunk(): tiles of keys that a split is given
     int32_t least, most;       // this launch takes the requests that have least .. most rows (token, head of a group)
-    int32_t part_rows;         // part rows per unit; a request with more rows is not split
+    int32_t part_rows;         // decode(): part rows per unit; a request with more rows is not split
     int32_t tiles;             // chunk(): row tiles of all requests, at most
     int32_t sorted;            // cache_decode_kernel: the longest requests go first
     int32_t join;              // the workgroup of a unit that comes last joins its parts; else a launch of its own does
@@ -653,6 +653,11 @@ __device__ __forceinline__ Tile find_tile(const CacheAttnArgs& a, int tile) {
     return Tile{-1, 0, Request{0, 0, 0}};
 }
 
+// Part row of row r of a request: the rows of a head lie one after another, as the tokens are packed.
+__device__ __forceinline__ int64_t part_row_of(const CacheAttnArgs& a, int h, const Request& rq, int r) {
+    return (h * a.tokens + rq.t0) * a.group + r;
+}
+
 // The keys of the request that some row of the tile sees, and the splits that they are given: as many as there are runs of them.
 __device__ __forceinline__ int keys_seen(const CacheAttnArgs& a, const Tile& t) {
     return max(0, t.rq.len - t.rq.n + min(t.index * kTileRows + kTileRows - 1, t.rq.n * a.group - 1) / a.group + 1);
@@ -1032,7 +1037,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
         const float ll = __uint_as_float(both[0]) + __uint_as_float(both[1]);
         const float inv = splits > 1 ? 1.f : ll > 0.f ? 1.f / ll : 0.f;
-        const int64_t prow = (((int64_t)tile_id * a.heads + h) * kTileRows + 32 * wave + i) * a.splits + split;
+        const int64_t prow = part_row_of(a, h, rq, r) * a.splits + split;
         if (splits > 1 && h2 == 0) a.part_ml[prow] = make_float2(m, ll);
         const int64_t to = (int64_t)(rq.t0 + tok) * a.ldo + (int64_t)head * dim;
 #pragma unroll
@@ -1069,8 +1074,9 @@ template <int TYPE, bool CHUNK>
 __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
     __shared__ float4 lds[8][32];
     const int group = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t prow = blockIdx.x;
-    const int unit = (int)(prow / a.part_rows), row = (int)(prow - (int64_t)unit * a.part_rows);
+    int64_t prow = blockIdx.x;
+    const int per_unit = CHUNK ? kTileRows : a.part_rows;
+    const int unit = (int)(prow / per_unit), row = (int)(prow - (int64_t)unit * per_unit);
     const int h = unit % a.heads;
     int b = unit / a.heads, r = row, splits = a.splits;
     if constexpr (CHUNK) {
@@ -1088,6 +1094,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(CacheAttnArgs a) {
     const int64_t rows = (int64_t)rq.n * a.group;
     if (r >= rows || rows < a.least || rows > a.most || (!CHUNK && rows > a.part_rows)) return;
     const int tok = r / a.group, head = h * a.group + (r - tok * a.group);
+    if constexpr (CHUNK) prow = part_row_of(a, h, rq, r);
 
     float2 ml[2];
 #pragma unroll
@@ -1140,7 +1147,7 @@ __global__ __launch_bounds__(256) void cache_join_tiles_kernel(CacheAttnArgs a) 
     if (t.b < 0) return;
     const int first = t.index * kTileRows, rows = min(kTileRows, t.rq.n * a.group - first);
     const int d = 4 * lane < a.dim ? 4 * lane : 0;
-    const int64_t part_row = (int64_t)unit * kTileRows;
+    const int64_t part_row = part_row_of(a, h, t.rq, first);
     const int splits = splits_of(a, keys_seen(a, t));
     if (base >= rows || splits == 1) return;                               // (of a single split the rows are there)
     float x[4][4], m[4], l[4];
@@ -1213,8 +1220,14 @@ struct Plan {
     bool decode, chunk;
     int part_rows, splits;         // of cache_decode_kernel
     int tiles, chunk_splits, run;
-    size_t few_bytes, bytes;
+    size_t few_bytes;
 };
+
+// Workgroups that split keys, at most: 40 and 8 times what the GPU holds of either kind, past which finer runs even nothing out.  They
+// bound the parts, so that a workspace for a batch serves every smaller one, which may well be split more often.
+constexpr int64_t kMostDecode = 32768, kMostChunks = 4096;
+constexpr int kDecodeSlots = 768;                  // of bfloat16 calls; 512 of fp32 ones
+constexpr int kLongRun = 4096;                     // keys of a run in decode(), at most, while kMostDecode allows it
 
 // Splits of the longest tiles' keys, `tiles` tiles of 64 each, for `groups` workgroups, `slots` of which the GPU holds at once, and
 // `other` tiles' time of work beside them.  A workgroup's start and end count as kStart tiles, a part's store and its join as two.
@@ -1226,7 +1239,7 @@ int chunk_splits(int64_t groups, int64_t tiles, int64_t slots, int64_t other, bo
     constexpr int kStart = 5;
     int best = 1;
     double least = 1e300;
-    for (int s = 1; s <= kMaxSplits && s <= tiles; ++s) {
+    for (int s = 1; s <= kMaxSplits && s <= tiles && (s == 1 || groups * s <= kMostChunks); ++s) {
         const int64_t fixed = kStart + (s > 1 ? 2 : 0), longest = ceil_div(tiles, s) + fixed, rounds = ceil_div(groups * s, slots);
         double cost = (double)(rounds * longest);
         if (!one) {
@@ -1255,6 +1268,8 @@ int decode_splits(int64_t blocks, int least, int most, int rows) {
     return best;
 }
 
+size_t part_bytes(const mx_cache& c, int64_t parts) { return ((size_t)parts * ((size_t)c.dim * 4 + 8) + 255) / 256 * 256; }
+
 Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len) {
     Plan p{};
     if (max_len > INT32_MAX) max_len = INT32_MAX;      // no sum or product below leaves 64 bits
@@ -1265,8 +1280,11 @@ Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, 
     p.part_rows = (int)(most < kFewRows ? most : kFewRows);
     auto clamp = [](int64_t v, int64_t hi) { return (int)(v > hi ? (hi < 1 ? 1 : hi) : v < 1 ? 1 : v); };
     const int64_t units = requests * c.heads;
-    // at most as many workgroups as the GPU holds at once, but no run of keys over 4096, which would leave the last ones alone at the end
-    const int64_t slots = type == MX_F32 ? 512 : 768, even = units > 0 ? slots / units : 1, fine = ceil_div(max_len, 4096);
+    // at most as many workgroups as the GPU holds at once, but no run of keys over kLongRun, which would leave the last ones alone at
+    // the end
+    const int64_t slots = type == MX_F32 ? 512 : kDecodeSlots, even = units > 0 ? slots / units : 1;
+    int64_t fine = ceil_div(max_len, kLongRun);
+    if (units > 0 && units * fine > kMostDecode) fine = kMostDecode / units;
     p.splits = units <= kCounterBytes / 4 ? decode_splits(ceil_div(max_len, 128), clamp(fine, kMaxSplits), clamp(even > fine ? even : fine, kMaxSplits),
                                                               p.chunk ? 0 : p.part_rows) : 1;
     const int64_t rows = tokens * group;
@@ -1276,10 +1294,22 @@ Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, 
     p.chunk_splits = p.chunk ? chunk_splits((rows / kTileRows + 1) * c.heads, ceil_div(max_len, kTileKeys), type == MX_F32 ? 256 : 512,
                                             p.decode ? units * (max_len / 128) : 0, requests == 1) : 1;
     p.run = clamp(ceil_div(ceil_div(max_len, kTileKeys), p.chunk_splits), 1 << 24);
-    auto part_bytes = [&](size_t rows, int splits) { return splits > 1 ? (rows * splits * ((size_t)c.dim * 4 + 8) + 255) / 256 * 256 : 0; };
-    p.few_bytes = p.decode ? part_bytes((size_t)units * p.part_rows, p.splits) : 0;
-    p.bytes = kCounterBytes + p.few_bytes + (p.chunk ? part_bytes((size_t)p.tiles * c.heads * kTileRows, p.chunk_splits) : 0);
+    p.few_bytes = p.decode && p.splits > 1 ? part_bytes(c, units * p.part_rows * p.splits) : 0;
     return p;
+}
+
+// What any plan for these arguments, or for smaller ones, needs: every term grows with every argument.  Parts of decode(): units * splits is
+// at most what the GPU holds, or units times the runs of kLongRun keys; of chunk(): the workgroups that split are at least a
+// 128th of the rows.  At most 273 MB a kind with heads of 128.
+size_t workspace_bytes(const mx_cache& c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len) {
+    if (max_len > INT32_MAX) max_len = INT32_MAX;
+    auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
+    const int64_t group = heads_q / c.heads, most = least(max_new, tokens) * group;
+    const int64_t units = least(requests * c.heads, kCounterBytes / 4), fine = least(ceil_div(max_len, kLongRun), kMaxSplits);
+    const int64_t long_runs = fine > 1 ? least(units * fine, kMostDecode) : 0;
+    const int64_t few = least(units * least(ceil_div(max_len, 128), kMaxSplits), long_runs > kDecodeSlots ? long_runs : kDecodeSlots);
+    const int64_t many = most > kFewRows ? least(tokens * heads_q * least(ceil_div(max_len, kTileKeys), kMaxSplits), kMostChunks * kTileRows) : 0;
+    return kCounterBytes + part_bytes(c, few * least(most, kFewRows)) + part_bytes(c, many);
 }
 
 template <int TYPE, int DT, int BLOCK, int DC>
@@ -1307,10 +1337,9 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         many.splits = p.chunk_splits;
         many.run = p.run;
         many.tiles = p.tiles;
-        many.part_rows = kTileRows;
         many_rows = (int64_t)p.tiles * base.heads * kTileRows;
         many.part_o = (float*)parts;
-        many.part_ml = (float2*)(many.part_o + many_rows * p.chunk_splits * base.dim);
+        many.part_ml = (float2*)(many.part_o + base.tokens * base.heads_q * p.chunk_splits * base.dim);
         constexpr int lds = 4 * kTileKeys * DT * 2;
         static_assert(sizeof(DecodeLds<DT>) <= lds, "both share the workgroup's LDS");
         static std::atomic<uint64_t> raised{0};
@@ -1362,9 +1391,7 @@ extern "C" size_t mx_cache_attention_workspace_bytes(mx_cache c, int64_t tokens,
     if (cache_status(c) != MX_OK || !attention_args_ok(c, tokens, requests, heads_q, max_new, max_len) ||
         !attention_supported(c, tokens, requests, heads_q))
         return 0;
-    const size_t a = plan_of(c, MX_F32, tokens, requests, heads_q, max_new, max_len).bytes;
-    const size_t b = plan_of(c, MX_BF16, tokens, requests, heads_q, max_new, max_len).bytes;
-    return a > b ? a : b;                             // the same buffer serves calls of either type
+    return workspace_bytes(c, tokens, requests, heads_q, max_new, max_len);
 }
 
 extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32_t heads_q, mx_cache c,

@@ -505,9 +505,11 @@ def cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Te
 
 
 def cache_workspace(c: mx_cache, tokens: int, requests: int, heads_q: int, max_new: int, max_len: int, device) -> torch.Tensor:
-    """A zero-filled workspace for mx_cache_attention (its counters must be zero before the first call)."""
-    return torch.zeros(max(1, mx_cache_attention_workspace_bytes(c, tokens, requests, heads_q, max_new, max_len)),
-                       dtype=torch.uint8, device=device)
+    """A workspace for mx_cache_attention with these or smaller numbers; its counters, the first 65536 bytes, are zero."""
+    space = torch.empty(max(1, mx_cache_attention_workspace_bytes(c, tokens, requests, heads_q, max_new, max_len)),
+                        dtype=torch.uint8, device=device)
+    space[:65536].zero_()
+    return space
 
 
 def cache_attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int,
