@@ -515,7 +515,8 @@ def cache_workspace(c: mx_cache, tokens: int, requests: int, heads_q: int, max_n
 def cache_attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor, max_new: int,
                     max_len: int, scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None,
                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """q: [tokens, heads_q*dim]; scale: 1/sqrt(dim) unless given.  Returns [tokens, heads_q*dim] in the type of q."""
+    """q: [tokens, heads_q*dim]; scale: 1/sqrt(dim) unless given; workspace: of cache_workspace with these or larger numbers, made
+    for this call unless given.  Returns [tokens, heads_q*dim] in the type of q."""
     dim, requests = cache.c.dim, table.shape[0]
     assert table.dim() == 2 and table.is_contiguous() and q_start.numel() == requests + 1 and kv_len.numel() == requests
     for t in (table, q_start, kv_len):
@@ -526,6 +527,10 @@ def cache_attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, q_start:
     assert out.shape == q.shape and out.dtype == q.dtype and out.stride(-1) == 1 and q.shape[1] == heads_q * dim
     if workspace is None:
         workspace = cache_workspace(cache.c, q.shape[0], requests, heads_q, max_new, max_len, q.device)
+    else:                                                    # the call itself cannot tell, and would write past its end
+        need = mx_cache_attention_workspace_bytes(cache.c, q.shape[0], requests, heads_q, max_new, max_len)
+        if workspace.device != q.device or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
+            raise MxError(MX_ERR_BAD_ARG, "cache_attention: a workspace of %d bytes on the GPU of q is wanted" % need)
     mx_cache_attention(q, _activation_type(q), q.shape[0], q.stride(0), heads_q, cache.c, cache.k, cache.k_exps, cache.v,
                        cache.v_exps, table, table.shape[1], q_start, kv_len, requests, max_new, max_len,
                        dim ** -0.5 if scale is None else scale, workspace, out, out.stride(0))

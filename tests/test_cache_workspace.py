@@ -63,3 +63,18 @@ def test_one_workspace_for_all_steps(dtype, heads, group, dim):
             assert step.tokens <= most[0] and len(lens) <= most[1] and max_new <= most[2] and max_len <= most[3]
             step.check(workspace=space[:need], max_new=max_new, max_len=max_len)
         assert bool((space[need:] == 0xA5).all()) and not space[:65536].any()
+
+
+@gpu
+def test_a_workspace_that_does_not_fit_is_refused():
+    step = Step([(1, 5000), (20, 300)], 4, 3, 64, 16, FORMATS["mx32"], torch.float32, seed=3)
+    need = size(4, 3, 64, step.tokens, 2, step.max_new, step.max_len)
+    whole = torch.zeros(2 * need, dtype=torch.uint8, device=DEV)
+    for bad in (whole[:need - 1], whole[:65536], whole[::2], torch.zeros(need, dtype=torch.uint8), whole[:0]):
+        with pytest.raises(mx.MxError) as e:
+            step.run(workspace=bad)
+        assert e.value.status == mx.MX_ERR_BAD_ARG
+    step.check(workspace=whole[:need])
+    step.check(workspace=torch.zeros(need // 4 + 1, dtype=torch.int32, device=DEV))
+    with pytest.raises(mx.MxError):                          # enough for its own numbers, not for larger bounds
+        step.run(workspace=whole[:need], max_new=1000, max_len=50000)
