@@ -61,8 +61,8 @@ class Server:
         self.places = [None] * batch
         self.free = list(range(pages))
         self.owned = [[] for _ in range(batch)]       # the host's own list of the pages that a place holds
-        tokens = batch * chunk
-        self.workspace = mx.cache_workspace(self.cache.c, tokens, batch, HEADS_Q, chunk, max_len, device)
+        # of the largest step; smaller ones need no more
+        self.workspace = mx.cache_workspace(self.cache.c, batch * chunk, batch, HEADS_Q, chunk, max_len, device)
 
     def admit(self, waiting):
         for i in range(self.batch):
@@ -81,7 +81,7 @@ class Server:
         y = self.qkv(self.embedding[torch.tensor(ids).to(self.device)])
         q, k, v = y[:, :HEADS_Q * DIM], y[:, HEADS_Q * DIM:(HEADS_Q + HEADS) * DIM], y[:, (HEADS_Q + HEADS) * DIM:]
         mx.cache_append(self.cache, k, v, slots)
-        o = mx.cache_attention(self.cache, q, self.table, q_start, kv_len, max(new), self.max_len, None, self._space(len(ids)))
+        o = mx.cache_attention(self.cache, q, self.table, q_start, kv_len, max(new), self.max_len, None, self.workspace)
         self.last = (q, o, q_start, kv_len)                           # for a look at the step from outside
         last = [sum(new[:i + 1]) - 1 for i in range(self.batch) if new[i]]
         answers = iter((self.out(o[last]) @ self.embedding.T).argmax(-1).tolist())
@@ -106,12 +106,6 @@ class Server:
                     self.owned[i], self.places[i] = [], None
         assert taken == 0
         return done
-
-    def _space(self, tokens):
-        need = mx.mx_cache_attention_workspace_bytes(self.cache.c, tokens, self.batch, HEADS_Q, self.chunk, self.max_len)
-        if need > self.workspace.numel():                             # (rare: the first one is made for the most tokens)
-            self.workspace = torch.zeros(need, dtype=torch.uint8, device=self.device)
-        return self.workspace
 
 
 def main():
