@@ -52,7 +52,7 @@ class Server:
 
         def matrix(rows, cols):
             return torch.randn((rows, cols), generator=g, device=device) * cols ** -0.5
-        self.device, self.batch, self.page, self.chunk, self.max_len = device, batch, page, chunk, max_len
+        self.device, self.batch, self.pages, self.page, self.chunk, self.max_len = device, batch, pages, page, chunk, max_len
         self.embedding = torch.randn((VOCAB, HIDDEN), generator=g, device=device)
         self.qkv, self.out = Linear(matrix(QKV, HIDDEN)), Linear(matrix(HIDDEN, HEADS_Q * DIM))
         self.cache = mx.Cache(pages, page, HEADS, DIM, f, device)
@@ -64,10 +64,20 @@ class Server:
         # of the largest step; smaller ones need no more
         self.workspace = mx.cache_workspace(self.cache.c, batch * chunk, batch, HEADS_Q, chunk, max_len, device)
 
+    def _pages_of(self, request):
+        """The pages that a request holds at its end."""
+        return -(-request.stop // self.page)
+
     def admit(self, waiting):
+        """Gives places to the first that wait, as long as the pages cover what all with a place will hold at their ends."""
+        for request in waiting:
+            if not request.tokens or request.stop > self.max_len or self._pages_of(request) > self.pages:
+                raise ValueError("a request of 1 to %d tokens is wanted" % min(self.max_len, self.pages * self.page))
+        lacking = sum(self._pages_of(r) - len(o) for r, o in zip(self.places, self.owned) if r is not None)
         for i in range(self.batch):
-            if self.places[i] is None and waiting and len(self.free) >= self.width:
+            if self.places[i] is None and waiting and lacking + self._pages_of(waiting[0]) <= len(self.free):
                 self.places[i] = waiting.pop(0)
+                lacking += self._pages_of(self.places[i])
 
     def step(self):
         """Feeds every request its next chunk or token.  Returns the finished requests."""
