@@ -138,7 +138,7 @@ def _stream(stream) -> int:
 
 
 def _p(t) -> Optional[int]:
-    return t.data_ptr() if isinstance(t, torch.Tensor) else t
+    return t if t is None or isinstance(t, int) else t.data_ptr()
 
 
 def _raise(status: int, what: str):
