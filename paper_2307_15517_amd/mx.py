@@ -499,7 +499,7 @@ def cache_plan(ctx_len: torch.Tensor, new_len: torch.Tensor, page: int, free_pag
 def cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """k, v: [tokens, heads*dim], float32 or bfloat16, contiguous along the last axis (slices of a projection will do)."""
     assert k.shape == v.shape and k.shape[1] == cache.c.heads * cache.c.dim and k.dtype == v.dtype and slots.numel() == k.shape[0]
-    assert slots.dtype == torch.int32 and v.is_cuda and v.stride(-1) == 1
+    assert slots.dtype == torch.int32 and slots.is_cuda and slots.is_contiguous() and v.is_cuda and v.stride(-1) == 1
     mx_cache_append(k, v, _activation_type(k), k.shape[0], k.stride(0), v.stride(0), cache.c, cache.k, cache.k_exps, cache.v,
                     cache.v_exps, slots)
 
@@ -524,7 +524,7 @@ def cache_attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, q_start:
     heads_q = q.shape[1] // dim
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape and out.dtype == q.dtype and out.stride(-1) == 1 and q.shape[1] == heads_q * dim
+    assert out.shape == q.shape and out.dtype == q.dtype and out.is_cuda and out.stride(-1) == 1 and q.shape[1] == heads_q * dim
     if workspace is None:
         workspace = cache_workspace(cache.c, q.shape[0], requests, heads_q, max_new, max_len, q.device)
     else:                                                    # the call itself cannot tell, and would write past its end

@@ -14,3 +14,25 @@ def test_anything_with_a_data_pointer_is_a_pointer():
             with pytest.raises(mx.MxError) as e:
                 call()
             assert e.value.status == mx.MX_ERR_BAD_ARG
+
+
+@pytest.mark.gpu
+def test_index_arrays_and_outputs_elsewhere_are_refused():
+    """A slot array on the host or with gaps, an output on the host: refused before the call, and nothing is written."""
+    dev = "cuda:0"
+    cache = mx.Cache(4, 16, 2, 64, mx.fmt(32, 8), dev)
+    x = torch.ones((8, 128), device=dev)
+    slots = torch.arange(16, dtype=torch.int32, device=dev)
+    for bad in (slots[:8].cpu(), slots[::2], slots[:8].long(), slots[:7]):
+        with pytest.raises(AssertionError):
+            mx.cache_append(cache, x, x, bad)
+    assert not cache.k.any() and not cache.v.any()
+    mx.cache_append(cache, x, x, slots[:8])
+    table, q_start, kv_len = (torch.tensor(t, dtype=torch.int32, device=dev) for t in ([[0, 1]], [0, 8], [8]))
+    for out in (torch.empty((8, 256)), torch.empty((8, 256), device=dev, dtype=torch.bfloat16), torch.empty((8, 512), device=dev)[:, ::2]):
+        with pytest.raises(AssertionError):
+            mx.cache_attention(cache, x.repeat(1, 2), table, q_start, kv_len, 8, 8, out=out)
+    for bad in (table.cpu(), table.long(), table.repeat(1, 2)[:, ::2]):
+        with pytest.raises(AssertionError):
+            mx.cache_attention(cache, x.repeat(1, 2), bad, q_start, kv_len, 8, 8)
+    assert bool((mx.cache_attention(cache, x.repeat(1, 2), table, q_start, kv_len, 8, 8) == 1.0).all())
