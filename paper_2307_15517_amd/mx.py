@@ -483,6 +483,11 @@ def _activation_type(x: torch.Tensor) -> int:
     return MX_F32 if x.dtype == torch.float32 else MX_BF16
 
 
+def _row_stride(x: torch.Tensor) -> int:
+    """Elements from a row to the next; the stride of a single row says nothing."""
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
 def cache_plan(ctx_len: torch.Tensor, new_len: torch.Tensor, page: int, free_pages: torch.Tensor, table: torch.Tensor,
                tokens: int) -> Tuple[torch.Tensor, ...]:
     """(q_start, kv_len, slots, positions, counts) of a step; ``table`` [requests, width] receives the new pages."""
@@ -500,7 +505,7 @@ def cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Te
     """k, v: [tokens, heads*dim], float32 or bfloat16, contiguous along the last axis (slices of a projection will do)."""
     assert k.shape == v.shape and k.shape[1] == cache.c.heads * cache.c.dim and k.dtype == v.dtype and slots.numel() == k.shape[0]
     assert slots.dtype == torch.int32 and slots.is_cuda and slots.is_contiguous() and v.is_cuda and v.stride(-1) == 1
-    mx_cache_append(k, v, _activation_type(k), k.shape[0], k.stride(0), v.stride(0), cache.c, cache.k, cache.k_exps, cache.v,
+    mx_cache_append(k, v, _activation_type(k), k.shape[0], _row_stride(k), _row_stride(v), cache.c, cache.k, cache.k_exps, cache.v,
                     cache.v_exps, slots)
 
 
@@ -531,7 +536,7 @@ def cache_attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, q_start:
         need = mx_cache_attention_workspace_bytes(cache.c, q.shape[0], requests, heads_q, max_new, max_len)
         if workspace.device != q.device or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
             raise MxError(MX_ERR_BAD_ARG, "cache_attention: a workspace of %d bytes on the GPU of q is wanted" % need)
-    mx_cache_attention(q, _activation_type(q), q.shape[0], q.stride(0), heads_q, cache.c, cache.k, cache.k_exps, cache.v,
+    mx_cache_attention(q, _activation_type(q), q.shape[0], _row_stride(q), heads_q, cache.c, cache.k, cache.k_exps, cache.v,
                        cache.v_exps, table, table.shape[1], q_start, kv_len, requests, max_new, max_len,
-                       dim ** -0.5 if scale is None else scale, workspace, out, out.stride(0))
+                       dim ** -0.5 if scale is None else scale, workspace, out, _row_stride(out))
     return out

@@ -36,3 +36,20 @@ def test_index_arrays_and_outputs_elsewhere_are_refused():
         with pytest.raises(AssertionError):
             mx.cache_attention(cache, x.repeat(1, 2), bad, q_start, kv_len, 8, 8)
     assert bool((mx.cache_attention(cache, x.repeat(1, 2), table, q_start, kv_len, 8, 8) == 1.0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_single_row_of_any_stride(dtype):
+    """One new token whose row comes from a column: its stride from row to row is one element, and means nothing."""
+    dev = "cuda:0"
+    cache = mx.Cache(1, 16, 2, 64, None, dev)
+    x = torch.randn((128, 1), device=dev).to(dtype).t()
+    assert x.shape == (1, 128) and x.stride() == (1, 1)
+    mx.cache_append(cache, x, x, torch.tensor([3], dtype=torch.int32, device=dev))
+    assert torch.equal(cache.k.view(torch.bfloat16).reshape(2, 16, 64)[:, 3].reshape(1, 128), x.to(torch.bfloat16))
+    table, q_start, kv_len = (torch.tensor(t, dtype=torch.int32, device=dev) for t in ([[0]], [0, 1], [4]))
+    q = torch.randn((128, 1), device=dev).to(dtype).t()
+    out = torch.empty((128, 1), device=dev, dtype=dtype).t()
+    got = mx.cache_attention(cache, q, table, q_start, kv_len, 1, 4, out=out)
+    assert got is out and torch.equal(out, mx.cache_attention(cache, q.clone(memory_format=torch.contiguous_format), table, q_start, kv_len, 1, 4))
