@@ -375,7 +375,7 @@ MX_API mx_status mx_linear_static_workspace(const float* x, int64_t M, int64_t K
  * A cache is a pool of pages; a page holds `page` consecutive tokens of one request for every key/value head.  Keys and
  * values are two arrays of the same geometry, data [pages][heads][page][dim]: the tokens of a page and head lie one after
  * another, so attention streams them, and a page is free for any request.  With f.block = 0 an element is a bfloat16 number
- * (exps is not used and may be null).  Otherwise the elements are MXInt with blocks of f.block along the head dimension (the
+ * (the other fields of f and exps are not used; exps may be null).  Otherwise the elements are MXInt with blocks of f.block along the head dimension (the
  * axis the scores are reduced over; Section 3.2: an operator takes quantized inputs): data holds the mantissas, one byte each,
  * exps [pages][heads][page][dim/f.block] the exponent bytes.  That is the canonical form of a (pages*heads*page) x dim tensor,
  * so mx_dequantize reads a cache back.

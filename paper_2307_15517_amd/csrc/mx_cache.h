@@ -21,6 +21,9 @@ inline mx_status cache_status(const mx_cache& c) {
     return MX_OK;
 }
 
+// An exponent byte e stands for 2^(e - bias) of a block's elements.  With bfloat16 elements the format's other fields may be anything.
+inline int exponent_bias(const mx_cache& c) { return c.f.block == 0 ? 0 : (1 << (c.f.exp_bits - 1)) - 1; }
+
 inline bool aligned(const void* p, uintptr_t n) { return (uintptr_t)p % n == 0; }
 
 // Floats of type MX_F32 or MX_BF16: bytes, and eight of them from memory that is (VEC) or need not be 16-byte aligned.

@@ -284,8 +284,8 @@ extern "C" mx_status mx_cache_append(const void* k, const void* v, int32_t type,
     a.heads = c.heads;
     a.row_octets = c.dim / 8;
     a.page_log2 = log2_of(c.page);
-    a.bias = (1 << (c.f.exp_bits - 1)) - 1;
-    a.emax = 1 << (c.f.exp_bits - 1);
+    a.bias = exponent_bias(c);
+    a.emax = a.bias + 1;
     a.rounding = c.f.rounding;
     const int64_t slice = (((int64_t)1 << 31) - 256) / (row / 8);         // tokens whose octets a launch can number
     for (int64_t t = 0; t < tokens; t += slice) {

@@ -1431,7 +1431,7 @@ extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tok
     a.pages = (uint32_t)c.pages;
     a.requests = (int32_t)requests; a.heads = c.heads; a.group = heads_q / c.heads; a.heads_q = heads_q; a.dim = c.dim;
     a.page_log2 = log2_of(c.page);
-    a.exp_shift = (1 << (c.f.exp_bits - 1)) - 1 + 6;
+    a.exp_shift = exponent_bias(c) + 6;
     a.vec_q = aligned(q, 16) && ldq % (16 / tb) == 0;
     a.vec_o = aligned(out, 4 * tb) && ldo % 4 == 0;
     a.c = __builtin_fmaxf(__builtin_fabsf(scale) * 1.4426950408889634f, 0x1p-126f);   // never 0: minus infinity stays a mask

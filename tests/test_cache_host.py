@@ -1,0 +1,92 @@
+"""The host side of the paged cache's calls under UndefinedBehaviorSanitizer (host code only, no GPU): compiled with a runtime
+that registers nothing and launches nothing, so that every call runs up to its last launch."""
+import os
+import re
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+CLANG, NM = "/opt/rocm/llvm/bin/clang++", "nm"
+
+RUNTIME = r"""
+#include <cstdint>
+#include <cstdio>
+#include <cstring>
+#include <initializer_list>
+#include "mx.h"
+extern "C" {
+struct dim { unsigned x, y, z; };
+static dim grid, block;
+static size_t lds;
+static void* on;
+static int launches;
+static uint64_t threads;
+void** __hipRegisterFatBinary(const void*) { static void* handle; return &handle; }
+void __hipUnregisterFatBinary(void**) {}
+void __hipRegisterFunction(void**, const void*, char*, const char*, unsigned, void*, void*, void*, void*, int*) {}
+int __hipPushCallConfiguration(dim g, dim b, size_t n, void* s) { grid = g; block = b; lds = n; on = s; return 0; }
+int __hipPopCallConfiguration(dim* g, dim* b, size_t* n, void** s) { *g = grid; *b = block; *n = lds; *s = on; return 0; }
+int hipLaunchKernel(const void*, dim g, dim b, void**, size_t, void*) { ++launches; threads = (uint64_t)g.x * b.x; return 0; }
+int hipGetLastError() { return 0; }
+int hipGetDevice(int* d) { *d = 0; return 0; }
+int hipFuncSetAttribute(const void*, int, int) { return 0; }
+}
+static char at[1 << 12] __attribute__((aligned(256)));
+static mx_status append(const mx_cache& c, int64_t tokens) {
+    const int64_t row = (int64_t)c.heads * c.dim;
+    return mx_cache_append(at, at, MX_F32, tokens, row, row, c, at, (uint8_t*)at, at, (uint8_t*)at, (int32_t*)at, nullptr);
+}
+static mx_status attend(const mx_cache& c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len, int64_t width) {
+    const int64_t row = (int64_t)heads_q * c.dim;
+    return mx_cache_attention(at, MX_BF16, tokens, row, heads_q, c, at, (uint8_t*)at, at, (uint8_t*)at, (int32_t*)at, width, (int32_t*)at,
+                              (int32_t*)at, requests, max_new, max_len, 0.125f, at, at, row, nullptr);
+}
+"""
+
+
+@pytest.fixture(scope="module")
+def run(tmp_path_factory):
+    """Builds a program of the library's host code, the runtime above and a main(), and gives what it prints."""
+    if not (os.path.exists(HIPCC) and os.path.exists(CLANG) and shutil.which(NM)):
+        pytest.skip("no hipcc")
+    where = tmp_path_factory.mktemp("host")
+    include = ["-I" + os.path.join(ROOT, "include"), "-I" + os.path.join(ROOT, "paper_2307_15517_amd", "csrc")]
+    objects, fatbins = [], ""
+    for name in ("mx_cache", "mx_cache_attention"):
+        objects.append(str(where / (name + ".o")))
+        cmd = [HIPCC, "--offload-arch=gfx950", "--offload-host-only", "-O1", "-std=c++17", "-w", *include, "-Xarch_host",
+               "-fsanitize=undefined", "-Xarch_host", "-fno-sanitize-recover=all", "-Xarch_host", "-fno-sanitize=vptr,function",
+               "-c", os.path.join(ROOT, "paper_2307_15517_amd", "csrc", name + ".hip"), "-o", objects[-1]]
+        made = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        assert made.returncode == 0, made.stdout[-4000:]
+        names = subprocess.run([NM, "-u", objects[-1]], stdout=subprocess.PIPE, text=True, check=True).stdout
+        fatbins += "".join('extern "C" { char %s[64]; }\n' % n for n in re.findall(r"__hip_fatbin\w*", names))
+
+    def program(body):
+        source = where / "main.cpp"
+        source.write_text(RUNTIME + fatbins + "int main() {\n" + body + "\nreturn 0;\n}\n")
+        cmd = [CLANG, "-O1", "-std=c++17", "-w", *include, "-fsanitize=undefined", "-fno-sanitize-recover=all",
+               "-fno-sanitize=vptr,function", str(source), *objects, "-o", str(where / "main")]
+        made = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        assert made.returncode == 0, made.stdout[-4000:]
+        ran = subprocess.run([str(where / "main")], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=60)
+        assert ran.returncode == 0, ran.stdout[-4000:]
+        return ran.stdout.split()
+    return program
+
+
+def test_a_bfloat16_cache_needs_no_format(run):
+    """A format of zeros, as a C program leaves it for bfloat16 elements, and one of nonsense: block 0 is all that is read."""
+    assert run("""
+        mx_cache c{};
+        c.pages = 4; c.page = 16; c.heads = 2; c.dim = 64;
+        for (int bits : {0, -5, 40}) {
+            c.f.exp_bits = bits;
+            printf("%d ", append(c, 8));
+            printf("%d ", append(c, 0));
+            printf("%d ", attend(c, 8, 2, 4, 1, 64, 4));
+            printf("%d ", attend(c, 80, 2, 4, 60, 64, 4));
+        }""") == ["0"] * 12
