@@ -408,8 +408,9 @@ MX_API size_t mx_cache_exps_bytes(mx_cache c);
  * Out: q_start[requests + 1], the running sum of new_len from 0: the place of a request's tokens in the packed token dimension
  *   (it counts refused requests' tokens too; sums past 2^31 - 1 stay there); kv_len[requests] = ctx + new, 0 for a refused
  *   request; for each of `tokens` packed tokens slots[t], its place in the pool, and positions[t], its position in its request,
- *   both -1 for tokens of a refused request or past the last request's; counts[0] = pages taken from the head of free_pages,
- *   counts[1] = requests refused.  positions and counts may be null.
+ *   both -1 for tokens of a refused request or past the last request's, the slot also where the page index is negative or so
+ *   large that its slots pass 2^31 - 1; counts[0] = pages taken from the head of free_pages, counts[1] = requests refused.
+ *   positions and counts may be null.
  * All arrays are int32, on the device, 4-byte aligned.  page: a power of two from 16 to 1024.  requests <= 16384, else
  * MX_ERR_UNSUPPORTED.
  */

@@ -1,0 +1,22 @@
+"""Block tables and slots at the ends of 32 bits."""
+import pytest
+import torch
+
+from paper_2307_15517_amd import mx
+from test_cache import DEV, ints, run_plan
+
+gpu = pytest.mark.gpu
+
+
+@gpu
+@pytest.mark.parametrize("page", [16, 64, 1024])
+def test_page_indices_whose_slots_pass_32_bits_give_none(page):
+    """The largest page with slots below 2^31, the next, those that would come out at page 0 and 1 again, and negative ones; taken
+    from the free list (three tokens of a new request) and from the table (the next token of an old one)."""
+    last = (1 << 31) // page - 1
+    for entry in (last, last + 1, 2 * last + 1, 2 * last + 2, 2 * last + 3, 2 ** 31 - 1, -1, -2 ** 31):
+        if not -2 ** 31 <= entry < 2 ** 31:
+            continue
+        table, _, kv_len, slots, positions, _ = run_plan([0, 5], [3, 1], page, [entry], [[-1], [entry]], 4)
+        assert table == [[entry], [entry]] and kv_len == [3, 6] and positions == [0, 1, 2, 5]
+        assert slots == ([entry * page + i for i in (0, 1, 2, 5)] if 0 <= entry <= last else [-1] * 4), entry
