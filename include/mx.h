@@ -406,7 +406,7 @@ MX_API size_t mx_cache_exps_bytes(mx_cache c);
  * and including it exceed n_free; later requests that need pages are then refused too, others are served.  A refused request's
  * row stays as it is.
  * Out: q_start[requests + 1], the running sum of new_len from 0: the place of a request's tokens in the packed token dimension
- *   (it counts refused requests' tokens too; sums past 2^31 - 1 stay there); kv_len[requests] = ctx + new, 0 for a refused
+ *   (it counts refused requests' tokens too; sums, lengths and positions past 2^31 - 1 stay there); kv_len[requests] = ctx + new, 0 for a refused
  *   request; for each of `tokens` packed tokens slots[t], its place in the pool, and positions[t], its position in its request,
  *   both -1 for tokens of a refused request or past the last request's, the slot also where the page index is negative or so
  *   large that its slots pass 2^31 - 1; counts[0] = pages taken from the head of free_pages, counts[1] = requests refused.

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kPlanThreads) void cache_plan_kernel(PlanArgs a) {
             const int64_t c = length(a.ctx[lo]), pos = c + (t - start[lo]), have = pages_of(c);
             const int64_t j = pos >> a.page_log2;
             const int32_t entry = j < have ? a.table[lo * a.width + j] : a.free_pages[at[lo] + (j - have)];
-            position = (int32_t)pos;
+            position = (int32_t)(pos < INT32_MAX ? pos : INT32_MAX);
             if (entry >= 0 && entry <= INT32_MAX >> a.page_log2) slot = (int32_t)(((uint32_t)entry << a.page_log2) + (uint32_t)(pos & (page - 1)));
         }
         a.slots[t] = slot;

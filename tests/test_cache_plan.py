@@ -20,3 +20,16 @@ def test_page_indices_whose_slots_pass_32_bits_give_none(page):
         table, _, kv_len, slots, positions, _ = run_plan([0, 5], [3, 1], page, [entry], [[-1], [entry]], 4)
         assert table == [[entry], [entry]] and kv_len == [3, 6] and positions == [0, 1, 2, 5]
         assert slots == ([entry * page + i for i in (0, 1, 2, 5)] if 0 <= entry <= last else [-1] * 4), entry
+
+
+@gpu
+def test_positions_past_32_bits_stay_at_the_last():
+    """A request whose new tokens take it past 2^31 positions, in a table row wide enough for them."""
+    page, have = 16, (1 << 27) - 1                           # pages of the 2^31 - 20 cached tokens
+    table = torch.full((1, have + 4), 7, dtype=torch.int32, device=DEV)
+    q_start, kv_len, slots, positions, counts = mx.cache_plan(ints([2 ** 31 - 20]), ints([40]), page, ints([1, 2, 3, 4]), table, 40)
+    at = [2 ** 31 - 20 + i for i in range(40)]
+    pages = [7 if p // page < have else 1 + p // page - have for p in at]
+    assert positions.tolist() == [min(p, 2 ** 31 - 1) for p in at] and kv_len.tolist() == [2 ** 31 - 1]
+    assert slots.tolist() == [e * page + p % page for e, p in zip(pages, at)]
+    assert counts.tolist() == [3, 0] and table[0, have - 1:].tolist() == [7, 1, 2, 3, 7]
