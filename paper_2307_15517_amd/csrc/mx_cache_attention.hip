@@ -1377,8 +1377,11 @@ mx_status launch(const CacheAttnArgs& a, const Plan& p, int block, uint8_t* work
 bool attention_args_ok(const mx_cache& c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len) {
     return tokens >= 0 && requests >= 0 && heads_q >= 1 && c.heads >= 1 && heads_q % c.heads == 0 && max_new >= 1 && max_len >= 1;
 }
+// Keys of a request and its rows are counted in 32 bits, and the kernels look past the last one by tiles: of 128 keys for each of 64
+// splits, which is the most.
+constexpr int32_t kMostCounted = INT32_MAX - 65536;
 bool attention_supported(const mx_cache& c, int64_t tokens, int64_t requests, int32_t heads_q) {
-    return requests <= kCacheMaxRequests && tokens < ((int64_t)1 << 31) / heads_q && requests * c.heads < ((int64_t)1 << 24);
+    return requests <= kCacheMaxRequests && tokens <= kMostCounted / heads_q && requests * c.heads < ((int64_t)1 << 24);
 }
 
 }  // namespace
@@ -1417,7 +1420,7 @@ extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tok
         }
     }
     if (st != MX_OK) return st;
-    if (!attention_supported(c, tokens, requests, heads_q) || width > INT32_MAX / c.page) return MX_ERR_UNSUPPORTED;
+    if (!attention_supported(c, tokens, requests, heads_q) || width > kMostCounted / c.page) return MX_ERR_UNSUPPORTED;
     if (tokens == 0) return MX_OK;
     const Plan p = plan_of(c, type, tokens, requests, heads_q, max_new, max_len);
     if ((int64_t)p.tiles * c.heads * (p.chunk_splits > 1 ? kTileRows : 1) > INT32_MAX) return MX_ERR_UNSUPPORTED;

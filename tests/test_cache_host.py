@@ -90,3 +90,21 @@ def test_a_bfloat16_cache_needs_no_format(run):
             printf("%d ", attend(c, 8, 2, 4, 1, 64, 4));
             printf("%d ", attend(c, 80, 2, 4, 60, 64, 4));
         }""") == ["0"] * 12
+
+
+def test_lengths_near_the_end_of_32_bits_are_refused(run):
+    """A table row or packed rows so long that a kernel's key or row number, a tile past the last, would leave 32 bits."""
+    got = run("""
+        mx_cache c{};
+        c.pages = 4; c.heads = 1; c.dim = 64;
+        for (int page : {16, 128, 1024}) {
+            c.page = page;
+            for (int64_t room : {0, 127, 8192, 65535}) printf("%d ", attend(c, 1, 1, 1, 1, 1 << 20, (2147483647 - room) / page));
+            printf("%d ", attend(c, 1, 1, 1, 1, 1 << 20, (2147483647 - 65536) / page));
+        }
+        c.page = 16;
+        for (int heads_q : {1, 2, 7}) {
+            printf("%d ", attend(c, 2147483647 / heads_q, 1, heads_q, 1, 64, 4));
+            printf("%d ", attend(c, (2147483647 - 65536) / heads_q, 1, heads_q, 1, 64, 4));
+        }""")
+    assert got == ["2", "2", "2", "2", "0"] * 3 + ["2", "0"] * 3
