@@ -1203,10 +1203,11 @@ mx_status launch_join(const CacheAttnArgs& a, int64_t rows, hipStream_t stream) 
 template <int TYPE>
 __global__ __launch_bounds__(256) void cache_zero_kernel(CacheAttnArgs a) {
     const int64_t row = (int64_t)a.heads_q * a.dim;
-    for (int64_t d = threadIdx.x; d < row; d += 256) {
-        if constexpr (TYPE == MX_F32) static_cast<float*>(a.out)[blockIdx.x * a.ldo + d] = 0.f;
-        else static_cast<uint16_t*>(a.out)[blockIdx.x * a.ldo + d] = 0;
-    }
+    for (int64_t t = blockIdx.x; t < a.tokens; t += gridDim.x)
+        for (int64_t d = threadIdx.x; d < row; d += 256) {
+            if constexpr (TYPE == MX_F32) static_cast<float*>(a.out)[t * a.ldo + d] = 0.f;
+            else static_cast<uint16_t*>(a.out)[t * a.ldo + d] = 0;
+        }
 }
 
 // ---- what a call launches -------------------------------------------------------------------------------
@@ -1366,7 +1367,7 @@ mx_status launch_block(const CacheAttnArgs& a, const Plan& p, int block, uint8_t
 template <int TYPE>
 mx_status launch(const CacheAttnArgs& a, const Plan& p, int block, uint8_t* workspace, hipStream_t stream) {
     if (a.requests == 0) {
-        cache_zero_kernel<TYPE><<<(unsigned)a.tokens, 256, 0, stream>>>(a);
+        cache_zero_kernel<TYPE><<<(unsigned)(a.tokens < 65536 ? a.tokens : 65536), 256, 0, stream>>>(a);
         MX_HIP_LAUNCH_CHECK();
         return MX_OK;
     }

@@ -22,14 +22,16 @@ struct dim { unsigned x, y, z; };
 static dim grid, block;
 static size_t lds;
 static void* on;
-static int launches;
-static uint64_t threads;
+static uint64_t threads;   // of the largest launch
 void** __hipRegisterFatBinary(const void*) { static void* handle; return &handle; }
 void __hipUnregisterFatBinary(void**) {}
 void __hipRegisterFunction(void**, const void*, char*, const char*, unsigned, void*, void*, void*, void*, int*) {}
 int __hipPushCallConfiguration(dim g, dim b, size_t n, void* s) { grid = g; block = b; lds = n; on = s; return 0; }
 int __hipPopCallConfiguration(dim* g, dim* b, size_t* n, void** s) { *g = grid; *b = block; *n = lds; *s = on; return 0; }
-int hipLaunchKernel(const void*, dim g, dim b, void**, size_t, void*) { ++launches; threads = (uint64_t)g.x * b.x; return 0; }
+int hipLaunchKernel(const void*, dim g, dim b, void**, size_t, void*) {
+    if ((uint64_t)g.x * b.x > threads) threads = (uint64_t)g.x * b.x;
+    return 0;
+}
 int hipGetLastError() { return 0; }
 int hipGetDevice(int* d) { *d = 0; return 0; }
 int hipFuncSetAttribute(const void*, int, int) { return 0; }
@@ -108,3 +110,16 @@ def test_lengths_near_the_end_of_32_bits_are_refused(run):
             printf("%d ", attend(c, (2147483647 - 65536) / heads_q, 1, heads_q, 1, 64, 4));
         }""")
     assert got == ["2", "2", "2", "2", "0"] * 3 + ["2", "0"] * 3
+
+
+def test_launches_of_many_tokens_stay_below_32_bits(run):
+    """The threads of a launch are counted in 32 bits: padding tokens of a step without requests, as many as a call takes."""
+    got = run("""
+        mx_cache c{};
+        c.pages = 4; c.page = 16; c.heads = 1; c.dim = 16;
+        for (int64_t tokens : {(int64_t)1, (int64_t)1 << 24, (int64_t)1 << 25, (int64_t)2147483647 - 65536}) {
+            threads = 0;
+            printf("%d ", attend(c, tokens, 0, 1, 1, 1, 4));
+            printf("%d ", threads > 0 && threads < (1ull << 32));
+        }""")
+    assert got == ["0", "1"] * 4

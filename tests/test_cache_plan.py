@@ -33,3 +33,14 @@ def test_positions_past_32_bits_stay_at_the_last():
     assert positions.tolist() == [min(p, 2 ** 31 - 1) for p in at] and kv_len.tolist() == [2 ** 31 - 1]
     assert slots.tolist() == [e * page + p % page for e, p in zip(pages, at)]
     assert counts.tolist() == [3, 0] and table[0, have - 1:].tolist() == [7, 1, 2, 3, 7]
+
+
+@gpu
+def test_a_step_without_requests_clears_more_tokens_than_a_launch_has_workgroups():
+    cache = mx.Cache(1, 16, 1, 16, None, DEV)
+    none = ints([])
+    for tokens in (70001, (1 << 24) + 5):
+        q = torch.zeros((tokens, 16), dtype=torch.bfloat16, device=DEV)
+        out = torch.ones((tokens, 24), dtype=torch.bfloat16, device=DEV)
+        mx.cache_attention(cache, q, none.reshape(0, 1), ints([0]), none, 1, 1, out=out[:, :16])
+        assert not out[:, :16].any() and bool((out[:, 16:] == 1.0).all())
