@@ -452,7 +452,8 @@ MX_API mx_status mx_cache_append(const void* k, const void* v, int32_t type, int
  *   tokens, requests, max_new and max_len, to 0.55 GB at most: a workspace made for the largest batch serves all), 256-byte
  *   aligned, caller-owned; its first 65536 bytes must be zero when the call starts and are zero again afterwards, the rest needs
  *   no initial value.  Calls that may overlap in time need a workspace each.
- * heads_q a multiple of c.heads; requests <= 16384, width * page and tokens * heads_q below 2^31 - 2^16, else MX_ERR_UNSUPPORTED.
+ * heads_q a multiple of c.heads.  requests <= 16384, width * page and tokens * heads_q below 2^31 - 2^16, and below 2^24 the
+ * workgroups of the launch (one per 128 rows of a request and head, and one per request and head), else MX_ERR_UNSUPPORTED.
  */
 MX_API size_t mx_cache_attention_workspace_bytes(mx_cache c, int64_t tokens, int64_t requests, int32_t heads_q,
                                                  int64_t max_new, int64_t max_len);

@@ -1424,7 +1424,8 @@ extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tok
     if (!attention_supported(c, tokens, requests, heads_q) || width > kMostCounted / c.page) return MX_ERR_UNSUPPORTED;
     if (tokens == 0) return MX_OK;
     const Plan p = plan_of(c, type, tokens, requests, heads_q, max_new, max_len);
-    if ((int64_t)p.tiles * c.heads * (p.chunk_splits > 1 ? kTileRows : 1) > INT32_MAX) return MX_ERR_UNSUPPORTED;
+    // the threads of a launch, 256 a workgroup, are counted in 32 bits (joins, of few workgroups by kMostChunks, stay far below)
+    if ((int64_t)p.tiles * c.heads * p.chunk_splits + (p.decode ? requests * c.heads * p.splits : 0) >= 1 << 24) return MX_ERR_UNSUPPORTED;
     CacheAttnArgs a{};
     a.q = q; a.out = out; a.ldq = ldq; a.ldo = ldo;
     a.k = (const uint8_t*)k_data; a.v = (const uint8_t*)v_data;

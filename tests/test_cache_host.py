@@ -123,3 +123,19 @@ def test_launches_of_many_tokens_stay_below_32_bits(run):
             printf("%d ", threads > 0 && threads < (1ull << 32));
         }""")
     assert got == ["0", "1"] * 4
+
+
+def test_batches_of_more_workgroups_than_a_launch_can_have_are_refused(run):
+    """Requests times heads near 2^24 with as many row tiles again: refused, not launched in part."""
+    got = run("""
+        mx_cache c{};
+        c.pages = 4; c.page = 16; c.dim = 16;
+        for (int heads : {8, 300, 600, 1000}) {
+            c.heads = heads;
+            threads = 0;
+            printf("%d ", attend(c, 16384 * 20, 16384, heads, 20, 64, 4));
+            printf("%d ", threads < (1ull << 32));
+        }
+        c.heads = 1;
+        printf("%d ", attend(c, 2147483647 - 65536, 16384, 1, 1 << 20, 64, 4));""")
+    assert got == ["0", "1", "0", "1", "2", "1", "2", "1", "2"]
