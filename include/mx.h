@@ -423,7 +423,7 @@ MX_API mx_status mx_cache_plan(const int32_t* ctx_len, const int32_t* new_len, i
  * Writes the keys and values of `tokens` tokens into their slots: k and v of element type `type` (MX_F32, MX_BF16), token t's
  * element (head, d) at k[t*ldk + head*dim + d], ldk, ldv >= heads*dim (so k and v may be slices of one fused projection).  An
  * element becomes the nearest bfloat16 (ties to even), or the block becomes what mx_quantize makes of it (the same bits).
- * A token whose slot lies outside [0, pages*page) is skipped.  Two tokens with one slot: either of them.
+ * A token whose slot lies outside [0, pages*page) is skipped.  Slots must differ: of two tokens with one slot parts of either stay.
  * k and v aligned to their elements (16-byte aligned rows are read faster), cache arrays 16-byte aligned; *_exps may be null
  * when f.block is 0.
  */
