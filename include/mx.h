@@ -375,9 +375,9 @@ MX_API mx_status mx_linear_static_workspace(const float* x, int64_t M, int64_t K
  * A cache is a pool of pages; a page holds `page` consecutive tokens of one request for every key/value head.  Keys and
  * values are two arrays of the same geometry, data [pages][heads][page][dim]: the tokens of a page and head lie one after
  * another, so attention streams them, and a page is free for any request.  With f.block = 0 an element is a bfloat16 number
- * (the other fields of f and exps are not used; exps may be null).  Otherwise the elements are MXInt with blocks of f.block along the head dimension (the
- * axis the scores are reduced over; Section 3.2: an operator takes quantized inputs): data holds the mantissas, one byte each,
- * exps [pages][heads][page][dim/f.block] the exponent bytes.  That is the canonical form of a (pages*heads*page) x dim tensor,
+ * (the other fields of f and exps are not used; exps may be null).  Otherwise the elements are MXInt with blocks of f.block
+ * along the head dimension (the axis the scores are reduced over; Section 3.2: an operator takes quantized inputs): data holds the
+ * mantissas, one byte each, exps [pages][heads][page][dim/f.block] the exponent bytes.  That is the canonical form of a (pages*heads*page) x dim tensor,
  * so mx_dequantize reads a cache back.
  * A slot is a token's place in the pool, page_index * page + place in the page.
  * Built for page a power of two from 16 to 1024, dim a multiple of 16 up to 128, f.block 0, 16 or 32 (dividing dim),
@@ -406,8 +406,8 @@ MX_API size_t mx_cache_exps_bytes(mx_cache c);
  * and including it exceed n_free; later requests that need pages are then refused too, others are served.  A refused request's
  * row stays as it is.
  * Out: q_start[requests + 1], the running sum of new_len from 0: the place of a request's tokens in the packed token dimension
- *   (it counts refused requests' tokens too; sums, lengths and positions past 2^31 - 1 stay there); kv_len[requests] = ctx + new, 0 for a refused
- *   request; for each of `tokens` packed tokens slots[t], its place in the pool, and positions[t], its position in its request,
+ *   (it counts refused requests' tokens too; sums, lengths and positions past 2^31 - 1 stay there); kv_len[requests] = ctx + new,
+ *   0 for a refused request; for each of `tokens` packed tokens slots[t], its place in the pool, and positions[t], its position in its request,
  *   both -1 for tokens of a refused request or past the last request's, the slot also where the page index is negative or so
  *   large that its slots pass 2^31 - 1; counts[0] = pages taken from the head of free_pages, counts[1] = requests refused.
  *   positions and counts may be null.

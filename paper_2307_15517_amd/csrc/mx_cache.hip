@@ -7,11 +7,11 @@ namespace {
 // ---- mx_cache_plan --------------------------------------------------------------------------------------
 // have = ceil(ctx / page), want = ceil((ctx + new) / page), need = want - have; the pages of request b start at the sum of the
 // needs before it, its tokens at the sum of the new tokens before it.  Integers only, a few hundred kilobytes at most: bound by
-// the latency of one launch and of the scan.  Every workgroup scans all requests for itself into LDS (two sums per request),
-// so that nothing is exchanged between workgroups and one launch does it; then it takes its share of the requests (a wave
-// each: the new entries of the row) and of the tokens (a thread each: its request by binary search in LDS).  4 requests 3.5 us
-// in the kernel, 5.5 a call; 700 requests, 10 percent with prompts of up to 1024 tokens, 7.6 a call (8.6 with a request a thread
-// and three scans; 4000 requests of one token 9.8 against 17).
+// the latency of one launch and, with prompts, of the searches that a thread makes for its tokens, one after another.  Every
+// workgroup scans all requests for itself into LDS (two sums per request), so that nothing is exchanged between workgroups and one
+// launch does it; then it takes its share of the requests (a wave each: the new entries of the row) and of the tokens (a thread
+// each: its request by binary search in LDS).  4 requests 3.4 us in the kernel, 5.6 a call; 700 requests, 10 percent with prompts of
+// up to 1024 tokens, 7.4 a call: of the 1.6 us more than 4 requests take 0.1 are the scan, 0.2 the rows, 1.3 the 32740 tokens.
 struct PlanArgs {
     const int32_t* ctx;
     const int32_t* fresh;
@@ -252,7 +252,7 @@ extern "C" mx_status mx_cache_plan(const int32_t* ctx_len, const int32_t* new_le
     int64_t groups = max(ceil_div(tokens, 1024), ceil_div(requests, 16));
     groups = groups < 1 ? 1 : groups > 512 ? 512 : groups;
     // one round of the scan with a request a thread is enough (60 prompts 6.2 us, four a thread 6.6), or several with four (700
-    // requests 7.6 us, one a thread 8.5)
+    // requests 7.6 us, one a thread 8.5; 4000 requests of one token 9.8 and 17)
     if (requests <= kPlanThreads) cache_plan_kernel<1><<<(unsigned)groups, kPlanThreads, lds, (hipStream_t)stream>>>(a);
     else cache_plan_kernel<4><<<(unsigned)groups, kPlanThreads, lds, (hipStream_t)stream>>>(a);
     MX_HIP_LAUNCH_CHECK();

@@ -221,11 +221,11 @@ __device__ __forceinline__ float power2(int n) { return __builtin_ldexpf(1.f, n)
 // DT: head dimension padded to 64 or 128 (in registers only).  BLOCK: 0 bfloat16, else MXInt.
 // Pieces: K and V are bfloat16 numbers as they are (an MXInt element has 7 bits and a sign).  bfloat16 q is one piece, float q
 // three, and the probabilities are three, so that nothing but the result is rounded to fewer than 24 bits.  The matrix instructions
-// are idle most of the time here: the third piece takes 1 % (32 ragged sequences, bfloat16: 75.0 us with two, 75.9).
+// are idle most of the time here: the third piece takes 1 % (32 ragged sequences, bfloat16: 74.6 us with two, 74.9 to 75.8).
 // Bound by the reads of K and V: one sequence of 100003 keys (8 heads x 5, bfloat16) 77 us = 5.3 TB/s of the 5.6 that a bare read
-// reaches; 32 of up to 8191 (8 heads x 4, MXInt 32) 74 us = 4.3 TB/s, the vector arithmetic of the MXInt conversion taking as long as
+// reaches; 32 of up to 8191 (8 heads x 4, MXInt 32) 75 us = 4.3 TB/s, the vector arithmetic of the MXInt conversion taking as long as
 // the reads and the last requests ending alone.  Short calls by the chain of loads (lengths, table, K and V), about 0.9 us a step, and
-// the meeting of the splits: 1936 keys of 32 heads 12.4 us, one sequence of 61 keys 6.1.
+// the meeting of the splits: 1936 keys of 32 heads 12.5 us, one sequence of 61 keys 6.2.
 template <int TYPE>
 constexpr int kQueryPieces = TYPE == MX_F32 ? 3 : 1;
 
@@ -607,16 +607,18 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
 //
 // K and V are bfloat16 numbers as they are, so nothing bounds their sizes.  fp32 activations: three bfloat16 pieces of q and of the
 // probabilities, all their bits.  bfloat16 activations: q as it is and two pieces of the probabilities, what is left out being 2^-16
-// of one, 2^-8 of what the rounding of the result leaves out.  (Three: 648 us for the five prompts below.  One half-precision
-// piece: 485, with 11 bits and V scaled to half precision's range by the largest of sixteen keys, which loses small values next to
-// large ones, also to those of tokens that a row must not see.)
+// of one, 2^-8 of what the rounding of the result leaves out.  (Three: 648 us for the five prompts below, 526 with two.  One
+// half-precision piece: 485, with 11 bits and V scaled to half precision's range by the largest of sixteen keys, which loses small
+// values next to large ones, also to those of tokens that a row must not see.)
 //
-// Measured: five prompts of 1687 .. 4096 tokens (8 heads x 4 of 128, bfloat16) 526 us = 704 TFLOP/s; 300 tokens on 2000 keys (32
-// heads, fp32: three times the matrix instructions, one wave per SIMD) 68 us, of which 8 join the splits.
+// Measured: five prompts of 1687 .. 4096 tokens (8 heads x 4 of 128, bfloat16) 530 us = 698 TFLOP/s, 1047 with the second piece
+// counted; matrix cores busy 57 % and vector ALUs 56 % of the cycles.  300 tokens on 2000 keys (32 heads, fp32: three times the
+// matrix instructions, one wave per SIMD) 69 us, of which 8 join the splits; its 96 row tiles, a third of them with 44 of 128 rows,
+// are 192 workgroups on 256 compute units.
 //
 // DT is the head dimension that LDS is laid out for, 64 or 128, DC the one that is computed with: up to 96 of 128 the matrix
-// instructions leave the last quarter out (3 prompts of 1000 tokens, 8 heads x 4 of 96: 58.6 us with 128, 53.4 with 96, in half
-// precision).
+// instructions leave the last quarter out (3 prompts of 1000 tokens, 8 heads x 4 of 96: 57.8 us with 128, 50.7 with 96; MXInt
+// 68.5 and 61.5).
 constexpr int kTileRows = 128, kTileKeys = 64;
 
 // The request that tile number `tile` belongs to, and which of its tiles of rows it is; b < 0: none.  Every wave looks for itself, 64
@@ -1214,7 +1216,7 @@ __global__ __launch_bounds__(256) void cache_zero_kernel(CacheAttnArgs a) {
 // Requests with at most sixteen rows are the work of decode(), the others of chunk().  The host knows bounds only: when no request can
 // have more rows by them, cache_decode_kernel takes all (any number of rows is right there, sixteen at a time), else
 // cache_mixed_kernel has workgroups of both, each of which leaves the other's requests alone; a single request needs those of
-// the one or the other only.  (24 mixed requests: 66 us in one launch, 80 in two.)
+// the one or the other only.  (24 mixed requests, with one half-precision piece of a probability: 66 us in one launch, 80 in two.)
 constexpr int kFewRows = 16;
 
 struct Plan {
@@ -1224,7 +1226,7 @@ struct Plan {
     size_t few_bytes;
 };
 
-// Workgroups that split keys, at most: 40 and 8 times what the GPU holds of either kind, past which finer runs even nothing out.  They
+// Workgroups that split keys, at most: about 40 and 8 times what the GPU holds of either kind, past which finer runs even nothing out.  They
 // bound the parts, so that a workspace for a batch serves every smaller one, which may well be split more often.
 constexpr int64_t kMostDecode = 32768, kMostChunks = 4096;
 constexpr int kDecodeSlots = 768;                  // of bfloat16 calls; 512 of fp32 ones
@@ -1234,8 +1236,8 @@ constexpr int kLongRun = 4096;                     // keys of a run in decode(),
 // `other` tiles' time of work beside them.  A workgroup's start and end count as kStart tiles, a part's store and its join as two.
 // One request: all have as many keys, so the fewest rounds times tiles.  Several: half as many keys on average (the host knows the
 // longest only), so the longest workgroup or the work over the slots, whichever takes longer.  Measured on 168 groups of 47 tiles at
-// most beside 21 requests of one token: 1 split 97 us, 2 73, 3 (taken) 67, 4 79; 80 groups of 32 tiles of one request: 1 64 us, 3 38,
-// 6 (taken) 39, 8 48.
+// most beside 21 requests of one token: 1 split 103 us, 2 79, 3 (taken) 70, 4 82; 80 groups of 32 tiles of one request: 1 74 us, 3 42,
+// 6 (taken) 43, 8 49; 96 groups of 32 tiles, fp32: 1 109 us, 2 (taken) 70, 3 90, 4 79.
 int chunk_splits(int64_t groups, int64_t tiles, int64_t slots, int64_t other, bool one) {
     constexpr int kStart = 5;
     int best = 1;
