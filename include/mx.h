@@ -463,6 +463,88 @@ MX_API mx_status mx_cache_attention(const void* q, int32_t type, int64_t tokens,
                                     int64_t requests, int64_t max_new, int64_t max_len, float scale, void* workspace,
                                     void* out, int64_t ldo, void* stream);
 
+/*
+ * A step that checks drafted tokens (speculative decoding): every request brings a tree of new tokens instead of one, the model
+ * computes all of them at once, and of each tree the path stays that the model's own distributions accept.
+ *   mx_cache_plan       new_len = the nodes of a request's tree; node i gets the place ctx_len + i in its pages
+ *   mx_tree_plan        masks of ancestors and positions, once a step
+ *   mx_cache_append, mx_cache_tree_attention    for every layer
+ *   mx_verify           the accepted path of every request and its next token, from the logits
+ *   mx_cache_move       for every layer: the path's keys and values to the places that follow the cached tokens
+ * after which ctx_len + kept tokens are cached, and the pages behind them are the caller's to hand out again.
+ * Node 0 is the token that the step before gave, the others are drafted; parents[t] is the index of a node's parent among its request's
+ * new tokens, less than its own (-1, and any other value, for a node that stands on the cached tokens directly, as node 0 does).
+ */
+enum { MX_TREE_MAX_NODES = 1024 };             /* of a request: 16 words of 64 bits */
+enum { MX_VERIFY_MAX_VOCAB = 1 << 28 };
+
+/*
+ * Masks and positions of a step's trees, on the GPU.  masks [tokens][words]: bit j % 64 of word j / 64 of a token is set when new token j of
+ * its request is the token itself or one of its ancestors.  positions[t] = ctx_len + number of ancestors (past 2^31 - 1 stays there;
+ * negative lengths count as 0).  What lies past the first 64 * words new tokens of a request is no part of its tree, nor are
+ * tokens before the first request's and past the last one's: no bits, position -1.
+ * All arrays on the device; int32, 4-byte aligned, masks 8-byte; positions may be null.  q_start as mx_cache_plan gives it, i.e. it does
+ * not fall (else a token that is claimed twice gets what either claim gives; nothing outside the arrays is read or written).
+ * requests <= 16384, words <= MX_TREE_MAX_NODES / 64, else MX_ERR_UNSUPPORTED.
+ */
+MX_API mx_status mx_tree_plan(const int32_t* parents, const int32_t* q_start, const int32_t* ctx_len, int64_t requests, int64_t tokens,
+                              int32_t words, uint64_t* masks, int32_t* positions, void* stream);
+
+/*
+ * mx_cache_attention with a mask in place of the causal order among the new tokens: new token i of a request with n of them sees the
+ * kv_len - n cached ones and those new ones whose bits are set in its mask (of mx_tree_plan, or any other; bits at n and past it
+ * mean nothing, tokens past the words are not seen).  A token that sees no key gives zeros.  Everything else, arguments, numerics and
+ * refusals, is as there; masks is 8-byte aligned, words 1 .. MX_TREE_MAX_NODES / 64.
+ */
+MX_API size_t mx_cache_tree_attention_workspace_bytes(mx_cache c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new,
+                                                      int64_t max_len);
+MX_API mx_status mx_cache_tree_attention(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32_t heads_q, mx_cache c,
+                                         const void* k_data, const uint8_t* k_exps, const void* v_data, const uint8_t* v_exps,
+                                         const int32_t* table, int64_t width, const int32_t* q_start, const int32_t* kv_len,
+                                         const uint64_t* masks, int32_t words, int64_t requests, int64_t max_new, int64_t max_len,
+                                         float scale, void* workspace, void* out, int64_t ldo, void* stream);
+
+/*
+ * Walks down every request's tree.  At node c, with p = softmax(logits[c] / T), T = temperature[request], the children of c are tried in the
+ * order of their indices; child i with token x is accepted when
+ *     uniform[i] * Z * q(x) < r(x),    r = p and Z = 1 at first,
+ * and the walk goes on from it; else r <- max(r - Z q, 0), Z <- sum of r, for the next child.  q is softmax(draft[c] / T), the distribution
+ * that c's children were drawn from independently of each other, or, with draft = null, 1 at the child's own token and 0 elsewhere
+ * (drafts that were chosen, not drawn).  Where no child is accepted, or there is none, or the path is full, the walk ends with
+ *     next = the token with the largest r(x) / noise(x), the first of equal ones
+ * (r = p where the path is full, and where nothing is left of r): with independent exponential numbers as noise that is a draw from r / Z, and
+ * tokens of a walk are distributed as if the model had drawn them one by one.
+ * T = 0 (or less, or NaN): greedy.  p is 1 at the first of the largest logits; the first child with that token is accepted, and draft,
+ * uniform and noise play no part.
+ * logits, draft: element type `type`, the row of packed token t at t * ldl / t * ldd, `vocab` values, aligned to their elements (rows need not
+ * be).  Minus infinity is a token that cannot come; a row of nothing else accepts no child and gives next = -1.  NaN and plus infinity
+ * give unspecified tokens (no fault).
+ * ids[tokens], parents[tokens], uniform[tokens] (in [0, 1)); noise: a row of `vocab` positive floats for request b at b * ldn.
+ * path[requests][path_width]: the indices of the accepted nodes, 0 first, then -1; kept[b]: how many, 0 (and next = -1) for a request without
+ * new tokens.  The first MX_TREE_MAX_NODES new tokens of a request are its tree.  A token outside [0, vocab) is never accepted.
+ * Numerics: exponentials to about 2^-22, sums in 64 bits; the acceptance test in 64 bits.  Probabilities below 2^-126 of a row's largest
+ * may count as 0.  Same inputs, same results.
+ * workspace: mx_verify_workspace_bytes(...) bytes for the same arguments or larger ones, 256-byte aligned, caller-owned; its first 65536 bytes
+ * must be zero when the call starts and are zero again afterwards.  Calls that may overlap in time need a workspace each.
+ * requests <= 16384, vocab <= MX_VERIFY_MAX_VOCAB, else MX_ERR_UNSUPPORTED.
+ */
+MX_API size_t mx_verify_workspace_bytes(int64_t tokens, int64_t requests, int64_t vocab);
+MX_API mx_status mx_verify(const void* logits, const void* draft, int32_t type, int64_t tokens, int64_t vocab, int64_t ldl, int64_t ldd,
+                           const int32_t* ids, const int32_t* parents, const int32_t* q_start, int64_t requests,
+                           const float* temperature, const float* uniform, const float* noise, int64_t ldn, void* workspace,
+                           int32_t* path, int64_t path_width, int32_t* kept, int32_t* next, void* stream);
+
+/*
+ * Moves the keys and values of the accepted nodes together: for i < kept[b] (at most path_width) the row at position ctx_len[b] + path[b][i]
+ * of request b goes to position ctx_len[b] + i, in every head of both tensors.  A path's entries rise (path[i] >= i), as
+ * mx_verify's do; other entries give unspecified rows among those written.  Negative entries, and rows whose position or page lies
+ * outside the table row or the pool, are skipped.  Pages of the rows written must belong to one request only.
+ * Bytes are moved as they are.  Arrays and cache as in mx_cache_append; table as in mx_cache_attention.
+ */
+MX_API mx_status mx_cache_move(mx_cache c, void* k_data, uint8_t* k_exps, void* v_data, uint8_t* v_exps, const int32_t* table,
+                               int64_t width, const int32_t* ctx_len, const int32_t* path, int64_t path_width, const int32_t* kept,
+                               int64_t requests, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

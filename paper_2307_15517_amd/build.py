@@ -44,6 +44,8 @@ def translation_units() -> List[List[str]]:
                               "-DMX_GEMM_BLOCK=%d" % b])
         else:
             units.append([os.path.join(CSRC, name), os.path.join(OBJ, stem + ".o")])
+        if stem == "mx_cache_attention":              # the same kernels for trees of drafted tokens
+            units.append([os.path.join(CSRC, name), os.path.join(OBJ, stem + "_tree.o"), "-DMX_CACHE_TREE=1"])
     return units
 
 

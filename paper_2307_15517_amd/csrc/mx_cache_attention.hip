@@ -1,4 +1,5 @@
-// Attention of new tokens over the paged key/value cache, causal, grouped heads.
+// Attention of new tokens over the paged key/value cache, grouped heads: causal, or (compiled with MX_CACHE_TREE=1, a unit of its own) of
+// trees of drafted tokens, where masks say which of the new tokens a token sees.
 #include <type_traits>
 
 #include "mx_cache.h"
@@ -10,6 +11,11 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef float v4f __attribute__((ext_vector_type(4)));
+
+#ifndef MX_CACHE_TREE
+#define MX_CACHE_TREE 0
+#endif
+constexpr bool kTree = MX_CACHE_TREE;
 
 constexpr int kCounterBytes = 65536;
 
@@ -44,6 +50,8 @@ struct CacheAttnArgs {
     int32_t vec_q, vec_o;      // rows of q / out allow 16-byte (bfloat16 out: 8-byte) accesses
     float c;                   // |scale| * log2(e)
     uint32_t flip;             // sign bit of the scale: carried by q
+    const uint32_t* masks;     // kTree: [tokens][mask_words], bit j: new token j of the request is seen
+    int32_t mask_words;        // 32-bit words of a token's mask
 };
 
 // One request as a workgroup sees it, every length bounded by what the arrays hold.
@@ -58,6 +66,14 @@ __device__ __forceinline__ Request request_of(const CacheAttnArgs& a, int b) {
     r.n = (int)(t1 > t0 ? t1 - t0 : 0);
     r.len = (int)(len < 0 ? 0 : len > a.max_keys ? a.max_keys : len);
     return r;
+}
+
+// Which of 32 keys from new token `at` on (negative: cached ones) packed token `t` sees, a bit each.
+__device__ __forceinline__ uint32_t seen_from(const CacheAttnArgs& a, int64_t t, int at) {
+    const uint32_t* mask = a.masks + t * a.mask_words;
+    const int w = at >> 5;
+    const uint32_t lo = mask[min(max(w, 0), a.mask_words - 1)], hi = mask[min(max(w + 1, 0), a.mask_words - 1)];
+    return __builtin_amdgcn_alignbit(w + 1 < 0 ? ~0u : w + 1 < a.mask_words ? hi : 0u, w < 0 ? ~0u : w < a.mask_words ? lo : 0u, at & 31);
 }
 
 // Zeros for the tokens before the first request's and after the last one's.
@@ -373,11 +389,11 @@ __device__ __forceinline__ void decode(const CacheAttnArgs& a, int index, Decode
         // q: column n of the score product, elements d(step, g, i); rows past the last repeat it
         const int r = min(r0 + n, rows - 1);
         const int tok = r / a.group, head = h * a.group + (r - tok * a.group);
-        const int last = len - rq.n + tok;                                // the last key this row sees
+        const int last = kTree ? len - 1 : len - rq.n + tok;              // the last key this row sees
         v4u qf[QP][NS];
         // keys past the last one any row of this tile sees are left out
-        const int first_last = len - rq.n + r0 / a.group;                 // the last key that all its rows see
-        const int stop = min(end, len - rq.n + min(r0 + 15, rows - 1) / a.group + 1);
+        const int first_last = kTree ? len - rq.n - 1 : len - rq.n + r0 / a.group;   // the last key that all its rows see
+        const int stop = kTree ? end : min(end, len - rq.n + min(r0 + 15, rows - 1) / a.group + 1);
 
         float m = -__builtin_inff(), l = 0.f;
         v4f o[NJ];
@@ -455,11 +471,12 @@ __device__ __forceinline__ void decode(const CacheAttnArgs& a, int index, Decode
             }
             if (kb + 31 > min(first_last, stop - 1)) {
                 const int seen = min(last, stop - 1) - kb - 4 * g;
+                const uint32_t bits = kTree ? seen_from(a, rq.t0 + tok, kb - (len - rq.n)) >> (4 * g) : ~0u;
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        s[t][e] = 16 * t + e <= seen ? s[t][e] : -__builtin_inff();
+                        s[t][e] = 16 * t + e <= seen && (!kTree || (bits >> (16 * t + e) & 1)) ? s[t][e] : -__builtin_inff();
                     }
             }
             float top = -__builtin_inff();
@@ -662,6 +679,7 @@ __device__ __forceinline__ int64_t part_row_of(const CacheAttnArgs& a, int h, co
 
 // The keys of the request that some row of the tile sees, and the splits that they are given: as many as there are runs of them.
 __device__ __forceinline__ int keys_seen(const CacheAttnArgs& a, const Tile& t) {
+    if (kTree) return t.rq.len;
     return max(0, t.rq.len - t.rq.n + min(t.index * kTileRows + kTileRows - 1, t.rq.n * a.group - 1) / a.group + 1);
 }
 __device__ __forceinline__ int splits_of(const CacheAttnArgs& a, int keys) {
@@ -752,8 +770,8 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
     // this wave's rows: q is the right operand of the scores, lane (i, h2) row i, elements 16kk + 8h2 ..
     const int r = min(r0 + 32 * wave + i, rows - 1);
     const int tok = r / a.group, head = h * a.group + (r - tok * a.group);
-    const int last = min(len - rq.n + tok, stop - 1);                     // the last key of this split that the row sees
-    const int all_see = min(len - rq.n + min(r0 + 32 * wave, rows - 1) / a.group, stop - 1);   // the last one all of the wave's see
+    const int last = min(kTree ? len - 1 : len - rq.n + tok, stop - 1);   // the last key of this split that the row sees
+    const int all_see = min(kTree ? len - rq.n - 1 : len - rq.n + min(r0 + 32 * wave, rows - 1) / a.group, stop - 1);   // the last one all of the wave's see
     v4u qf[QP][NK];
     load_q<TYPE, QP, NK>(a, (int64_t)(rq.t0 + tok) * a.ldq + (int64_t)head * dim, [&](int n) { return 16 * n + 8 * h2; }, qf);
 
@@ -925,8 +943,12 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
             if (n == NO - 1) read_k(NK / 2, NK, k_next);
             if (n == 0 && kb + 31 > all_see) {
                 const int most = last - kb - 4 * h2;
+                const uint32_t bits = kTree ? seen_from(a, rq.t0 + tok, kb - (len - rq.n)) >> (4 * h2) : ~0u;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[set][e] = 8 * (e >> 2) + (e & 3) <= most ? s[set][e] : -__builtin_inff();
+                for (int e = 0; e < 16; ++e) {
+                    const int x = 8 * (e >> 2) + (e & 3);
+                    s[set][e] = x <= most && (!kTree || (bits >> x & 1)) ? s[set][e] : -__builtin_inff();
+                }
             }
             if (n == NO / 2) {
                 float t[2];
@@ -1387,28 +1409,22 @@ bool attention_supported(const mx_cache& c, int64_t tokens, int64_t requests, in
     return requests <= kCacheMaxRequests && tokens <= kMostCounted / heads_q && requests * c.heads < ((int64_t)1 << 24);
 }
 
-}  // namespace
-}  // namespace mx
 
-using namespace mx;
-
-extern "C" size_t mx_cache_attention_workspace_bytes(mx_cache c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new,
-                                                     int64_t max_len) {
+size_t workspace_checked(const mx_cache& c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new, int64_t max_len) {
     if (cache_status(c) != MX_OK || !attention_args_ok(c, tokens, requests, heads_q, max_new, max_len) ||
         !attention_supported(c, tokens, requests, heads_q))
         return 0;
     return workspace_bytes(c, tokens, requests, heads_q, max_new, max_len);
 }
 
-extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32_t heads_q, mx_cache c,
-                                        const void* k_data, const uint8_t* k_exps, const void* v_data, const uint8_t* v_exps,
-                                        const int32_t* table, int64_t width, const int32_t* q_start, const int32_t* kv_len,
-                                        int64_t requests, int64_t max_new, int64_t max_len, float scale, void* workspace, void* out,
-                                        int64_t ldo, void* stream) {
+mx_status attend(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32_t heads_q, mx_cache c, const void* k_data,
+                 const uint8_t* k_exps, const void* v_data, const uint8_t* v_exps, const int32_t* table, int64_t width,
+                 const int32_t* q_start, const int32_t* kv_len, const uint64_t* masks, int32_t words, int64_t requests, int64_t max_new,
+                 int64_t max_len, float scale, void* workspace, void* out, int64_t ldo, void* stream) {
     if (type != MX_F32 && type != MX_BF16) return MX_ERR_BAD_ARG;
     const mx_status st = cache_status(c);
     if (st == MX_ERR_BAD_ARG || !attention_args_ok(c, tokens, requests, heads_q, max_new, max_len)) return MX_ERR_BAD_ARG;
-    if (!__builtin_isfinite(scale) || width < 0) return MX_ERR_BAD_ARG;
+    if (!__builtin_isfinite(scale) || width < 0 || words < 0 || (kTree && words < 1)) return MX_ERR_BAD_ARG;
     const int64_t row = (int64_t)heads_q * c.dim;
     const int tb = type_bytes(type);
     if (tokens > 0) {
@@ -1420,10 +1436,11 @@ extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tok
             if (c.f.block != 0 && (k_exps == nullptr || v_exps == nullptr)) return MX_ERR_BAD_ARG;
             if (!aligned(k_data, 16) || !aligned(v_data, 16) || !aligned(table, 4) || !aligned(q_start, 4) || !aligned(kv_len, 4))
                 return MX_ERR_BAD_ARG;
+            if (kTree && (masks == nullptr || !aligned(masks, 8))) return MX_ERR_BAD_ARG;
         }
     }
     if (st != MX_OK) return st;
-    if (!attention_supported(c, tokens, requests, heads_q) || width > kMostCounted / c.page) return MX_ERR_UNSUPPORTED;
+    if (!attention_supported(c, tokens, requests, heads_q) || width > kMostCounted / c.page || words > MX_TREE_MAX_NODES / 64) return MX_ERR_UNSUPPORTED;
     if (tokens == 0) return MX_OK;
     const Plan p = plan_of(c, type, tokens, requests, heads_q, max_new, max_len);
     // the threads of a launch, 256 a workgroup, are counted in 32 bits (joins, of few workgroups by kMostChunks, stay far below)
@@ -1443,6 +1460,43 @@ extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tok
     a.vec_o = aligned(out, 4 * tb) && ldo % 4 == 0;
     a.c = __builtin_fmaxf(__builtin_fabsf(scale) * 1.4426950408889634f, 0x1p-126f);   // never 0: minus infinity stays a mask
     a.flip = scale < 0.f ? 0x80000000u : 0u;
+    a.masks = (const uint32_t*)masks;
+    a.mask_words = 2 * words;
     uint8_t* ws = (uint8_t*)workspace;
     return type == MX_F32 ? launch<MX_F32>(a, p, c.f.block, ws, (hipStream_t)stream) : launch<MX_BF16>(a, p, c.f.block, ws, (hipStream_t)stream);
 }
+
+}  // namespace
+}  // namespace mx
+
+using namespace mx;
+
+#if MX_CACHE_TREE
+extern "C" size_t mx_cache_tree_attention_workspace_bytes(mx_cache c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new,
+                                                          int64_t max_len) {
+    return workspace_checked(c, tokens, requests, heads_q, max_new, max_len);
+}
+
+extern "C" mx_status mx_cache_tree_attention(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32_t heads_q, mx_cache c,
+                                             const void* k_data, const uint8_t* k_exps, const void* v_data, const uint8_t* v_exps,
+                                             const int32_t* table, int64_t width, const int32_t* q_start, const int32_t* kv_len,
+                                             const uint64_t* masks, int32_t words, int64_t requests, int64_t max_new, int64_t max_len,
+                                             float scale, void* workspace, void* out, int64_t ldo, void* stream) {
+    return attend(q, type, tokens, ldq, heads_q, c, k_data, k_exps, v_data, v_exps, table, width, q_start, kv_len, masks, words, requests,
+                  max_new, max_len, scale, workspace, out, ldo, stream);
+}
+#else
+extern "C" size_t mx_cache_attention_workspace_bytes(mx_cache c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new,
+                                                     int64_t max_len) {
+    return workspace_checked(c, tokens, requests, heads_q, max_new, max_len);
+}
+
+extern "C" mx_status mx_cache_attention(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32_t heads_q, mx_cache c,
+                                        const void* k_data, const uint8_t* k_exps, const void* v_data, const uint8_t* v_exps,
+                                        const int32_t* table, int64_t width, const int32_t* q_start, const int32_t* kv_len,
+                                        int64_t requests, int64_t max_new, int64_t max_len, float scale, void* workspace, void* out,
+                                        int64_t ldo, void* stream) {
+    return attend(q, type, tokens, ldq, heads_q, c, k_data, k_exps, v_data, v_exps, table, width, q_start, kv_len, nullptr, 0, requests,
+                  max_new, max_len, scale, workspace, out, ldo, stream);
+}
+#endif

@@ -27,7 +27,8 @@ EXPORTS = ("mx_version", "mx_status_string", "mx_mant_bytes", "mx_exps_bytes", "
            "mx_gemm_q", "mx_attention", "mx_linear", "mx_linear_workspace_bytes", "mx_linear_static_workspace",
            "mx_linear_static_workspace_max", "mx_quantize_minifloat",
            "mx_dequantize_minifloat", "mx_cache_data_bytes", "mx_cache_exps_bytes", "mx_cache_plan", "mx_cache_append",
-           "mx_cache_attention_workspace_bytes", "mx_cache_attention")
+           "mx_cache_attention_workspace_bytes", "mx_cache_attention", "mx_tree_plan", "mx_cache_tree_attention_workspace_bytes",
+           "mx_cache_tree_attention", "mx_verify_workspace_bytes", "mx_verify", "mx_cache_move")
 
 
 class mx_format(ctypes.Structure):
@@ -113,7 +114,16 @@ def load() -> ctypes.CDLL:
     lib.mx_cache_attention_workspace_bytes.restype = sz
     lib.mx_cache_attention.argtypes = [vp, i32, i64, i64, i32, mx_cache, vp, vp, vp, vp, vp, i64, vp, vp, i64, i64, i64,
                                        ctypes.c_float, vp, vp, i64, vp]
-    for name in ("mx_cache_plan", "mx_cache_append", "mx_cache_attention"):
+    lib.mx_tree_plan.argtypes = [vp, vp, vp, i64, i64, i32, vp, vp, vp]
+    lib.mx_cache_tree_attention_workspace_bytes.argtypes = [mx_cache, i64, i64, i32, i64, i64]
+    lib.mx_cache_tree_attention_workspace_bytes.restype = sz
+    lib.mx_cache_tree_attention.argtypes = [vp, i32, i64, i64, i32, mx_cache, vp, vp, vp, vp, vp, i64, vp, vp, vp, i32, i64, i64, i64,
+                                            ctypes.c_float, vp, vp, i64, vp]
+    lib.mx_verify_workspace_bytes.argtypes, lib.mx_verify_workspace_bytes.restype = [i64, i64, i64], sz
+    lib.mx_verify.argtypes = [vp, vp, i32, i64, i64, i64, i64, vp, vp, vp, i64, vp, vp, vp, i64, vp, vp, i64, vp, vp, vp]
+    lib.mx_cache_move.argtypes = [mx_cache, vp, vp, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp]
+    for name in ("mx_cache_plan", "mx_cache_append", "mx_cache_attention", "mx_tree_plan", "mx_cache_tree_attention", "mx_verify",
+                 "mx_cache_move"):
         getattr(lib, name).restype = i32
     for name in ("mx_quantize", "mx_dequantize", "mx_cast", "mx_pack", "mx_quantize_pack", "mx_quantize_pack_axis0",
                  "mx_unpack", "mx_gemm",
@@ -353,6 +363,75 @@ def mx_cache_attention(q, type, tokens, ldq, heads_q, c, k_data, k_exps, v_data,
     return s
 
 
+# A step that checks drafted tokens: the same way.
+def mx_tree_plan(parents, q_start, ctx_len, requests, tokens, words, masks, positions, stream=None, check: bool = True) -> int:
+    h = _stream(stream)
+    try:
+        s = _lib.mx_tree_plan(parents.data_ptr(), q_start.data_ptr(), ctx_len.data_ptr(), requests, tokens, words, masks.data_ptr(),
+                              positions.data_ptr(), h)
+    except AttributeError:
+        s = load().mx_tree_plan(_p(parents), _p(q_start), _p(ctx_len), requests, tokens, words, _p(masks), _p(positions), h)
+    if check:
+        _raise(s, "mx_tree_plan")
+    return s
+
+
+def mx_cache_tree_attention_workspace_bytes(c: mx_cache, tokens: int, requests: int, heads_q: int, max_new: int,
+                                            max_len: int) -> int:
+    return int(load().mx_cache_tree_attention_workspace_bytes(c, tokens, requests, heads_q, max_new, max_len))
+
+
+def mx_cache_tree_attention(q, type, tokens, ldq, heads_q, c, k_data, k_exps, v_data, v_exps, table, width, q_start, kv_len, masks,
+                            words, requests, max_new, max_len, scale, workspace, out, ldo, stream=None, check: bool = True) -> int:
+    h = _stream(stream)
+    try:
+        s = _lib.mx_cache_tree_attention(q.data_ptr(), type, tokens, ldq, heads_q, c, k_data.data_ptr(), k_exps.data_ptr(),
+                                         v_data.data_ptr(), v_exps.data_ptr(), table.data_ptr(), width, q_start.data_ptr(),
+                                         kv_len.data_ptr(), masks.data_ptr(), words, requests, max_new, max_len, scale,
+                                         workspace.data_ptr(), out.data_ptr(), ldo, h)
+    except AttributeError:
+        s = load().mx_cache_tree_attention(_p(q), type, tokens, ldq, heads_q, c, _p(k_data), _p(k_exps), _p(v_data), _p(v_exps),
+                                           _p(table), width, _p(q_start), _p(kv_len), _p(masks), words, requests, max_new, max_len,
+                                           scale, _p(workspace), _p(out), ldo, h)
+    if check:
+        _raise(s, "mx_cache_tree_attention")
+    return s
+
+
+def mx_verify_workspace_bytes(tokens: int, requests: int, vocab: int) -> int:
+    return int(load().mx_verify_workspace_bytes(tokens, requests, vocab))
+
+
+def mx_verify(logits, draft, type, tokens, vocab, ldl, ldd, ids, parents, q_start, requests, temperature, uniform, noise, ldn,
+              workspace, path, path_width, kept, next, stream=None, check: bool = True) -> int:
+    h = _stream(stream)
+    try:
+        s = _lib.mx_verify(logits.data_ptr(), None if draft is None else draft.data_ptr(), type, tokens, vocab, ldl, ldd, ids.data_ptr(),
+                           parents.data_ptr(), q_start.data_ptr(), requests, temperature.data_ptr(), uniform.data_ptr(),
+                           noise.data_ptr(), ldn, workspace.data_ptr(), path.data_ptr(), path_width, kept.data_ptr(),
+                           next.data_ptr(), h)
+    except AttributeError:
+        s = load().mx_verify(_p(logits), _p(draft), type, tokens, vocab, ldl, ldd, _p(ids), _p(parents), _p(q_start), requests,
+                             _p(temperature), _p(uniform), _p(noise), ldn, _p(workspace), _p(path), path_width, _p(kept), _p(next), h)
+    if check:
+        _raise(s, "mx_verify")
+    return s
+
+
+def mx_cache_move(c, k_data, k_exps, v_data, v_exps, table, width, ctx_len, path, path_width, kept, requests, stream=None,
+                  check: bool = True) -> int:
+    h = _stream(stream)
+    try:
+        s = _lib.mx_cache_move(c, k_data.data_ptr(), k_exps.data_ptr(), v_data.data_ptr(), v_exps.data_ptr(), table.data_ptr(), width,
+                               ctx_len.data_ptr(), path.data_ptr(), path_width, kept.data_ptr(), requests, h)
+    except AttributeError:
+        s = load().mx_cache_move(c, _p(k_data), _p(k_exps), _p(v_data), _p(v_exps), _p(table), width, _p(ctx_len), _p(path),
+                                 path_width, _p(kept), requests, h)
+    if check:
+        _raise(s, "mx_cache_move")
+    return s
+
+
 def bound(name: str, *args, stream=None):
     """Marshal the arguments of entry point ``name`` once and return a zero-argument callable that
     issues exactly that call again (status checked).  For loops that launch the same call many times:
@@ -540,3 +619,94 @@ def cache_attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, q_start:
                        cache.v_exps, table, table.shape[1], q_start, kv_len, requests, max_new, max_len,
                        dim ** -0.5 if scale is None else scale, workspace, out, _row_stride(out))
     return out
+
+
+def _int32(*tensors: torch.Tensor) -> None:
+    for t in tensors:
+        assert t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()
+
+
+def tree_plan(parents: torch.Tensor, q_start: torch.Tensor, ctx_len: torch.Tensor, words: int = 1) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(masks [tokens, words] int64, positions [tokens]) of a step's trees; parents: of every packed token, -1 for node 0."""
+    _int32(parents, q_start, ctx_len)
+    tokens, requests = parents.numel(), ctx_len.numel()
+    assert q_start.numel() == requests + 1
+    masks = torch.empty((tokens, words), dtype=torch.int64, device=parents.device)
+    positions = torch.empty(tokens, dtype=torch.int32, device=parents.device)
+    mx_tree_plan(parents, q_start, ctx_len, requests, tokens, words, masks, positions)
+    return masks, positions
+
+
+def cache_tree_workspace(c: mx_cache, tokens: int, requests: int, heads_q: int, max_new: int, max_len: int, device) -> torch.Tensor:
+    """A workspace for mx_cache_tree_attention with these or smaller numbers; its counters, the first 65536 bytes, are zero."""
+    space = torch.empty(max(1, mx_cache_tree_attention_workspace_bytes(c, tokens, requests, heads_q, max_new, max_len)),
+                        dtype=torch.uint8, device=device)
+    space[:65536].zero_()
+    return space
+
+
+def cache_tree_attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                         masks: torch.Tensor, max_new: int, max_len: int, scale: Optional[float] = None,
+                         workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """cache_attention with masks [tokens, words] (of tree_plan) in place of the causal order; workspace: of cache_tree_workspace."""
+    dim, requests = cache.c.dim, table.shape[0]
+    assert table.dim() == 2 and q_start.numel() == requests + 1 and kv_len.numel() == requests
+    _int32(table, q_start, kv_len)
+    assert masks.dtype == torch.int64 and masks.is_cuda and masks.is_contiguous() and masks.dim() == 2 and masks.shape[0] == q.shape[0]
+    heads_q = q.shape[1] // dim
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape and out.dtype == q.dtype and out.is_cuda and out.stride(-1) == 1 and q.shape[1] == heads_q * dim
+    if workspace is None:
+        workspace = cache_tree_workspace(cache.c, q.shape[0], requests, heads_q, max_new, max_len, q.device)
+    else:
+        need = mx_cache_tree_attention_workspace_bytes(cache.c, q.shape[0], requests, heads_q, max_new, max_len)
+        if workspace.device != q.device or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
+            raise MxError(MX_ERR_BAD_ARG, "cache_tree_attention: a workspace of %d bytes on the GPU of q is wanted" % need)
+    mx_cache_tree_attention(q, _activation_type(q), q.shape[0], _row_stride(q), heads_q, cache.c, cache.k, cache.k_exps, cache.v,
+                            cache.v_exps, table, table.shape[1], q_start, kv_len, masks, masks.shape[1], requests, max_new, max_len,
+                            dim ** -0.5 if scale is None else scale, workspace, out, _row_stride(out))
+    return out
+
+
+def verify_workspace(tokens: int, requests: int, vocab: int, device) -> torch.Tensor:
+    """A workspace for mx_verify with these or smaller numbers; its first 65536 bytes are zero."""
+    space = torch.empty(max(1, mx_verify_workspace_bytes(tokens, requests, vocab)), dtype=torch.uint8, device=device)
+    space[:65536].zero_()
+    return space
+
+
+def verify(logits: torch.Tensor, ids: torch.Tensor, parents: torch.Tensor, q_start: torch.Tensor, temperature: torch.Tensor,
+           uniform: torch.Tensor, noise: torch.Tensor, path_width: int, draft: Optional[torch.Tensor] = None,
+           workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, ...]:
+    """(path [requests, path_width], kept [requests], next [requests]) of a step's trees from the logits [tokens, vocab] (float32 or
+    bfloat16); draft: the logits that the nodes' children were drawn from; temperature [requests], uniform [tokens] in [0, 1) and
+    noise [requests, vocab], independent exponential numbers above 0, are float32."""
+    tokens, vocab = logits.shape
+    requests = temperature.numel()
+    _int32(ids, parents, q_start)
+    assert ids.numel() == parents.numel() == uniform.numel() == tokens and q_start.numel() == requests + 1
+    for t in (temperature, uniform, noise):
+        assert t.dtype == torch.float32 and t.is_cuda and t.stride(-1) == 1
+    assert temperature.is_contiguous() and uniform.is_contiguous() and noise.shape == (requests, vocab) and path_width >= 1
+    assert draft is None or (draft.shape == logits.shape and draft.dtype == logits.dtype and draft.is_cuda and draft.stride(-1) == 1)
+    if workspace is None:
+        workspace = verify_workspace(tokens, requests, vocab, logits.device)
+    else:
+        need = mx_verify_workspace_bytes(tokens, requests, vocab)
+        if workspace.device != logits.device or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need:
+            raise MxError(MX_ERR_BAD_ARG, "verify: a workspace of %d bytes on the GPU of the logits is wanted" % need)
+    path = torch.empty((requests, path_width), dtype=torch.int32, device=logits.device)
+    kept, following = (torch.empty(requests, dtype=torch.int32, device=logits.device) for _ in range(2))
+    mx_verify(logits, draft, _activation_type(logits), tokens, vocab, _row_stride(logits), vocab if draft is None else _row_stride(draft),
+              ids, parents, q_start, requests, temperature, uniform, noise, _row_stride(noise), workspace, path, path_width, kept,
+              following)
+    return path, kept, following
+
+
+def cache_move(cache: Cache, table: torch.Tensor, ctx_len: torch.Tensor, path: torch.Tensor, kept: torch.Tensor) -> None:
+    """The rows of the accepted nodes (verify's path and kept) to the places that follow the ctx_len cached tokens."""
+    _int32(table, ctx_len, path, kept)
+    assert table.dim() == path.dim() == 2 and table.shape[0] == path.shape[0] == ctx_len.numel() == kept.numel()
+    mx_cache_move(cache.c, cache.k, cache.k_exps, cache.v, cache.v_exps, table, table.shape[1], ctx_len, path, path.shape[1], kept,
+                  path.shape[0])

@@ -1,0 +1,416 @@
+"""Trees of drafted tokens over the paged cache: masks and positions, attention, moved rows, against plain implementations in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2307_15517_amd import mx
+from test_cache import DEV, FORMATS, Step, ints
+
+gpu = pytest.mark.gpu
+
+
+# ---- refusals (no GPU: every call returns before a launch) ------------------------------------------------
+def test_plan_refusals():
+    def call(parents=256, qs=256, ctx=256, B=2, tokens=8, words=1, masks=256, pos=256):
+        return mx.mx_tree_plan(parents, qs, ctx, B, tokens, words, masks, pos, stream=0, check=False)
+    for kw in (dict(parents=0), dict(qs=0), dict(ctx=0), dict(masks=0), dict(B=-1), dict(tokens=-1), dict(words=0), dict(parents=258),
+               dict(qs=257), dict(ctx=259), dict(masks=260), dict(pos=258)):
+        assert call(**kw) == mx.MX_ERR_BAD_ARG, kw
+    for kw in (dict(B=16385), dict(tokens=1 << 31), dict(words=17)):
+        assert call(**kw) == mx.MX_ERR_UNSUPPORTED, kw
+    assert call(tokens=0) == mx.MX_OK and call(tokens=0, parents=0, masks=0, qs=0) == mx.MX_OK
+
+
+def test_attention_refusals():
+    f = mx.fmt(32, 8)
+
+    def call(q=256, type=mx.MX_F32, tokens=4, ldq=256, hq=4, c=mx.cache_format(4, 16, 2, 64, f), kd=256, ke=256, vd=256, ve=256, table=256,
+             width=4, qs=256, kv=256, masks=256, words=1, B=2, mn=1, ml=64, scale=0.125, ws=256, out=512, ldo=256):
+        return mx.mx_cache_tree_attention(q, type, tokens, ldq, hq, c, kd, ke, vd, ve, table, width, qs, kv, masks, words, B, mn, ml, scale,
+                                          ws, out, ldo, stream=0, check=False)
+    for kw in (dict(masks=0), dict(masks=260), dict(words=0), dict(words=-1), dict(q=0), dict(out=0), dict(ws=0), dict(ws=300), dict(kd=0),
+               dict(ke=0), dict(table=0), dict(qs=0), dict(kv=0), dict(type=7), dict(tokens=-1), dict(ldq=255), dict(ldo=255), dict(hq=3),
+               dict(width=-1), dict(B=-1), dict(mn=0), dict(ml=0), dict(scale=float("nan")), dict(q=258), dict(out=513),
+               dict(c=mx.cache_format(4, 16, 2, 48, f))):
+        assert call(**kw) == mx.MX_ERR_BAD_ARG, kw
+    for kw in (dict(words=17), dict(B=16385), dict(width=1 << 27), dict(c=mx.cache_format(4, 48, 2, 64, f)), dict(tokens=1 << 30)):
+        assert call(**kw) == mx.MX_ERR_UNSUPPORTED, kw
+    assert call(tokens=0) == mx.MX_OK
+
+
+def test_move_refusals():
+    f = mx.fmt(32, 8)
+
+    def call(c=mx.cache_format(4, 16, 2, 64, f), kd=256, ke=256, vd=256, ve=256, table=256, width=4, ctx=256, path=256, pw=3, kept=256, B=2):
+        return mx.mx_cache_move(c, kd, ke, vd, ve, table, width, ctx, path, pw, kept, B, stream=0, check=False)
+    for kw in (dict(kd=0), dict(ke=0), dict(vd=0), dict(ve=0), dict(table=0), dict(ctx=0), dict(path=0), dict(kept=0), dict(width=-1),
+               dict(pw=-1), dict(B=-1), dict(kd=264), dict(vd=260), dict(table=258), dict(ctx=257), dict(path=258), dict(kept=259),
+               dict(c=mx.cache_format(0, 16, 2, 64, f)), dict(c=mx.cache_format(4, 16, 2, 48, f))):
+        assert call(**kw) == mx.MX_ERR_BAD_ARG, kw
+    for kw in (dict(c=mx.cache_format(4, 24, 2, 64, f)), dict(c=mx.cache_format(4, 16, 2, 64, mx.fmt(32, 4))), dict(B=16385),
+               dict(width=1 << 31), dict(pw=1 << 31)):
+        assert call(**kw) == mx.MX_ERR_UNSUPPORTED, kw
+    assert call(B=0) == call(pw=0) == call(width=0, table=0) == mx.MX_OK
+
+
+# ---- masks and positions ----------------------------------------------------------------------------------
+def random_parents(r, n, reach=None):
+    """A tree of n nodes, node 0 at its root."""
+    return [-1] + [int(r.integers(max(0, i - (reach or i)), i)) for i in range(1, n)]
+
+
+def plan_oracle(parents, starts, ctx, tokens, words):
+    masks, positions = np.zeros((tokens, words), np.uint64), np.full(tokens, -1, np.int64)
+    for b in range(len(ctx)):
+        lo, hi = min(max(starts[b], 0), tokens), min(starts[b + 1], tokens)
+        for i in range(min(max(hi - lo, 0), 64 * words)):
+            node, depth = i, -1
+            while node >= 0:
+                masks[lo + i, node // 64] |= np.uint64(1) << np.uint64(node % 64)
+                depth += 1
+                p = parents[lo + node]
+                node = p if 0 <= p < node else -1
+            positions[lo + i] = min(max(ctx[b], 0) + depth, 2 ** 31 - 1)
+    return masks.view(np.int64), positions
+
+
+@gpu
+@pytest.mark.parametrize("sizes,words,lead,pad", [
+    ([1], 1, 0, 0), ([5], 1, 0, 0), ([5, 0, 64, 1, 63, 2, 9], 1, 2, 3), ([70], 1, 0, 0), ([65, 64, 130, 1, 0], 2, 1, 0), ([200, 7, 129, 300], 5, 0, 70),
+    ([1024, 3, 1000], 16, 0, 0), ([1100, 2], 16, 0, 5), ([33] * 700, 1, 0, 1), ([1] * 5000, 1, 0, 0)])
+@pytest.mark.parametrize("reach", [1, 3, None])
+def test_plan(sizes, words, lead, pad, reach):
+    r = np.random.default_rng(len(sizes) + sum(sizes))
+    parents = [-1] * lead + [p for n in sizes for p in random_parents(r, n, reach)[:n]] + [3] * pad
+    starts = lead + np.concatenate([[0], np.cumsum(sizes)])
+    ctx = r.integers(0, 3000, len(sizes)).tolist()
+    masks, positions = mx.tree_plan(ints(parents), ints(starts.tolist()), ints(ctx), words)
+    want = plan_oracle(parents, starts.tolist(), ctx, len(parents), words)
+    assert np.array_equal(masks.cpu().numpy(), want[0]) and np.array_equal(positions.cpu().numpy(), want[1])
+
+
+@gpu
+@pytest.mark.parametrize("words", [1, 2, 16])
+def test_plan_of_anything(words):
+    """Parents that are none (their own number, later ones, far outside), starts outside the tokens or falling, lengths at the ends."""
+    r = np.random.default_rng(words)
+    tokens, big = 300, 2 ** 31 - 1
+    parents = r.integers(-5, 200, tokens)
+    parents[::7], parents[3::11] = big, -big - 1
+    for starts in ([-5, 40, 90, 300], [10, 5, 130, 400], [0, 0, big, big], [-big, 299, 300, 300], [300, 300, 300, 300]):
+        ctx = [-3, big - 1, 17]
+        masks = torch.full((tokens, words), 99, dtype=torch.int64, device=DEV)
+        positions = torch.full((tokens,), 99, dtype=torch.int32, device=DEV)
+        mx.mx_tree_plan(ints(parents.tolist()), ints(starts), ints(ctx), 3, tokens, words, masks, positions)
+        got = masks.cpu().numpy(), positions.cpu().numpy()
+        want = plan_oracle(parents.tolist(), starts, ctx, tokens, words)
+        # of a token that two requests claim, or a request and the padding before the first start or after the last, either's will do
+        owners = np.zeros(tokens, int)
+        lead = min(max(starts[0], 0), tokens)
+        owners[:lead] += 1
+        owners[max(lead, min(starts[-1], tokens)):] += 1
+        for lo, hi in zip(starts, starts[1:]):
+            owners[min(max(lo, 0), tokens):max(min(hi, tokens), 0)] += 1
+        assert np.array_equal(got[0][owners < 2], want[0][owners < 2]) and np.array_equal(got[1][owners < 2], want[1][owners < 2])
+    # no requests: nothing but padding; positions are optional
+    mx.mx_tree_plan(None, None, None, 0, tokens, words, masks, positions)
+    assert not masks.any() and bool((positions == -1).all())
+    mx.mx_tree_plan(ints(parents.tolist()), ints([0, 300]), ints([4]), 1, tokens, words, masks, None)
+    assert np.array_equal(masks.cpu().numpy(), plan_oracle(parents.tolist(), [0, 300], [4], tokens, words)[0])
+
+
+# ---- attention --------------------------------------------------------------------------------------------
+class TreeStep(Step):
+    """A step whose requests bring trees: lens = [(nodes, cached with them), ...]; masks as given, or of random trees."""
+
+    def __init__(self, lens, *args, words=None, masks=None, reach=None, **kw):
+        super().__init__(lens, *args, **kw)
+        r = np.random.default_rng(kw["seed"] + 77)
+        self.words = words or max(1, -(-max([n for n, _ in lens] + [1]) // 64))
+        lead = self.starts[0]
+        if masks is None:
+            parents = [-1] * lead + [p for n, _ in lens for p in random_parents(r, n, reach)[:n]]
+            parents += [-1] * (self.tokens - len(parents))
+            self.parents = parents
+            masks = plan_oracle(parents, self.starts, [0] * len(lens), self.tokens, self.words)[0]
+        elif masks == "random":
+            masks = r.integers(-2 ** 63, 2 ** 63, (self.tokens, self.words))
+            masks[::3] &= r.integers(-2 ** 63, 2 ** 63, (self.tokens, self.words))[::3]
+            masks[1::5] = 0
+        self.masks = torch.from_numpy(np.ascontiguousarray(masks).reshape(self.tokens, self.words)).to(DEV)
+
+    def run(self, scale=None, max_new=None, max_len=None, opad=0, workspace=None):
+        row = self.heads * self.group * self.dim
+        out = torch.full((max(1, self.tokens), row + opad), 77.0, device=DEV, dtype=self.dtype)
+        mx.cache_tree_attention(self.cache, self.q, self.table, self.q_start, self.kv_len, self.masks, max_new or self.max_new,
+                                max_len or self.max_len, scale, workspace, out[:self.tokens, :row])
+        torch.cuda.synchronize()
+        assert bool((out[:, row:] == 77.0).all())
+        return out[:self.tokens, :row]
+
+    def seen(self, b):
+        """[new tokens, cached tokens]: who sees whom."""
+        n, m = self.lens[b]
+        bits = self.masks[self.starts[b]:self.starts[b] + n].cpu().numpy().view(np.uint64)
+        j = np.arange(m) - (m - n)
+        word = np.where(j[None, :] < 64 * self.words, bits[:, np.clip(j // 64, 0, self.words - 1)], np.uint64(0))
+        return (j[None, :] < 0) | ((word >> (j[None, :] % 64).astype(np.uint64)) & np.uint64(1)).astype(bool)
+
+    def reference(self, scale=None):
+        """(output, how far the kernel may be from it): as the base class's, whose comment counts the roundings."""
+        scale = self.dim ** -0.5 if scale is None else scale
+        K, V = self.values()
+        q = self.q.double().cpu().numpy().reshape(self.tokens, self.heads * self.group, self.dim)
+        out, tol = np.zeros(q.shape), np.zeros(q.shape)
+        at = 0
+        for b, (n, m) in enumerate(self.lens):
+            k, v = K[at:at + m], V[at:at + m]
+            at += m
+            if m == 0 or n == 0:
+                continue
+            seen = self.seen(b)
+            rows = slice(self.starts[b], self.starts[b] + n)
+            for a in range(self.heads * self.group):
+                x, h = q[rows, a], a // self.group
+                s = np.where(seen, scale * (x @ k[:, h].T), -np.inf)
+                top = s.max(-1, keepdims=True)
+                p = np.where(seen, np.exp(s - np.where(np.isfinite(top), top, 0.0)), 0.0)
+                total = p.sum(-1, keepdims=True)
+                p = np.divide(p, total, out=np.zeros_like(p), where=total > 0)
+                o = p @ v[:, h]
+                mag = np.where(seen, abs(scale) * (np.abs(x) @ np.abs(k[:, h]).T), 0.0).max(-1, keepdims=True)
+                eps = 2 * 2.0 ** -24 * ((self.dim + 8) * mag + 4 * mag) + 2 * (m + 64) * 2.0 ** -24
+                size = p @ np.abs(v[:, h])
+                t = eps * size + 2.0 ** -126 * (1.0 + np.abs(v[:, h]).sum(0))
+                if self.dtype == torch.bfloat16:
+                    t = t + 2.0 ** -9 * size + 2.0 ** -8 * np.abs(o)
+                out[rows, a], tol[rows, a] = o, t
+        return out.reshape(self.tokens, -1), tol.reshape(self.tokens, -1)
+
+
+CHAIN = [(5, 178)]
+SMALL = [(1, 1), (2, 2), (7, 40), (16, 16), (3, 129), (1, 700), (8, 33)]
+MIDDLE = [(17, 17), (25, 300), (33, 64), (40, 1000), (64, 64), (1, 90), (12, 31)]
+LARGE = [(64, 700), (61, 61), (200, 333), (3, 40), (130, 130)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("kind", ["bf16", "mx16", "mx32"])
+@pytest.mark.parametrize("lens,heads,group,dim,page", [
+    (CHAIN, 12, 1, 64, 16), (CHAIN, 2, 5, 128, 64), (SMALL, 2, 2, 128, 16), (SMALL, 3, 1, 96, 32), (MIDDLE, 2, 1, 128, 16), (MIDDLE, 2, 2, 64, 128),
+    (MIDDLE, 1, 4, 128, 32), (LARGE, 1, 8, 128, 64), (LARGE, 2, 3, 96, 16), (LARGE, 1, 1, 32, 1024)])
+def test_attention(dtype, kind, lens, heads, group, dim, page):
+    TreeStep(lens, heads, group, dim, page, FORMATS[kind], dtype, seed=dim + len(lens)).check()
+
+
+@gpu
+@pytest.mark.parametrize("dim", [16, 48, 80, 112])
+@pytest.mark.parametrize("kind", ["bf16", "mx16"])
+def test_attention_head_dimensions(dim, kind):
+    for group in (1, 3):
+        TreeStep(SMALL + MIDDLE, 2, group, dim, 16, FORMATS[kind], torch.float32, seed=dim).check()
+        TreeStep(SMALL + MIDDLE, 1, group, dim, 32, FORMATS[kind], torch.bfloat16, seed=dim).check()
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "mx32"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lens", [[(9, 9001)], [(5, 5000), (2, 17), (1, 300), (4, 4999)], [(61, 6000)], [(30, 3000), (8, 5003), (64, 64)],
+                                  [(150, 4000), (1, 3000)]])
+def test_attention_split_over_a_long_axis(dtype, kind, lens):
+    for heads, group, dim in ((1, 4, 128), (2, 1, 64), (1, 8, 128)):
+        TreeStep(lens, heads, group, dim, 16, FORMATS[kind], dtype, seed=4).check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("group", [1, 2, 5])
+def test_attention_any_masks(dtype, group):
+    """Bits that are no tree's: later tokens, past the request's own, none at all; words that do not reach the last tokens."""
+    for lens in (SMALL, MIDDLE, LARGE, [(3, 3), (40, 40)], [(64, 2000)]):
+        TreeStep(lens, 2, group, 64, 16, FORMATS["mx32"], dtype, seed=20, masks="random").check()
+        TreeStep(lens, 1, group, 128, 16, FORMATS["bf16"], dtype, seed=21, masks="random", words=1).check()
+        TreeStep(lens, 1, group, 64, 16, FORMATS["bf16"], dtype, seed=22, masks="random", words=16).check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("group", [1, 3])
+def test_attention_rows_without_keys_and_padding(dtype, group):
+    """Idle requests, requests without cached tokens (refused ones), more new tokens than cached ones, padding at both ends."""
+    for lens in ([(0, 40), (3, 0), (5, 2), (1, 50), (0, 0)], [(2, 0)], [(40, 39), (70, 100), (64, 1)], [(0, 17)], [(30, 0), (30, 12)], []):
+        s = TreeStep(lens, 2, group, 64, 16, FORMATS["mx32"], dtype, seed=6, pad=5, lead=3)
+        got = s.check()
+        assert not got[:3].any() and not got[s.tokens - 5:].any()
+
+
+@gpu
+@pytest.mark.parametrize("lead,qpad,opad", [(0, 0, 1), (1, 3, 5), (0, 64, 8)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attention_strides(dtype, lead, qpad, opad):
+    for lens in (SMALL, MIDDLE, LARGE):
+        TreeStep(lens, 2, 2, 64, 16, FORMATS["mx16"], dtype, seed=8, qpad=qpad, lead=lead).check(opad=opad)
+
+
+@gpu
+@pytest.mark.parametrize("lens", [SMALL, MIDDLE, LARGE, [(6, 4000)], [(30, 4000)]])
+def test_attention_bounds_on_lengths_only_shape_the_launch(lens):
+    for dtype in (torch.float32, torch.bfloat16):
+        s = TreeStep(lens, 2, 2, 128, 16, FORMATS["mx32"], dtype, seed=9)
+        for mn, ml in ((1, 1), (10000, 100000), (1, 100000), (500, 1), (20, 3000), (2 ** 31 - 1, 2 ** 40), (2 ** 63 - 1, 2 ** 63 - 1)):
+            s.check(max_new=mn, max_len=ml)
+
+
+@gpu
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 1.0, 3.0])
+def test_attention_scales_and_spread(scale):
+    for lens in (SMALL, MIDDLE, LARGE):
+        TreeStep(lens, 2, 2, 64, 16, FORMATS["mx32"], torch.float32, seed=10).check(scale)
+        TreeStep(lens, 2, 2, 64, 16, FORMATS["bf16"], torch.bfloat16, seed=10).check(scale)
+    for spread in (1e-6, 30.0):
+        TreeStep(SMALL + MIDDLE, 2, 2, 64, 16, FORMATS["mx32"], torch.float32, seed=12, spread=spread).check()
+        TreeStep(SMALL + MIDDLE, 2, 2, 64, 16, FORMATS["bf16"], torch.bfloat16, seed=12, spread=spread).check()
+
+
+@gpu
+def test_attention_offsets_past_32_bits():
+    """A pool whose bytes and whose rows' offsets pass 32 bits, with the pages in use at its end."""
+    for lens in ([(2, 200), (40, 70)], [(20, 300)]):
+        s = TreeStep(lens, 8, 2, 128, 16, None, torch.bfloat16, seed=13, garbage=False, pages=(1 << 20) + 200000)
+        assert int(s.table.max()) * 16 * 8 * 128 * 2 > 1 << 32
+        s.check()
+    TreeStep([(2, 200), (40, 70)], 8, 2, 128, 16, FORMATS["mx32"], torch.float32, seed=13, garbage=False, pages=(1 << 20) + 200000).check()
+
+
+@gpu
+def test_attention_bad_indices_do_not_reach_memory():
+    """Page indices outside the pool read page 0, lengths stop at the table row, token ranges at the packed tokens."""
+    s = TreeStep([(2, 60), (30, 64)], 2, 2, 64, 16, FORMATS["mx32"], torch.float32, seed=14)
+    s.table[0, :4] = ints([2 ** 31 - 1, -5, s.cache.c.pages, -2 ** 31])
+    s.kv_len.fill_(2 ** 31 - 1)
+    s.q_start.copy_(ints([-4, 2, 2 ** 31 - 1]))
+    for lens in ((1, 1), (30, 64), (100, 100000)):
+        assert s.run(max_new=lens[0], max_len=lens[1]).shape == (32, 256)
+
+
+@gpu
+@pytest.mark.parametrize("lens", [[(9, 5000), (64, 900)], [(25, 3000), (20, 20)], [(7, 4000), (2, 60)]])
+def test_attention_same_inputs_same_bits_also_on_another_stream(lens):
+    s = TreeStep(lens, 2, 4, 128, 16, FORMATS["mx32"], torch.float32, seed=15)
+    ws = mx.cache_tree_workspace(s.cache.c, s.tokens, len(s.lens), 8, s.max_new, s.max_len, DEV)
+    first = s.check(workspace=ws)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        again = s.run(workspace=ws)
+    assert torch.equal(first, again) and not ws[:65536].any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attention_of_a_chain_is_causal_attention(dtype):
+    """Chains are prompts: the same values as mx_cache_attention's, up to twice what either may be off."""
+    s = TreeStep([(70, 200), (5, 900), (24, 24)], 2, 3, 64, 16, FORMATS["mx32"], dtype, seed=16, reach=1)
+    got, causal = s.check(), Step.run(s)
+    assert ((got.double() - causal.double()).abs().cpu().numpy() <= 2 * s.reference()[1]).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("requests,heads,group,most_new,longest", [(40, 8, 4, 4, 41000), (64, 12, 1, 9, 600), (65, 8, 1, 30, 700),
+                                                                 (300, 4, 1, 5, 200), (150, 2, 2, 60, 90)])
+def test_attention_many_requests(dtype, requests, heads, group, most_new, longest):
+    r = np.random.default_rng(requests + longest)
+    lens = [(int(r.integers(0, most_new + 1)), int(r.integers(most_new, min(longest, 400) + 1))) for _ in range(requests)]
+    lens[requests // 2], lens[requests // 3] = (most_new, longest), (1, longest)
+    TreeStep(lens, heads, group, 64, 16, FORMATS["mx32"], dtype, seed=requests).check()
+
+
+def test_attention_smaller_batches_need_no_more_workspace():
+    import random
+    r = random.Random(6)
+
+    def size(heads, group, dim, *n):
+        return mx.mx_cache_tree_attention_workspace_bytes(mx.cache_format(4, 16, heads, dim), n[0], n[1], heads * group, n[2], n[3])
+    for _ in range(20000):
+        heads, group, dim = r.randint(1, 40), r.randint(1, 20), 16 * r.randint(1, 8)
+        top = [int(2 ** r.uniform(0, e)) for e in (18, 13, 14, 21)]
+        less = [r.choice([v, r.randint(1, v)]) for v in top]
+        assert 65536 <= size(heads, group, dim, *less) <= size(heads, group, dim, *top) < 600e6, (heads, group, dim, less, top)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("heads,group,dim", [(4, 3, 64), (8, 4, 128), (2, 1, 96)])
+def test_attention_one_workspace_for_all_steps(dtype, heads, group, dim):
+    """Steps of many kinds on the workspace of the largest, with a guard behind it that none of them may touch."""
+    most = (700, 12, 300, 6000)
+    need = mx.mx_cache_tree_attention_workspace_bytes(mx.cache_format(4, 16, heads, dim), most[0], most[1], heads * group, *most[2:])
+    space = torch.zeros(need + (64 << 20), dtype=torch.uint8, device=DEV)
+    space[need:] = 0xA5
+    for lens in ([(1, 5000)], [(3, 4096), (1, 4090)], [(1, 900)] * 8, [(9, 700)] * 12, [(4, 300), (1, 6000), (30, 31)], [(200, 2000)], [(1, 1)],
+                 [(9, 5000), (17, 5000)], [(64, 6000), (61, 310), (20, 5000)], [(40, 50)] * 12, [(60, 60), (0, 9), (5, 2)]):
+        step = TreeStep(lens, heads, group, dim, 16, FORMATS["mx32"], dtype, seed=len(lens) + lens[0][0])
+        for max_new, max_len in ((step.max_new, step.max_len), (300, 6000)):
+            step.check(workspace=space[:need], max_new=max_new, max_len=max_len)
+        assert bool((space[need:] == 0xA5).all()) and not space[:65536].any()
+    need = mx.mx_cache_tree_attention_workspace_bytes(step.cache.c, step.tokens, len(step.lens), heads * group, 300, 6000)
+    for bad in (space[:need - 1], space[:2 * need:2], torch.zeros(need, dtype=torch.uint8), space[:0]):
+        with pytest.raises(mx.MxError) as e:
+            step.run(workspace=bad, max_new=300, max_len=6000)
+        assert e.value.status == mx.MX_ERR_BAD_ARG
+
+
+# ---- moved rows -------------------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "mx16", "mx32"])
+@pytest.mark.parametrize("heads,dim,page,nodes,width", [(1, 16, 16, 5, 5), (3, 64, 16, 61, 9), (2, 128, 32, 130, 130), (5, 96, 128, 40, 12), (1, 80, 16, 64, 64)])
+def test_move(kind, heads, dim, page, nodes, width):
+    if kind == "mx32" and dim % 32:
+        kind = "mx16"
+    f, r = FORMATS[kind], np.random.default_rng(nodes + dim)
+    ctx = [0, 1, page - 1, page, 3 * page - 2, 17, 200]
+    B, need = len(ctx), [-(-(c + nodes) // page) for c in ctx]
+    cache = mx.Cache(sum(need) + 1, page, heads, dim, f, DEV)
+    arrays = [t for t in (cache.k, cache.v, cache.k_exps, cache.v_exps) if t is not None]
+    for t in arrays:
+        t.copy_(torch.from_numpy(r.integers(0, 256, t.numel(), dtype=np.uint8)))
+    ids = r.permutation(sum(need) + 1)
+    table = np.full((B, max(need)), -1, np.int32)
+    for b in range(B):
+        table[b, :need[b]] = ids[sum(need[:b]):sum(need[:b + 1])]
+    path, kept = np.full((B, width), -1, np.int32), [min(width, nodes), 0, 1, min(width, nodes) // 2 + 1, 3, min(width, nodes), 2]
+    for b, k in enumerate(kept):
+        path[b, :k] = np.concatenate([[0], np.sort(r.permutation(np.arange(1, nodes))[:k - 1])])[:k]
+    path[4, 1] = -7                                          # skipped
+    kept[5] += 1000                                          # the path's width is all there is
+    if width < nodes:
+        path[5, -1] = nodes
+        table[5, (ctx[5] + nodes) // page:] = -1             # no page there (unless it shares one)
+    want = [t.cpu().numpy().copy() for t in arrays]
+    was = [t.copy() for t in want]
+    for b in range(B):
+        for i in range(min(max(kept[b], 0), width)):
+            old, new = ctx[b] + path[b, i], ctx[b] + i
+            if path[b, i] < 0 or old >= table.shape[1] * page or new >= table.shape[1] * page or table[b, old // page] < 0 or table[b, new // page] < 0:
+                continue
+            for w, o in zip(want, was):
+                w, o = (x.reshape(cache.c.pages, heads, page, -1) for x in (w, o))
+                w[table[b, new // page], :, new % page] = o[table[b, old // page], :, old % page]
+    mx.cache_move(cache, torch.from_numpy(table).to(DEV), ints(ctx), torch.from_numpy(path).to(DEV), ints(kept))
+    for t, w in zip(arrays, want):
+        assert np.array_equal(t.cpu().numpy(), w)
+
+
+@gpu
+def test_move_of_anything_stays_in_the_pool():
+    cache, big = mx.Cache(4, 16, 2, 64, FORMATS["mx32"], DEV), 2 ** 31 - 1
+    guard = [t.clone() for t in (cache.k, cache.v, cache.k_exps, cache.v_exps)]
+    table = ints([[big, -5, 4, -big - 1], [0, 1, 2, 3], [0, 1, 2, 3]])
+    for ctx in ([0, -1, big], [-big - 1, big, 60]):
+        for path in ([[0, big, 5, 1]] * 3, [[-1, -big - 1, 70, big]] * 3):
+            mx.cache_move(cache, table, ints(ctx), ints(path), ints([4, big, 3]))
+    torch.cuda.synchronize()
+    for t, g in zip((cache.k, cache.v, cache.k_exps, cache.v_exps), guard):
+        assert torch.equal(t, g)                             # (zeros over zeros)

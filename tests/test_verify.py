@@ -1,0 +1,339 @@
+"""Verification of drafted tokens: the walk against a plain implementation in 64 bits, and what it draws against the distribution."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2307_15517_amd import mx
+from test_cache import DEV, ints
+
+gpu = pytest.mark.gpu
+
+
+def test_refusals():
+    def call(logits=256, draft=256, type=mx.MX_F32, tokens=4, vocab=100, ldl=100, ldd=100, ids=256, parents=256, qs=256, B=2, temp=256, u=256,
+             noise=256, ldn=100, ws=256, path=256, pw=4, kept=256, nxt=256):
+        return mx.mx_verify(logits, draft, type, tokens, vocab, ldl, ldd, ids, parents, qs, B, temp, u, noise, ldn, ws, path, pw, kept, nxt,
+                            stream=0, check=False)
+    for kw in (dict(logits=0), dict(ids=0), dict(parents=0), dict(qs=0), dict(temp=0), dict(u=0), dict(noise=0), dict(ws=0), dict(path=0),
+               dict(kept=0), dict(nxt=0), dict(type=2), dict(tokens=-1), dict(vocab=0), dict(ldl=99), dict(ldd=99), dict(ldn=99), dict(B=-1),
+               dict(pw=0), dict(logits=258), dict(draft=258), dict(logits=257, type=mx.MX_BF16), dict(ws=128), dict(ids=258),
+               dict(parents=258), dict(qs=258), dict(temp=257), dict(u=258), dict(noise=258), dict(path=258), dict(kept=258), dict(nxt=258)):
+        assert call(**kw) == mx.MX_ERR_BAD_ARG, kw
+    big = (1 << 28) + 1
+    for kw in (dict(B=16385), dict(tokens=1 << 31), dict(vocab=big, ldl=big, ldd=big, ldn=big), dict(pw=1 << 31)):
+        assert call(**kw) == mx.MX_ERR_UNSUPPORTED, kw
+    assert call(B=0) == mx.MX_OK and call(B=0, logits=0, ws=0, path=0) == mx.MX_OK
+    assert mx.mx_verify_workspace_bytes(4, 2, 100) >= 65536
+    for bad in ((-1, 2, 100), (4, -1, 100), (4, 2, 0), (4, 16385, 100), (1 << 31, 2, 100), (4, 2, big)):
+        assert mx.mx_verify_workspace_bytes(*bad) == 0
+
+
+def softmax(x, t):
+    with np.errstate(invalid="ignore"):
+        top = x.max()
+        e = np.exp((x - top) / t) if top > -np.inf else np.zeros_like(x)
+    return e / e.sum() if e.sum() > 0 else e
+
+
+def walk(logits, draft, ids, parents, temperature, uniform, noise, width):
+    """(path, next, sure) of one request; sure: no decision stands so near to its border that the call's numerics may tip it."""
+    n, vocab = logits.shape
+    if n == 0:
+        return [], -1, True
+    node, path, sure = 0, [0], True
+    cold = not temperature > 0
+    while True:
+        children = [i for i in range(node + 1, n) if parents[i] == node] if len(path) < width else []
+        x = logits[node]
+        if cold:
+            first = int(x.argmax()) if x.max() > -np.inf else -1
+            to = next((i for i in children if ids[i] == first and first >= 0), -1)
+            if to < 0:
+                return path, first, sure
+            node = to
+            path.append(node)
+            continue
+        p = softmax(x, temperature)
+        q = softmax(draft[node], temperature) if draft is not None and children else None
+        r, mass, off, to = p.copy(), 1.0, 2.0 ** -20 * p, -1   # off: how far a value of r may be from the call's
+        for i in children:
+            token = ids[i] if 0 <= ids[i] < vocab else -1
+            drawn = 1.0 if q is None else q[token] if token >= 0 else 0.0
+            left = r[token] if token >= 0 else 0.0
+            need = uniform[i] * mass * drawn
+            if abs(need - left) <= 2.0 ** -19 * (need + left) + (off[token] if token >= 0 else 0.0) and max(need, left) > 0:
+                sure = False
+            if need < left:
+                to = i
+                break
+            if q is None:
+                if token >= 0:
+                    mass, r[token] = max(mass - left, 0.0), 0.0
+            else:
+                off = off + 2.0 ** -19 * mass * q
+                r = np.maximum(r - mass * q, 0.0)
+                mass = r.sum()
+        if to >= 0:
+            node = to
+            path.append(node)
+            continue
+        if not r.max() > 0:
+            r, off = p, 2.0 ** -20 * p
+        if not r.max() > 0:
+            return path, -1, sure
+        score = r / noise
+        best = int(score.argmax())
+        most = (r + np.where(r > 0, off, 0.0)) / noise
+        most[best] = 0.0
+        if q is not None:                                      # values that cancel may come out a little above 0
+            most = np.maximum(most, np.where(np.arange(vocab) == best, 0.0, off / noise))
+        if most.max() >= score[best] * (1 - 2.0 ** -20) - off[best] / noise[best]:
+            sure = False
+        return path, best, sure
+
+
+class Batch:
+    def __init__(self, sizes, vocab, dtype, drawn, seed, branch=3, width=8, pad=(0, 0, 0), greedy=0.0, lead=0, tail=0, sharp=4.0, hide=0.0):
+        r = np.random.default_rng(seed)
+        self.sizes, self.vocab, self.width, self.lead = sizes, vocab, width, lead
+        T, B = lead + sum(sizes) + tail, len(sizes)
+        self.starts = (lead + np.concatenate([[0], np.cumsum(sizes)])).astype(int).tolist()
+
+        def rows(x, extra):
+            full = torch.zeros((max(1, T), vocab + extra), dtype=dtype, device=DEV)
+            full[:T, :vocab] = torch.from_numpy(x.astype(np.float32)).to(DEV).to(dtype)
+            return full[:T, :vocab]
+        x = sharp * r.standard_normal((T, vocab))
+        y = x + r.standard_normal((T, vocab))
+        if hide:
+            gone = r.random((T, vocab)) < hide
+            x[gone] = -np.inf
+            y[gone & (r.random((T, vocab)) < 0.5)] = -np.inf
+        self.logits = rows(x, pad[0])
+        self.draft = rows(y, pad[1]) if drawn else None
+        self.parents = np.full(T, -1)
+        self.ids = np.zeros(T, int)
+        heat = np.where(r.random(B) < greedy, 0.0, r.choice([0.5, 0.8, 1.0, 1.3], B))
+        near = rows(y, 0).double().cpu().numpy()
+        for b, n in enumerate(sizes):
+            lo = self.starts[b]
+            order = {}
+            for i in range(1, n):
+                p = int(r.integers(max(0, i - branch), i))
+                self.parents[lo + i] = p
+                row = near[lo + p]
+                if drawn and heat[b] > 0 and row.max() > -np.inf:
+                    self.ids[lo + i] = r.choice(vocab, p=softmax(row, heat[b]))
+                else:
+                    order[p] = order.get(p, -1) + 1
+                    self.ids[lo + i] = np.argsort(-row)[min(order[p], vocab - 1)]
+        self.temperature = torch.from_numpy(heat.astype(np.float32)).to(DEV)
+        self.uniform = torch.from_numpy(r.random(T).astype(np.float32) * (1 - 2.0 ** -24)).to(DEV)
+        self.noise = torch.from_numpy(np.maximum(r.exponential(1.0, (max(1, B), vocab + pad[2])), 1e-30).astype(np.float32)).to(DEV)[:B, :vocab]
+
+    def run(self, workspace=None):
+        got = mx.verify(self.logits, ints(self.ids.tolist()), ints(self.parents.tolist()), ints(self.starts), self.temperature, self.uniform,
+                        self.noise, self.width, self.draft, workspace)
+        torch.cuda.synchronize()
+        return got
+
+    def check(self, got=None):
+        path, kept, following = (t.cpu().numpy() for t in (got or self.run()))
+        x = self.logits.double().cpu().numpy()
+        y = None if self.draft is None else self.draft.double().cpu().numpy()
+        heat, u, z = (t.double().cpu().numpy() for t in (self.temperature, self.uniform, self.noise))
+        unsure = 0
+        for b, n in enumerate(self.sizes):
+            at = slice(self.starts[b], self.starts[b] + n)
+            want, token, sure = walk(x[at], None if y is None else y[at], self.ids[at], self.parents[at], heat[b], u[at], z[b], self.width)
+            if not sure:
+                unsure += 1
+                continue
+            assert kept[b] == len(want) and path[b, :len(want)].tolist() == want and following[b] == token, (b, want, token, path[b], following[b])
+            assert (path[b, len(want):] == -1).all()
+        assert unsure <= 1 + len(self.sizes) // 50, unsure
+        return got
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("vocab", [1, 2, 7, 8, 63, 1000, 8191, 50272, 100003])
+def test_walks(dtype, drawn, vocab):
+    Batch([5, 1, 0, 9, 17, 2], vocab, dtype, drawn, seed=vocab).check()
+    if vocab <= 8191:
+        Batch([6] * 30 + [1] * 20 + [25] * 10, vocab, dtype, drawn, seed=vocab + 1, branch=2, greedy=0.3, width=5).check()
+
+
+@gpu
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("sizes,branch,width", [([64, 61, 65, 130], 5, 20), ([1100, 3], 40, 30), ([200], 1, 300), ([200], 199, 4), ([9] * 50, 2, 1)])
+def test_trees(drawn, sizes, branch, width):
+    """Many nodes, deep chains, one node with hundreds of children, paths that are full at once."""
+    for sharp in (1.0, 8.0):
+        Batch(sizes, 300, torch.float32, drawn, seed=sum(sizes), branch=branch, width=width, sharp=sharp).check()
+
+
+@gpu
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_strides_padding_and_alignment(drawn, dtype):
+    for pad in ((1, 0, 0), (3, 5, 7), (8, 8, 4), (0, 1, 1)):
+        Batch([5, 8, 2, 0, 13], 515, dtype, drawn, seed=3, pad=pad, lead=4, tail=6).check()
+
+
+@gpu
+@pytest.mark.parametrize("drawn", [False, True])
+def test_tokens_that_cannot_come(drawn):
+    """Minus infinity in some places, in nearly all, in all; next = -1 where there is nothing."""
+    for hide in (0.3, 0.95):
+        Batch([7] * 40, 200, torch.float32, drawn, seed=4, hide=hide, greedy=0.2).check()
+    b = Batch([4, 4, 1, 1], 100, torch.float32, drawn, seed=5)
+    b.logits[b.starts[0]] = -np.inf
+    b.logits[b.starts[2]] = -np.inf
+    b.logits[b.starts[3], torch.arange(100, device=DEV) != 57] = -np.inf
+    b.temperature[2] = 0.0
+    path, kept, following = b.check(b.run())
+    assert kept.tolist()[0] == 1 and following[0] == -1 and following[2] == -1 and following[3] == 57
+
+
+@gpu
+def test_draft_tokens_that_are_none():
+    """Tokens outside the vocabulary, twice the same token among siblings, all probability on a rejected token."""
+    for drawn in (False, True):
+        b = Batch([10] * 20, 50, torch.float32, drawn, seed=6, branch=9)
+        b.ids[1::5], b.ids[2::7] = -1, 2 ** 31 - 1
+        b.ids[3::6] = b.ids[2::6][:len(b.ids[3::6])]
+        b.check()
+    b = Batch([3, 3], 16, torch.float32, False, seed=7)
+    b.logits[:] = -np.inf
+    b.logits[:, 5] = 0.0
+    b.ids[:], b.parents[:] = 5, [-1, 0, 0] * 2
+    b.uniform[:] = 1.0                                         # (a caller's mistake: nothing is accepted, p is drawn from itself)
+    path, kept, following = b.run()
+    assert kept.tolist() == [1, 1] and following.tolist() == [5, 5]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_greedy_takes_the_first_of_equal_ones(dtype):
+    b = Batch([6] * 10, 3000 + 5, dtype, True, seed=8, greedy=1.0)
+    b.logits[:] = torch.round(b.logits.float() / 4).to(dtype)
+    assert float((b.logits == b.logits.amax(-1, keepdim=True)).sum(-1).float().mean()) > 2
+    first = b.logits.float().cpu().numpy().argmax(-1)
+    b.ids[1:] = np.where(np.arange(1, len(b.ids)) % 3 > 0, first[b.parents[1:] + np.repeat(b.starts[:-1], 6)[1:]], b.ids[1:])
+    for t in (b.uniform, b.noise, b.draft):
+        t.fill_(float("nan"))                                  # play no part
+    b.check()
+
+
+@gpu
+def test_temperatures():
+    for heat in (1e-38, 1e-3, 1e4, 1e38, float("inf")):
+        b = Batch([6] * 10, 400, torch.float32, False, seed=9)
+        b.temperature.fill_(heat)
+        path, kept, following = b.run()
+        if heat == 1e-38:                                      # as good as greedy
+            b.temperature.fill_(0.0)
+            again = b.run()
+            assert torch.equal(path, again[0]) and torch.equal(following, again[2])
+        elif heat < 1e30:
+            b.check((path, kept, following))
+        assert bool((following >= 0).all()) and bool((following < 400).all())
+    for heat in (-1.0, float("nan"), -0.0):
+        b.temperature.fill_(heat)
+        again = b.run()
+        b.temperature.fill_(0.0)
+        assert all(torch.equal(x, y) for x, y in zip(again, b.run()))
+
+
+@gpu
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("drawn", [False, True])
+def test_numbers_that_are_none_do_not_fault(bad, drawn):
+    for where in ("logits", "draft", "uniform", "noise"):
+        b = Batch([6] * 10, 400, torch.float32, drawn, seed=10, greedy=0.3)
+        t = getattr(b, where)
+        if t is None:
+            continue
+        t.view(-1)[::3] = bad
+        path, kept, following = b.run()
+        assert bool((kept >= 1).all()) and bool((following >= -1).all()) and bool((following < 400).all())
+
+
+@gpu
+@pytest.mark.parametrize("drawn", [False, True])
+def test_token_ranges_that_are_none(drawn):
+    b = Batch([5, 5, 5], 300, torch.float32, drawn, seed=11)
+    big = 2 ** 31 - 1
+    for starts in ([-4, 3, 3, 15], [0, 9, 4, 15], [15, 15, 15, 15], [0, big, big, big], [20, -1, 5, 9]):
+        b.starts = starts
+        path, kept, following = b.run()
+        for i in range(3):
+            n = max(0, min(starts[i + 1], 15) - min(max(starts[i], 0), 15))
+            assert (int(kept[i]) == 0 and int(following[i]) == -1 and bool((path[i] == -1).all())) if n == 0 else int(kept[i]) >= 1
+
+
+@gpu
+@pytest.mark.parametrize("drawn,branch", [(True, 1), (True, 4), (False, 1), (False, 4)])
+def test_tokens_are_distributed_as_the_models(drawn, branch):
+    """16000 walks of the same tree of four nodes: the first token of each, accepted or drawn at the end, follows the model's
+    distribution, whatever the draft's.  Counts within six standard deviations (2e-9 a count)."""
+    N, vocab = 16000, 6
+    r = np.random.default_rng(12)
+    p, q = softmax(1.5 * r.standard_normal(vocab), 1.0), softmax(1.5 * r.standard_normal(vocab), 1.0)
+    x = np.tile(np.log(p), (4 * N, 1)).astype(np.float32)
+    y = np.tile(np.log(q), (4 * N, 1)).astype(np.float32)
+    parents = np.array([-1, 0, 1, 2] if branch == 1 else [-1, 0, 0, 0])
+    ids = r.choice(vocab, (N, 4), p=q) if drawn else np.tile([0, 3, 1, 4], (N, 1))
+    up = lambda v: torch.from_numpy(np.ascontiguousarray(v)).to(DEV)  # noqa: E731
+    path, kept, following = mx.verify(up(x), up(ids.reshape(-1).astype(np.int32)), up(np.tile(parents, N).astype(np.int32)),
+                                      up(np.arange(0, 4 * N + 1, 4, dtype=np.int32)), torch.ones(N, device=DEV),
+                                      up(r.random(4 * N).astype(np.float32)), up(r.exponential(1.0, (N, vocab)).astype(np.float32)), 4,
+                                      up(y) if drawn else None)
+    path, kept, following = path.cpu().numpy(), kept.cpu().numpy(), following.cpu().numpy()
+    first = np.where(kept > 1, ids[np.arange(N), np.where(kept > 1, path[:, 1], 0)], following)
+    count = np.bincount(first, minlength=vocab)
+    assert (np.abs(count - N * p) <= 6 * np.sqrt(N * p * (1 - p))).all(), (count, N * p)
+    assert kept.max() > 1 and kept.min() == 1
+
+
+@gpu
+def test_offsets_past_32_bits():
+    """Logits of more than 2^32 bytes, the request's rows at their end."""
+    vocab, T = 1 << 18, 4200
+    logits = torch.zeros((T, vocab), device=DEV)
+    b = Batch([6], vocab, torch.float32, False, seed=13)
+    logits[T - 6:] = b.logits
+    assert (T - 6) * vocab * 4 > 1 << 32
+    pad = T - 6
+    got = mx.verify(logits, ints([0] * pad + b.ids.tolist()), ints([-1] * pad + b.parents.tolist()), ints([pad, T]), b.temperature,
+                    torch.cat([torch.zeros(pad, device=DEV), b.uniform]), b.noise, b.width)
+    b.check(got)
+
+
+@gpu
+@pytest.mark.parametrize("drawn", [False, True])
+def test_same_results_on_another_stream_and_one_workspace(drawn):
+    most = mx.mx_verify_workspace_bytes(900, 70, 60000)
+    ws = torch.zeros(most + 4096, dtype=torch.uint8, device=DEV)
+    ws[most:] = 0xA5
+    for sizes, vocab in (([5], 50272), ([5] * 8, 32000), ([12] * 60, 2000), ([61] * 8, 9001), ([1], 3)):
+        assert mx.mx_verify_workspace_bytes(sum(sizes), len(sizes), vocab) <= most
+        b = Batch(sizes, vocab, torch.float32, drawn, seed=len(sizes))
+        first = b.check(b.run(ws[:most]))
+        other = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(other):
+            again = b.run(ws[:most])
+        assert all(torch.equal(x, y) for x, y in zip(first, again))
+        assert not ws[:65536].any() and bool((ws[most:] == 0xA5).all())
+
+
+def test_smaller_batches_need_no_more_workspace():
+    import random
+    r = random.Random(7)
+    for _ in range(20000):
+        top = [int(2 ** r.uniform(0, e)) for e in (15, 13, 20)]
+        less = [r.choice([v, r.randint(1, v)]) for v in top]
+        assert 65536 <= mx.mx_verify_workspace_bytes(*less) <= mx.mx_verify_workspace_bytes(*top), (less, top)
