@@ -25,28 +25,35 @@ struct VerifyArgs {
     int32_t* next;
     int64_t tokens, ldl, ldd, ldn, width;
     int32_t vocab, requests;
+    struct Control* control;
+    uint64_t* parts;           // [request][2][slots][3]
+    int32_t team;              // workgroups a request
+    int32_t segments;          // of a row
+    int32_t slots;
+    int32_t wide;              // a request with so many nodes or fewer has the rows of all of them read at once
+    int32_t ahead;             // else so many children's rows with a node's
 };
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr size_t kCounterBytes = 65536;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kNodes = MX_TREE_MAX_NODES;
+constexpr int kMostRows = 16;              // nodes whose rows are read at once
+constexpr int kMostSegments = 64;          // of a row, a lane each where they are joined
+constexpr int kMostMembers = 1024, kMostTeams = 512;
+constexpr int kMostParts = 64 * kMostSegments;   // segments times teams
+constexpr int kExcluded = 16;
+constexpr int kMostPolls = 512;
+constexpr size_t kControlBytes = 65536;
 
-// 2^((x) log2(e) / T), x <= 0: the factor as two floats, and what the product is rounded by as a factor of the result, so that the
-// result is off by little more than the instruction's last bit however large x is.
+// exp(x / T), x <= 0.  The subtraction that gives x, the factor and the product are rounded once each, which moves the exponent y of two by
+// 3 |y| 2^-24 at most; the instruction is off by one unit in the last place.
 struct Heat {
-    float hi, lo;
-    double inv;
+    float scale;               // log2(e) / T
+    double inv;                // 1 / T
     __device__ __forceinline__ explicit Heat(float t) {
         inv = 1.0 / fmin(fmax((double)t, 1e-30), 1e30);     // so that 0 and minus infinity times it are what they are
-        const double c = inv * 1.4426950408889634;
-        hi = (float)c;
-        lo = (float)(c - (double)hi);
+        scale = (float)(inv * 1.4426950408889634);
     }
-    __device__ __forceinline__ float exp_of(float x) const {
-        const float y = x * hi, rest = __builtin_fmaf(x, hi, -y) + x * lo;
-        const float e = __builtin_amdgcn_exp2f(y);
-        return y < -126.f ? 0.f : __builtin_fmaf(e, rest * 0.6931471805599453f, e);
-    }
+    __device__ __forceinline__ float exp_of(float x) const { return __builtin_amdgcn_exp2f(x * scale); }
 };
 
 template <int TYPE>
@@ -76,241 +83,605 @@ __device__ __forceinline__ const void* row_at(const void* base, int64_t element)
     return static_cast<const char*>(base) + element * (TYPE == MX_F32 ? 4 : 2);
 }
 
-// What a pass over a row of logits finds: the largest and the first place that has it, the sum of exp((x - top) / T), and of the
-// race exp((x - top) / T) / noise the winner, the first of equal ones, among the tokens that are not tried as children.
+// All lanes' values as one, in every lane, without LDS: neighbours, quads, rows of sixteen mirrored, then the rows.
+template <int STEP>
+__device__ __forceinline__ void pair_of(uint32_t v, uint32_t& x, uint32_t& y) {
+    if constexpr (STEP < 4) {
+        constexpr int ctrl = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;
+        x = v;
+        y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xF, 0xF, true);
+    } else {
+        const auto r = STEP == 4 ? __builtin_amdgcn_permlane16_swap(v, v, false, false) : __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        x = r[0];
+        y = r[1];
+    }
+}
+template <int STEP = 0, typename Op>
+__device__ __forceinline__ uint32_t over_wave(uint32_t v, Op op) {
+    if constexpr (STEP == 6) {
+        return v;
+    } else {
+        uint32_t x, y;
+        pair_of<STEP>(v, x, y);
+        return over_wave<STEP + 1>(op(x, y), op);
+    }
+}
+template <int STEP = 0, typename Op>
+__device__ __forceinline__ uint64_t over_wave64(uint64_t v, Op op) {
+    if constexpr (STEP == 6) {
+        return v;
+    } else {
+        uint32_t x0, y0, x1, y1;
+        pair_of<STEP>((uint32_t)v, x0, y0);
+        pair_of<STEP>((uint32_t)(v >> 32), x1, y1);
+        return over_wave64<STEP + 1>(op((uint64_t)x1 << 32 | x0, (uint64_t)y1 << 32 | y0), op);
+    }
+}
+
+// What a pass over a part of a row finds: the largest and the first place that has it, the sum of exp((x - top) / T), and of the race
+// exp((x - top) / T) / noise the winner, the first of equal ones, among the tokens that are not excluded.
 struct Found {
     float top;
     int top_at;
     double sum;
     float best;
     int best_at;               // -1: none with a probability above 0
+
+    // The parts of a wave's lanes as one
+    __device__ __forceinline__ void join(const Heat& heat) {
+        const float m = __uint_as_float(over_wave(__float_as_uint(top), [](uint32_t x, uint32_t y) {
+            return __float_as_uint(__builtin_fmaxf(__uint_as_float(x), __uint_as_float(y)));
+        }));
+        const float f = top == m ? 1.f : heat.exp_of(top - m);
+        top_at = (int)over_wave(top == m ? (uint32_t)top_at : INT_MAX, [](uint32_t x, uint32_t y) { return min(x, y); });
+        top = m;
+        sum = __builtin_bit_cast(double, over_wave64(__builtin_bit_cast(uint64_t, sum * f), [](uint64_t x, uint64_t y) {
+            return __builtin_bit_cast(uint64_t, __builtin_bit_cast(double, x) + __builtin_bit_cast(double, y));
+        }));
+        // scores are not negative: their bits are in their order, and of equal ones the smaller place is to win
+        best *= f;
+        const uint64_t key = over_wave64(best > 0.f ? (uint64_t)__float_as_uint(best) << 32 | (uint32_t)~best_at : 0ull,
+                                         [](uint64_t x, uint64_t y) { return x > y ? x : y; });
+        best = __uint_as_float((uint32_t)(key >> 32));
+        best_at = key == 0 ? -1 : (int)~(uint32_t)key;
+    }
+};
+constexpr Found kNothing{-__builtin_inff(), INT_MAX, 0.0, 0.f, -1};
+
+// What a team works on: rows of logits (kRows), or of one node what is left of p when c q is taken off, its sum (kSum) or the winner of its
+// race (kRace; c < 0 stands for p itself, whatever was tried).
+enum { kRows = 0, kSum = 1, kRace = 2 };
+struct Job {
+    int kind, node, kept;
+    int next_child;            // kSum: where the next child is looked for
+    float p_top, q_top;
+    double c, mass, p_sum, q_sum;
 };
 
-struct Child {
-    int node, token;
-    float uniform;
-    bool tried_before;         // an earlier sibling has the same token
-    double p, q;
+// Of the workspace, zero before its first use and the calls' own from then on.  A call's number is `number`; the last of its workgroups that
+// has read it puts the next one there.
+struct Control {
+    uint64_t number;
+    uint32_t teams, unused;             // teams of this call whose members have all read the number
+    uint32_t members[kMostTeams];       // of a team
+    uint64_t posted[kMostMembers];      // number << 16 | jobs done, of every member
 };
+static_assert(sizeof(Control) <= kControlBytes, "the workspace's first part");
 
 struct Shared {
-    float top[kWaves];
-    int top_at[kWaves];
-    double sum[kWaves];
-    float best[kWaves];
-    int best_at[kWaves];
-    Child child[kNodes];
+    Found found[2 * kMostRows];
+    int row[kMostRows];
+    uint64_t part[kMostSegments][3];    // of a row that a workgroup reads alone
+    int excluded[kWaves][kExcluded];
+    uint32_t all_here;
+    int parent[kNodes], id[kNodes];
+    float uniform[kNodes], lp[kNodes], lq[kNodes];   // lp, lq: the logits of node i's token in the rows of its parent
 };
 
-__device__ __forceinline__ bool is_child(const Shared& s, int children, int token) {
-    for (int k = 0; k < children; ++k)
-        if (s.child[k].token == token) return true;
-    return false;
+__device__ __forceinline__ void put(uint64_t* p, uint64_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ uint64_t get(const uint64_t* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ uint64_t both(uint32_t lo, uint32_t hi) { return (uint64_t)hi << 32 | lo; }
+// What this wave has stored is where every compute unit sees it
+__device__ __forceinline__ void stored() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+    __builtin_amdgcn_s_waitcnt(0);
 }
 
-// The parts of all threads as one, the same in every thread.
-__device__ __forceinline__ Found join(Found f, const Heat& heat, Shared& s) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    auto add = [&](float top, int top_at, double sum, float best, int best_at) __attribute__((always_inline)) {
-        const float m = __builtin_fmaxf(f.top, top);
-        const float mine = f.top == m ? 1.f : heat.exp_of(f.top - m), its = top == m ? 1.f : heat.exp_of(top - m);
-        f.top_at = f.top > top ? f.top_at : top > f.top ? top_at : min(f.top_at, top_at);
-        f.top = m;
-        f.sum = f.sum * mine + sum * its;
-        const float x = f.best * mine, y = best * its;
-        f.best_at = x > y ? f.best_at : y > x ? best_at : (int)min((uint32_t)f.best_at, (uint32_t)best_at);
-        f.best = __builtin_fmaxf(x, y);
-    };
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2)
-        add(__shfl_xor(f.top, d), __shfl_xor(f.top_at, d), __shfl_xor(f.sum, d), __shfl_xor(f.best, d), __shfl_xor(f.best_at, d));
-    __syncthreads();
-    if (lane == 0) {
-        s.top[wave] = f.top;
-        s.top_at[wave] = f.top_at;
-        s.sum[wave] = f.sum;
-        s.best[wave] = f.best;
-        s.best_at[wave] = f.best_at;
+// Once for every workgroup, after it has read the call's number
+__device__ __forceinline__ void team_counts_in(const VerifyArgs& a, int b, uint64_t number) {
+    Control* c = a.control;
+    if (__hip_atomic_fetch_add(&c->members[b], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != (uint32_t)a.team - 1) return;
+    __hip_atomic_store(&c->members[b], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (__hip_atomic_fetch_add(&c->teams, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != (uint32_t)a.requests - 1) return;
+    __hip_atomic_store(&c->teams, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    put(&c->number, number + 1);
+}
+
+__device__ __forceinline__ double lane_of(double v, int lane) {
+    const uint64_t x = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+template <int TYPE>
+struct Team {
+    const VerifyArgs& a;
+    Shared& s;
+    int b, member, n;
+    int64_t t0;
+    bool cold, drafted;
+    Heat heat;
+    const float* noise;
+    int lane, wave;
+    int base, up, id;          // of node base + lane: parent, token, random number, its logits in its parent's rows
+    float uniform, lp, lq;
+    int nodes;                 // on the list of rows
+
+    __device__ __forceinline__ Team(const VerifyArgs& args, Shared& shared)
+        : a(args), s(shared), b(blockIdx.x / args.team), member(blockIdx.x % args.team), heat(1.f), lane(threadIdx.x & 63),
+          wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), base(-1) {
+        const int64_t lo = a.q_start[b], hi = a.q_start[b + 1];
+        const float t = a.temperature[b];
+        t0 = lo < 0 ? 0 : lo > a.tokens ? a.tokens : lo;
+        const int64_t t1 = hi > a.tokens ? a.tokens : hi;
+        n = (int)min(max(t1 - t0, (int64_t)0), (int64_t)kNodes);
+        cold = !(t > 0.f);
+        drafted = a.draft != nullptr && !cold;
+        heat = Heat(cold ? 1.f : t);
+        noise = a.noise + b * a.ldn;
     }
-    __syncthreads();
-    f = Found{s.top[0], s.top_at[0], s.sum[0], s.best[0], s.best_at[0]};
-    for (int w = 1; w < kWaves; ++w) add(s.top[w], s.top_at[w], s.sum[w], s.best[w], s.best_at[w]);
-    return f;
-}
+    __device__ __forceinline__ const void* logits_of(int node) const { return row_at<TYPE>(a.logits, (t0 + node) * a.ldl); }
+    __device__ __forceinline__ const void* draft_of(int node) const { return row_at<TYPE>(a.draft, (t0 + node) * a.ldd); }
 
-// RACE: with the race against the random numbers; `children` of s.child do not take part in it.
-template <int TYPE, bool RACE>
-__device__ __forceinline__ Found pass(const VerifyArgs& a, const void* row, const float* noise, const Heat& heat, int children, Shared& s) {
-    Found f{-__builtin_inff(), INT_MAX, 0.0, 0.f, -1};
-    auto take = [&](int at, const float* x, const float* z, auto count_c) __attribute__((always_inline)) {
-        constexpr int N = decltype(count_c)::value;
-        float top = x[0];
-#pragma unroll
-        for (int e = 1; e < N; ++e) top = __builtin_fmaxf(top, x[e]);
-        if (top > f.top) {
-#pragma unroll
-            for (int e = N - 1; e >= 0; --e)
-                if (x[e] == top) f.top_at = at + e;
-            const float less = f.top == -__builtin_inff() ? 0.f : heat.exp_of(f.top - top);
-            f.sum *= less;
-            f.best *= less;
-            f.top = top;
+    // Lane i holds node base + i
+    __device__ __forceinline__ void look_at(int to) {
+        if (to == base) return;
+        base = to;
+        const int k = min(base + lane, kNodes - 1);
+        up = base + lane < n ? s.parent[k] : -2;
+        id = s.id[k];
+        uniform = s.uniform[k];
+        lp = s.lp[k];
+        lq = s.lq[k];
+    }
+    // The first child of `node` from number `from` on, n when there is none
+    __device__ __forceinline__ int child_from(int node, int from) {
+        while (from < n) {
+            look_at(from & ~63);
+            const uint64_t is = __ballot(up == node) & ~0ull << (from & 63);
+            if (is != 0) return base + __builtin_ctzll(is);
+            from = base + 64;
         }
-        if (f.top == -__builtin_inff()) return;
-        float sum = 0.f;
+        return n;
+    }
+    // Whether a child of `node` before number `i` (which is looked at) has the same token
+    __device__ __forceinline__ bool tried_before(int node, int i) {
+        const int token = __builtin_amdgcn_readlane(id, i - base);
+        if ((__ballot(up == node && id == token) & ((1ull << (i - base)) - 1)) != 0) return true;
+        for (int at = (node + 1) & ~63; at < base; at += 64)
+            if (__ballot(s.parent[at + lane] == node && s.id[at + lane] == token) != 0) return true;
+        return false;
+    }
+
+    // The nodes whose rows the walk may come to next, in s.row: all of a small tree, or the node and, as far as there is room, its children.
+    // Each counts for two rows, its logits and its draft's, when the draft plays a part.
+    __device__ __forceinline__ void list_rows(int node, bool all) {
+        int rows = all ? n : 1;
+        __syncthreads();
+        if (threadIdx.x < kMostRows) s.row[threadIdx.x] = all ? threadIdx.x : node;
+        __syncthreads();
+        for (int at = (node + 1) & ~63; !all && at < n && rows <= a.ahead; at += 64) {
+            look_at(at);
+            const uint64_t is = __ballot(up == node);
+            const int place = rows + __popcll(is & ((1ull << lane) - 1));
+            if (wave == 0 && up == node && place <= a.ahead) s.row[place] = base + lane;
+            rows = min(rows + (int)__popcll(is), 1 + a.ahead);
+        }
+        nodes = rows;
+        __syncthreads();
+    }
+    __device__ __forceinline__ int rows() const { return drafted ? 2 * nodes : nodes; }
+    __device__ __forceinline__ int row_of(int node) const {              // -1: not on the list
+        const uint64_t is = __ballot(lane < nodes && s.row[min(lane, kMostRows - 1)] == node);
+        return is == 0 ? -1 : drafted ? 2 * __builtin_ctzll(is) : __builtin_ctzll(is);
+    }
+
+    // Elements 8 o0 .. 8 o1 of a row (`tail`: and those behind them), by one wave; with `race` the race too, without the `excludes` tokens of
+    // node's children that lie there.
+    __device__ __forceinline__ Found scan(const void* row, int o0, int o1, bool tail, bool race, int node, int excludes) {
+        Found f = kNothing;
+        constexpr int U = 4;                       // octets of a lane in flight
+        // N elements from place `at` on: the largest is known to be no larger than f.top
+        auto take = [&](int at, const float* x, float* z, auto count_c) __attribute__((always_inline)) {
+            constexpr int N = decltype(count_c)::value;
+            float p[N], sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float p = heat.exp_of(x[e] - f.top);
-            sum += p;
-            if constexpr (RACE) {
-                const float score = p / z[e];
-                if (score > f.best && !is_child(s, children, at + e)) {
+            for (int e = 0; e < N; ++e) {
+                p[e] = heat.exp_of(x[e] - f.top);
+                sum += p[e];
+            }
+            f.sum += sum;
+            if (!race) return;
+            auto exclude = [&](int token) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) p[e] = token == at + e ? 0.f : p[e];
+            };
+            if (excludes <= kExcluded) {
+                for (int k = 0; k < excludes; ++k) exclude(s.excluded[wave][k]);
+            } else {                               // more than there is room for: all nodes are looked through
+                for (int i = node + 1; i < n; ++i) exclude(s.parent[i] == node ? s.id[i] : -1);
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float score = p[e] * __builtin_amdgcn_rcpf(z[e]);
+                if (score > f.best) {
                     f.best = score;
                     f.best_at = at + e;
                 }
             }
-        }
-        f.sum += sum;
-    };
-    const int octets = a.vocab / 8;
-    for (int o = threadIdx.x; o < octets; o += kThreads) {
-        float x[8], z[8];
-        values8<TYPE>(row, 8 * (int64_t)o, x);
-        if constexpr (RACE) values8<MX_F32>(noise, 8 * (int64_t)o, z);
-        take(8 * o, x, z, std::integral_constant<int, 8>{});
-    }
-    if (const int at = 8 * octets + threadIdx.x; at < a.vocab) {
-        float x[1] = {value_at<TYPE>(row, at)}, z[1] = {RACE ? noise[at] : 1.f};
-        take(at, x, z, std::integral_constant<int, 1>{});
-    }
-    return join(f, heat, s);
-}
-
-// r = max(p - c q, 0): its sum, or with RACE the winner of r / noise.
-template <int TYPE, bool RACE>
-__device__ __forceinline__ Found residual(const VerifyArgs& a, const void* row, const Found& p, const void* drafted, const Found& q, double c,
-                                          const float* noise, const Heat& heat, Shared& s) {
-    const float fp = (float)(1.0 / p.sum), fq = (float)(c / q.sum);
-    Found f{0.f, 0, 0.0, 0.f, -1};
-    auto take = [&](int at, float x, float y, float z) __attribute__((always_inline)) {
-        const float r = __builtin_fmaxf(__builtin_fmaf(heat.exp_of(x - p.top), fp, -(heat.exp_of(y - q.top) * fq)), 0.f);
-        if constexpr (RACE) {
-            const float score = r / z;
-            if (score > f.best) {
-                f.best = score;
-                f.best_at = at;
-            }
-        }
-        return r;
-    };
-    const int octets = a.vocab / 8;
-    for (int o = threadIdx.x; o < octets; o += kThreads) {
-        float x[8], y[8], z[8], sum = 0.f;
-        values8<TYPE>(row, 8 * (int64_t)o, x);
-        values8<TYPE>(drafted, 8 * (int64_t)o, y);
-        if constexpr (RACE) values8<MX_F32>(noise, 8 * (int64_t)o, z);
+        };
+        auto raise = [&](float top) __attribute__((always_inline)) {
+            const float less = f.top == -__builtin_inff() ? 0.f : heat.exp_of(f.top - top);
+            f.sum *= less;
+            f.best *= less;
+            f.top = top;
+        };
+        for (int o = o0 + lane; o < o1; o += 64 * U) {
+            float x[U][8], z[U][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += take(8 * o + e, x[e], y[e], z[e]);
-        f.sum += sum;
+            for (int u = 0; u < U; ++u) values8<TYPE>(row, 8 * (int64_t)min(o + u * 64, o1 - 1), x[u]);
+            if (race) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) values8<MX_F32>(noise, 8 * (int64_t)min(o + u * 64, o1 - 1), z[u]);
+            }
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[u][e] = o + u * 64 < o1 ? x[u][e] : -__builtin_inff();
+                    top = __builtin_fmaxf(top, x[u][e]);
+                }
+            if (top > f.top) {
+                raise(top);
+                if (cold) {
+#pragma unroll
+                    for (int e = 8 * U - 1; e >= 0; --e)
+                        if (x[e / 8][e % 8] == top) f.top_at = 8 * (o + e / 8 * 64) + e % 8;
+                }
+            }
+            if (!cold && f.top > -__builtin_inff()) {
+#pragma unroll 1
+                for (int u = 0; u < U; ++u) {      // (in a loop: the arithmetic is small next to the code it would be four times)
+                    if (o + u * 64 >= o1) break;
+                    take(8 * (o + u * 64), x[0], z[0], std::integral_constant<int, 8>{});
+#pragma unroll
+                    for (int v = 0; v + 1 < U; ++v)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            x[v][e] = x[v + 1][e];
+                            z[v][e] = z[v + 1][e];
+                        }
+                }
+            }
+        }
+        if (const int at = 8 * o1 + lane; tail && at < a.vocab) {
+            float x[1] = {value_at<TYPE>(row, at)}, z[1] = {race ? noise[at] : 1.f};
+            if (x[0] > f.top) {
+                raise(x[0]);
+                f.top_at = at;
+            }
+            if (!cold && f.top > -__builtin_inff()) take(at, x, z, std::integral_constant<int, 1>{});
+        }
+        return f;
     }
-    if (const int at = 8 * octets + threadIdx.x; at < a.vocab)
-        f.sum += take(at, value_at<TYPE>(row, at), value_at<TYPE>(drafted, at), RACE ? noise[at] : 1.f);
-    return join(f, heat, s);
+
+    // r = max(p - c q, 0) of a part of the rows: its sum, and with `race` the winner of r / noise
+    __device__ __forceinline__ Found residual(const Job& j, int o0, int o1, bool tail, bool race) {
+        const bool whole = j.c < 0.0;
+        const void* row = logits_of(j.node);
+        const void* other = whole ? row : draft_of(j.node);
+        const float fp = (float)(1.0 / j.p_sum), fq = whole ? 0.f : (float)(j.c / j.q_sum);
+        const float q_top = whole ? j.p_top : j.q_top;
+        Found f{0.f, 0, 0.0, 0.f, -1};
+        constexpr int U = 2;
+        auto take = [&](int at, const float* x, const float* y, const float* z, auto count_c) __attribute__((always_inline)) {
+            constexpr int N = decltype(count_c)::value;
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float r = __builtin_fmaxf(__builtin_fmaf(heat.exp_of(x[e] - j.p_top), fp, -(heat.exp_of(y[e] - q_top) * fq)), 0.f);
+                sum += r;
+                const float score = r * __builtin_amdgcn_rcpf(z[e]);
+                if (score > f.best) {
+                    f.best = score;
+                    f.best_at = at + e;
+                }
+            }
+            f.sum += sum;
+        };
+        for (int o = o0 + lane; o < o1; o += 64 * U) {
+            float x[U][8], y[U][8], z[U][8];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t at = 8 * (int64_t)min(o + u * 64, o1 - 1);
+                values8<TYPE>(row, at, x[u]);
+                values8<TYPE>(other, at, y[u]);
+            }
+            if (race) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) values8<MX_F32>(noise, 8 * (int64_t)min(o + u * 64, o1 - 1), z[u]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8 * U; ++e) z[e / 8][e % 8] = 1.f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (o + u * 64 < o1) take(8 * (o + u * 64), x[u], y[u], z[u], std::integral_constant<int, 8>{});
+        }
+        if (const int at = 8 * o1 + lane; tail && at < a.vocab) {
+            float x[1] = {value_at<TYPE>(row, at)}, y[1] = {value_at<TYPE>(other, at)}, z[1] = {race ? noise[at] : 1.f};
+            take(at, x, y, z, std::integral_constant<int, 1>{});
+        }
+        return f;
+    }
+
+    // Segment number `segment` of row number `r` of a job, by one wave; three words
+    __device__ __forceinline__ void work(const Job& j, int r, int segment, uint64_t (&words)[3]) {
+        const int octets = a.vocab / 8, each = (octets + a.segments - 1) / a.segments;
+        const int o0 = min(segment * each, octets), o1 = min(o0 + each, octets);
+        const bool tail = segment == a.segments - 1;
+        Found f;
+        if (j.kind == kRows) {
+            const int node = __builtin_amdgcn_readfirstlane(s.row[drafted ? r >> 1 : r]);
+            const bool second = drafted && (r & 1);
+            const int first = child_from(node, node + 1);
+            if (second && first >= n) return;          // nobody looks at it
+            const bool race = !(cold || second || (drafted && first < n));
+            int excludes = 0;
+            if (race) {                                // the children do not take part: it counts when all were rejected
+                const int lo = 8 * o0, hi = tail ? a.vocab : 8 * o1;
+                for (int i = first; i < n; i = child_from(node, i + 1)) {
+                    const int x = __builtin_amdgcn_readlane(id, i - base);
+                    if (x < lo || x >= hi) continue;
+                    if (lane == 0 && excludes < kExcluded) s.excluded[wave][excludes] = x;
+                    ++excludes;
+                }
+            }
+            f = scan(second ? draft_of(node) : logits_of(node), o0, o1, tail, race, node, excludes);
+        } else {
+            f = residual(j, o0, o1, tail, j.kind == kRace);
+        }
+        f.join(heat);
+        words[0] = both(__float_as_uint(f.top), (uint32_t)f.top_at);
+        words[1] = __builtin_bit_cast(uint64_t, f.sum);
+        words[2] = both(__float_as_uint(f.best), (uint32_t)f.best_at);
+    }
+
+    // What the segments of a row found together, lane i holding segment i's words; by a whole wave
+    __device__ __forceinline__ void keep(int r, uint64_t x, uint64_t y, uint64_t z) {
+        Found f = kNothing;
+        if (lane < a.segments)
+            f = Found{__uint_as_float((uint32_t)x), (int)(x >> 32), __builtin_bit_cast(double, y), __uint_as_float((uint32_t)z), (int)(z >> 32)};
+        f.join(heat);
+        if (lane == 0) s.found[r] = f;
+    }
+
+    __device__ __forceinline__ void finish(int kept, int next) {
+        if (member != 0) return;
+        for (int64_t i = kept + threadIdx.x; i < a.width; i += kThreads) a.path[b * a.width + i] = -1;
+        if (threadIdx.x == 0) {
+            a.kept[b] = kept;
+            a.next[b] = next;
+        }
+    }
+
+    // After a job: walks on as far as what is known goes, and says what is wanted next; false: nothing, the walk has ended.  All threads of all
+    // members take the same way.
+    __device__ __forceinline__ bool decide(Job& j) {
+        int node = j.node, child = j.next_child;
+        bool leaf = false;
+        if (j.kind == kRace) {
+            const int best = s.found[0].best_at;
+            if (best < 0 && j.c >= 0.0) {                // nothing is left: from p itself
+                j.c = -1.0;
+                return true;
+            }
+            finish(j.kept, best);
+            return false;
+        }
+        if (j.kind == kSum) j.mass = s.found[0].sum;
+        int at = 0;
+        while (true) {
+            Found p{};
+            if (j.kind == kRows) {
+                p = s.found[at];
+                j.p_top = p.top;
+                j.p_sum = p.sum;
+                if (drafted) {
+                    j.q_top = s.found[at + 1].top;
+                    j.q_sum = s.found[at + 1].sum;
+                }
+                child = child_from(node, node + 1);
+                leaf = child >= n;
+                j.c = 0.0;
+                j.mass = drafted ? 1.0 : p.sum;          // without a draft both sides of the test are left as they are summed
+            }
+            const bool full = j.kept >= a.width;
+            int to = -1;
+            if (cold) {
+                for (int i = full ? n : child; i < n && to < 0; i = child_from(node, i + 1))
+                    if (__builtin_amdgcn_readlane(id, i - base) == p.top_at && p.top > -__builtin_inff()) to = i;
+                if (to < 0) {
+                    finish(j.kept, p.top > -__builtin_inff() ? p.top_at : -1);
+                    return false;
+                }
+            } else {
+                // p and q of the nodes' tokens are computed for 64 neighbours at once, a lane each
+                int known = -1;
+                double ps = 0.0, qs = 1.0;
+                for (int i = full ? n : child; i < n; i = child_from(node, i + 1)) {
+                    look_at(i & ~63);
+                    if (known != base) {
+                        known = base;
+                        const bool in = id >= 0 && id < a.vocab;
+                        ps = in && j.p_sum > 0.0 ? exp(((double)lp - (double)j.p_top) * heat.inv) : 0.0;
+                        if (drafted) ps = in && j.p_sum > 0.0 ? ps / j.p_sum : 0.0;
+                        if (drafted) qs = in && j.q_sum > 0.0 ? exp(((double)lq - (double)j.q_top) * heat.inv) / j.q_sum : 0.0;
+                    }
+                    const double drawn = lane_of(qs, i - base);
+                    double r = lane_of(ps, i - base);
+                    if (drafted) r = fmax(r - j.c * drawn, 0.0);
+                    else if (tried_before(node, i)) r = 0.0;
+                    if ((double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(uniform), i - base)) * j.mass * drawn < r) {
+                        to = i;
+                        break;
+                    }
+                    if (!drafted) {
+                        j.mass = fmax(j.mass - r, 0.0);
+                        continue;
+                    }
+                    j.c += j.mass;
+                    j.node = node;
+                    j.next_child = child_from(node, i + 1);
+                    j.kind = j.next_child < n ? kSum : kRace;
+                    return true;
+                }
+                if (to < 0) {
+                    if (j.kind == kRows && (leaf || (!drafted && !full && p.best_at >= 0))) {
+                        finish(j.kept, p.best_at);
+                        return false;
+                    }
+                    if (!(j.p_top > -__builtin_inff())) {
+                        finish(j.kept, -1);
+                        return false;
+                    }
+                    j.kind = kRace;                      // the path is full, or nothing but its children was left: from p itself
+                    j.node = node;
+                    j.c = -1.0;
+                    return true;
+                }
+            }
+            if (member == 0 && threadIdx.x == 0) a.path[b * a.width + j.kept] = to;
+            ++j.kept;
+            node = to;
+            at = j.kind == kRows ? row_of(node) : -1;
+            j.kind = kRows;
+            j.node = node;
+            if (at < 0) return true;
+        }
+    }
+};
+
+// A team of workgroups a request.  A job's rows are read in segments, each by a wave of its own; members hand in what their segments gave,
+// look out for the others' a bounded number of times, join all parts in the order of the segments and decide, every one for itself
+// and all alike, what the next job is.  A member that has looked in vain goes on alone and reads all segments itself, with the same
+// result: nobody has to wait for a workgroup that may not be running.  Member 0 writes the results.
+template <int TYPE>
+__global__ __launch_bounds__(kThreads, 3) void verify_kernel(VerifyArgs a) {
+    __shared__ Shared s;
+    Team<TYPE> team(a, s);
+    const int n = team.n, b = team.b, tid = threadIdx.x, lane = team.lane, wave = team.wave;
+    const bool shared = a.team > 1;
+    const uint64_t number = shared ? get(&a.control->number) : 0;
+    for (int i = tid; i < n; i += kThreads) {
+        s.parent[i] = i == 0 ? -1 : a.parents[team.t0 + i];
+        s.id[i] = a.ids[team.t0 + i];
+        s.uniform[i] = a.uniform[team.t0 + i];
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += kThreads) {
+        const int up = s.parent[i], x = s.id[i];
+        const bool in = up >= 0 && up < i && x >= 0 && x < a.vocab;
+        s.lp[i] = in ? value_at<TYPE>(team.logits_of(up), x) : 0.f;
+        s.lq[i] = in && a.draft != nullptr ? value_at<TYPE>(team.draft_of(up), x) : 0.f;
+    }
+    if (team.member == 0 && tid == 0 && n > 0) a.path[b * a.width] = 0;
+    __syncthreads();
+
+    Job job{};
+    job.kept = 1;
+    bool alone = !shared, more = n > 0;
+    uint64_t* posted = shared ? a.control->posted + b * a.team : nullptr;
+    uint64_t* parts = a.parts + (int64_t)b * 2 * a.slots * 3;
+    if (!more) team.finish(0, -1);
+    for (uint32_t jobs = 1; more; ++jobs) {
+        if (job.kind == kRows) team.list_rows(job.node, jobs == 1 && n <= a.wide);
+        const int rows = job.kind == kRows ? team.rows() : 1;
+        // together with the others first; alone, a row at a time, when they are not seen
+        for (int r = alone ? 0 : -1; r < rows; ++r) {
+            const bool mine = r >= 0;
+            uint64_t* to = parts + (jobs & 1 ? 0 : (int64_t)a.slots * 3);
+            __syncthreads();
+            for (int i = mine ? wave : team.member * kWaves + wave; i < (mine ? 1 : rows) * a.segments; i += mine ? kWaves : a.team * kWaves) {
+                uint64_t words[3] = {0, 0, 0};
+                team.work(job, mine ? r : i / a.segments, i % a.segments, words);
+                if (lane < 3) {
+                    const uint64_t word = lane == 0 ? words[0] : lane == 1 ? words[1] : words[2];
+                    if (mine) s.part[i][lane] = word;
+                    else put(to + (int64_t)i * 3 + lane, word);
+                }
+            }
+            if (mine) {
+                __syncthreads();
+                if (wave == 0) {
+                    const int at = min(lane, a.segments - 1);
+                    team.keep(r, s.part[at][0], s.part[at][1], s.part[at][2]);
+                }
+                continue;
+            }
+            stored();
+            __syncthreads();
+            const uint64_t want = number << 16 | jobs;
+            if (tid == 0) put(posted + team.member, want);
+            if (wave == 0) {
+                bool here = false;
+                for (int polls = 0; !here && polls < kMostPolls; ++polls)
+                    here = __ballot(lane < a.team && get(posted + min(lane, a.team - 1)) < want) == 0;
+                if (lane == 0) s.all_here = here;
+            } else if (wave == 3 && jobs == 1 && lane == 0) {
+                team_counts_in(a, b, number);
+            }
+            __syncthreads();
+            alone = s.all_here == 0;
+            if (alone) continue;
+            for (int x = wave; x < rows; x += kWaves) {
+                const uint64_t* from = to + ((int64_t)x * a.segments + min(lane, a.segments - 1)) * 3;
+                team.keep(x, get(from), get(from + 1), get(from + 2));
+            }
+            break;
+        }
+        __syncthreads();
+        more = team.decide(job);
+        __syncthreads();
+    }
+    if (shared && n == 0 && tid == 0) team_counts_in(a, b, number);
 }
 
-// A workgroup a request: it reads the rows of the nodes that the walk comes to, one after another.
-template <int TYPE>
-__global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a) {
-    __shared__ Shared s;
-    const int b = blockIdx.x, lane = threadIdx.x & 63;
-    const int64_t lo = a.q_start[b], hi = a.q_start[b + 1];
-    const int64_t t0 = lo < 0 ? 0 : lo > a.tokens ? a.tokens : lo, t1 = hi > a.tokens ? a.tokens : hi;
-    const int n = (int)min(max(t1 - t0, (int64_t)0), (int64_t)kNodes);
-    const float t = a.temperature[b];
-    const bool cold = !(t > 0.f);
-    const Heat heat(cold ? 1.f : t);
-    const float* noise = a.noise + b * a.ldn;
-    int64_t kept = n > 0;
-    int node = 0, next = -1;
-    if (threadIdx.x == 0 && n > 0) a.path[b * a.width] = 0;
-    while (n > 0) {
-        // the children, in the order of their numbers
-        int children = 0;
-        if (kept < a.width) {
-            __syncthreads();
-            for (int base = node + 1; base < n; base += 64) {
-                const int i = base + lane;
-                const bool is = i < n && a.parents[t0 + i] == node;
-                const uint64_t all = __ballot(is);
-                if (is && threadIdx.x < 64) {
-                    Child& c = s.child[children + __popcll(all & ((1ull << lane) - 1))];
-                    c.node = i;
-                    c.token = a.ids[t0 + i];
-                    c.uniform = a.uniform[t0 + i];
-                }
-                children += __popcll(all);
-            }
-            __syncthreads();
-        }
-        const void* row = row_at<TYPE>(a.logits, (t0 + node) * a.ldl);
-        const void* drafted = a.draft ? row_at<TYPE>(a.draft, (t0 + node) * a.ldd) : nullptr;
-        const bool with_q = drafted != nullptr && children > 0 && !cold;
-        const Found p = cold || with_q ? pass<TYPE, false>(a, row, noise, heat, 0, s) : pass<TYPE, true>(a, row, noise, heat, children, s);
-        Found q{};
-        if (with_q) q = pass<TYPE, false>(a, drafted, noise, heat, 0, s);
-        if (cold) {
-            int to = -1;
-            for (int k = 0; k < children && to < 0; ++k)
-                if (s.child[k].token == p.top_at && p.top > -__builtin_inff()) to = s.child[k].node;
-            if (to < 0) {
-                next = p.top == -__builtin_inff() ? -1 : p.top_at;
-                break;
-            }
-            node = to;
-        } else {
-            for (int k = threadIdx.x; k < children; k += kThreads) {
-                Child& c = s.child[k];
-                const bool in = c.token >= 0 && c.token < a.vocab;
-                bool before = !in;
-                for (int j = 0; j < k && !with_q; ++j) before |= s.child[j].token == c.token;
-                c.tried_before = before;
-                c.p = in && p.sum > 0 ? exp(((double)value_at<TYPE>(row, in ? c.token : 0) - (double)p.top) * heat.inv) / p.sum : 0.0;
-                c.q = !with_q ? 1.0 : in && q.sum > 0 ? exp(((double)value_at<TYPE>(drafted, in ? c.token : 0) - (double)q.top) * heat.inv) / q.sum : 0.0;
-            }
-            __syncthreads();
-            int to = -1;
-            double mass = 1.0, c = 0.0;
-            for (int k = 0; k < children; ++k) {
-                const Child& d = s.child[k];
-                const double r = with_q ? fmax(d.p - c * d.q, 0.0) : d.tried_before ? 0.0 : d.p;
-                if ((double)d.uniform * mass * d.q < r) {
-                    to = d.node;
-                    break;
-                }
-                if (!with_q) {
-                    mass = fmax(mass - r, 0.0);
-                } else {
-                    c += mass;
-                    if (k + 1 < children) mass = residual<TYPE, false>(a, row, p, drafted, q, c, noise, heat, s).sum;
-                }
-            }
-            if (to < 0) {
-                int best = p.best_at;
-                if (with_q) best = residual<TYPE, true>(a, row, p, drafted, q, c, noise, heat, s).best_at;
-                if (best < 0 && p.top > -__builtin_inff()) best = pass<TYPE, true>(a, row, noise, heat, 0, s).best_at;   // nothing is left: from p itself
-                next = best;
-                break;
-            }
-            node = to;
-        }
-        if (threadIdx.x == 0) a.path[b * a.width + kept] = node;
-        ++kept;
-    }
-    for (int64_t i = kept + threadIdx.x; i < a.width; i += kThreads) a.path[b * a.width + i] = -1;
-    if (threadIdx.x == 0) {
-        a.kept[b] = (int32_t)kept;
-        a.next[b] = next;
-    }
+struct Plan {
+    int team, segments, slots, wide, ahead;
+};
+
+Plan plan_of(int64_t tokens, int64_t requests, int64_t vocab, int rows_each) {
+    Plan p{};
+    if (requests < 1) requests = 1;
+    const int64_t nodes = ceil_div(tokens, requests);
+    auto clamp = [](int64_t v, int64_t lo, int64_t hi) { return (int)(v < lo ? lo : v > hi ? hi : v); };
+    p.wide = nodes <= 8 ? kMostRows : 1;
+    p.ahead = rows_each == 1 ? 4 : 2;
+    const int64_t rows = (p.wide > 1 ? nodes : 1 + (nodes - 1 < p.ahead ? nodes - 1 : p.ahead)) * rows_each;
+    const int most = requests > kMostTeams ? 1 : clamp(kMostMembers * 3 / 4 / requests, 1, 64);
+    const int64_t coarse = ceil_div(vocab, 2048), fine = ceil_div(vocab, 512), even = rows > 0 ? most * kWaves / rows : 1;
+    p.segments = clamp(even > fine ? fine : even > coarse ? even : coarse, 1, clamp(kMostParts / requests, 4, kMostSegments));
+    p.team = clamp(ceil_div(p.segments * rows, kWaves), 1, most);
+    p.slots = 2 * kMostRows * p.segments;
+    return p;
+}
+
+// Parts of a team's rows, twice (a member may be a job ahead of another); a team of one keeps them in LDS.
+size_t workspace_bytes(int64_t requests) {
+    constexpr size_t all = (size_t)kMostParts * 2 * kMostRows * 2 * 24;
+    return kControlBytes + (requests < 64 ? all / 64 * requests : all);
 }
 
 }  // namespace
@@ -320,7 +691,7 @@ using namespace mx;
 
 extern "C" size_t mx_verify_workspace_bytes(int64_t tokens, int64_t requests, int64_t vocab) {
     if (tokens < 0 || requests < 0 || vocab < 1 || requests > kCacheMaxRequests || tokens > INT32_MAX || vocab > MX_VERIFY_MAX_VOCAB) return 0;
-    return kCounterBytes;
+    return workspace_bytes(requests);
 }
 
 extern "C" mx_status mx_verify(const void* logits, const void* draft, int32_t type, int64_t tokens, int64_t vocab, int64_t ldl, int64_t ldd,
@@ -341,10 +712,19 @@ extern "C" mx_status mx_verify(const void* logits, const void* draft, int32_t ty
     }
     if (requests > kCacheMaxRequests || tokens > INT32_MAX || vocab > MX_VERIFY_MAX_VOCAB || path_width > INT32_MAX) return MX_ERR_UNSUPPORTED;
     if (requests == 0) return MX_OK;
-    VerifyArgs a{logits, draft, ids, parents, q_start, temperature, uniform, noise, path, kept, next, tokens, ldl, ldd, ldn, path_width,
-                 (int32_t)vocab, (int32_t)requests};
-    if (type == MX_F32) verify_kernel<MX_F32><<<(unsigned)requests, kThreads, 0, (hipStream_t)stream>>>(a);
-    else verify_kernel<MX_BF16><<<(unsigned)requests, kThreads, 0, (hipStream_t)stream>>>(a);
+    VerifyArgs a{};
+    a.logits = logits; a.draft = draft; a.ids = ids; a.parents = parents; a.q_start = q_start;
+    a.temperature = temperature; a.uniform = uniform; a.noise = noise;
+    a.path = path; a.kept = kept; a.next = next;
+    a.tokens = tokens; a.ldl = ldl; a.ldd = ldd; a.ldn = ldn; a.width = path_width;
+    a.vocab = (int32_t)vocab; a.requests = (int32_t)requests;
+    const Plan p = plan_of(tokens, requests, vocab, draft != nullptr ? 2 : 1);
+    a.team = p.team; a.segments = p.segments; a.slots = p.slots; a.wide = p.wide; a.ahead = p.ahead;
+    a.control = (Control*)workspace;
+    a.parts = (uint64_t*)((uint8_t*)workspace + kControlBytes);
+    const unsigned grid = (unsigned)(requests * p.team);
+    if (type == MX_F32) verify_kernel<MX_F32><<<grid, kThreads, 0, (hipStream_t)stream>>>(a);
+    else verify_kernel<MX_BF16><<<grid, kThreads, 0, (hipStream_t)stream>>>(a);
     MX_HIP_LAUNCH_CHECK();
     return MX_OK;
 }

@@ -670,7 +670,7 @@ def cache_tree_attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, q_s
 
 
 def verify_workspace(tokens: int, requests: int, vocab: int, device) -> torch.Tensor:
-    """A workspace for mx_verify with these or smaller numbers; its first 65536 bytes are zero."""
+    """A workspace for mx_verify with these or smaller numbers, ready for its first use."""
     space = torch.empty(max(1, mx_verify_workspace_bytes(tokens, requests, vocab)), dtype=torch.uint8, device=device)
     space[:65536].zero_()
     return space
