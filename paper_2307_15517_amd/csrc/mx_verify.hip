@@ -26,10 +26,9 @@ struct VerifyArgs {
     int64_t tokens, ldl, ldd, ldn, width;
     int32_t vocab, requests;
     struct Control* control;
-    uint64_t* parts;           // [request][2][slots][3]
+    uint64_t* parts;           // [request][2][kSlots][3]
     int32_t team;              // workgroups a request
-    int32_t segments;          // of a row
-    int32_t slots;
+    int32_t finest;            // segments of a row, at most
     int32_t wide;              // a request with so many nodes or fewer has the rows of all of them read at once
     int32_t ahead;             // else so many children's rows with a node's
 };
@@ -39,7 +38,7 @@ constexpr int kNodes = MX_TREE_MAX_NODES;
 constexpr int kMostRows = 16;              // nodes whose rows are read at once
 constexpr int kMostSegments = 64;          // of a row, a lane each where they are joined
 constexpr int kMostMembers = 1024, kMostTeams = 512;
-constexpr int kMostParts = 64 * kMostSegments;   // segments times teams
+constexpr int kSlots = 64 * kWaves + 2 * kMostRows;   // parts of a job: rows times segments, no more than the waves of a team or the rows
 constexpr int kExcluded = 16;
 constexpr int kMostPolls = 512;
 constexpr size_t kControlBytes = 65536;
@@ -171,6 +170,7 @@ static_assert(sizeof(Control) <= kControlBytes, "the workspace's first part");
 struct Shared {
     Found found[2 * kMostRows];
     int row[kMostRows];
+    Job job;                            // (not in registers: the walk's state is read between the passes only)
     uint64_t part[kMostSegments][3];    // of a row that a workgroup reads alone
     int excluded[kWaves][kExcluded];
     uint32_t all_here;
@@ -216,6 +216,7 @@ struct Team {
     int base, up, id;          // of node base + lane: parent, token, random number, its logits in its parent's rows
     float uniform, lp, lq;
     int nodes;                 // on the list of rows
+    int segments;              // of a row, in this job: as many as give every wave of the team one
 
     __device__ __forceinline__ Team(const VerifyArgs& args, Shared& shared)
         : a(args), s(shared), b(blockIdx.x / args.team), member(blockIdx.x % args.team), heat(1.f), lane(threadIdx.x & 63),
@@ -290,7 +291,7 @@ struct Team {
     // node's children that lie there.
     __device__ __forceinline__ Found scan(const void* row, int o0, int o1, bool tail, bool race, int node, int excludes) {
         Found f = kNothing;
-        constexpr int U = 4;                       // octets of a lane in flight
+        constexpr int U = 2;                       // octets of a lane at a time; the next ones are in flight
         // N elements from place `at` on: the largest is known to be no larger than f.top
         auto take = [&](int at, const float* x, float* z, auto count_c) __attribute__((always_inline)) {
             constexpr int N = decltype(count_c)::value;
@@ -326,43 +327,41 @@ struct Team {
             f.best *= less;
             f.top = top;
         };
-        for (int o = o0 + lane; o < o1; o += 64 * U) {
-            float x[U][8], z[U][8];
+        float x[U][8], z[U][8], next_x[U][8], next_z[U][8];
+        auto load = [&](int o) __attribute__((always_inline)) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) values8<TYPE>(row, 8 * (int64_t)min(o + u * 64, o1 - 1), x[u]);
+            for (int u = 0; u < U; ++u) values8<TYPE>(row, 8 * (int64_t)min(o + u * 64, o1 - 1), next_x[u]);
             if (race) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) values8<MX_F32>(noise, 8 * (int64_t)min(o + u * 64, o1 - 1), z[u]);
+                for (int u = 0; u < U; ++u) values8<MX_F32>(noise, 8 * (int64_t)min(o + u * 64, o1 - 1), next_z[u]);
             }
+        };
+        if (o0 < o1) load(o0 + lane);
+#pragma unroll 1
+        for (int o = o0; o < o1; o += 64 * U) {
+            const int mine = o + lane;
             float top = -__builtin_inff();
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[u][e] = o + u * 64 < o1 ? x[u][e] : -__builtin_inff();
+                    x[u][e] = mine + u * 64 < o1 ? next_x[u][e] : -__builtin_inff();
+                    if (race) z[u][e] = next_z[u][e];
                     top = __builtin_fmaxf(top, x[u][e]);
                 }
+            if (o + 64 * U < o1) load(mine + 64 * U);
             if (top > f.top) {
                 raise(top);
                 if (cold) {
 #pragma unroll
                     for (int e = 8 * U - 1; e >= 0; --e)
-                        if (x[e / 8][e % 8] == top) f.top_at = 8 * (o + e / 8 * 64) + e % 8;
+                        if (x[e / 8][e % 8] == top) f.top_at = 8 * (mine + e / 8 * 64) + e % 8;
                 }
             }
             if (!cold && f.top > -__builtin_inff()) {
-#pragma unroll 1
-                for (int u = 0; u < U; ++u) {      // (in a loop: the arithmetic is small next to the code it would be four times)
-                    if (o + u * 64 >= o1) break;
-                    take(8 * (o + u * 64), x[0], z[0], std::integral_constant<int, 8>{});
 #pragma unroll
-                    for (int v = 0; v + 1 < U; ++v)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            x[v][e] = x[v + 1][e];
-                            z[v][e] = z[v + 1][e];
-                        }
-                }
+                for (int u = 0; u < U; ++u)
+                    if (u == 0 || mine + u * 64 < o1) take(8 * (mine + u * 64), x[u], z[u], std::integral_constant<int, 8>{});
             }
         }
         if (const int at = 8 * o1 + lane; tail && at < a.vocab) {
@@ -377,12 +376,14 @@ struct Team {
     }
 
     // r = max(p - c q, 0) of a part of the rows: its sum, and with `race` the winner of r / noise
-    __device__ __forceinline__ Found residual(const Job& j, int o0, int o1, bool tail, bool race) {
+    __device__ __forceinline__ Found residual(int o0, int o1, bool tail, bool race) {
+        const Job& j = s.job;
+        const int node = __builtin_amdgcn_readfirstlane(j.node);
         const bool whole = j.c < 0.0;
-        const void* row = logits_of(j.node);
-        const void* other = whole ? row : draft_of(j.node);
+        const void* row = logits_of(node);
+        const void* other = whole ? row : draft_of(node);
         const float fp = (float)(1.0 / j.p_sum), fq = whole ? 0.f : (float)(j.c / j.q_sum);
-        const float q_top = whole ? j.p_top : j.q_top;
+        const float p_top = j.p_top, q_top = whole ? j.p_top : j.q_top;
         Found f{0.f, 0, 0.0, 0.f, -1};
         constexpr int U = 2;
         auto take = [&](int at, const float* x, const float* y, const float* z, auto count_c) __attribute__((always_inline)) {
@@ -390,7 +391,7 @@ struct Team {
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const float r = __builtin_fmaxf(__builtin_fmaf(heat.exp_of(x[e] - j.p_top), fp, -(heat.exp_of(y[e] - q_top) * fq)), 0.f);
+                const float r = __builtin_fmaxf(__builtin_fmaf(heat.exp_of(x[e] - p_top), fp, -(heat.exp_of(y[e] - q_top) * fq)), 0.f);
                 sum += r;
                 const float score = r * __builtin_amdgcn_rcpf(z[e]);
                 if (score > f.best) {
@@ -400,6 +401,7 @@ struct Team {
             }
             f.sum += sum;
         };
+#pragma unroll 1
         for (int o = o0 + lane; o < o1; o += 64 * U) {
             float x[U][8], y[U][8], z[U][8];
 #pragma unroll
@@ -427,12 +429,12 @@ struct Team {
     }
 
     // Segment number `segment` of row number `r` of a job, by one wave; three words
-    __device__ __forceinline__ void work(const Job& j, int r, int segment, uint64_t (&words)[3]) {
-        const int octets = a.vocab / 8, each = (octets + a.segments - 1) / a.segments;
+    __device__ __forceinline__ void work(int kind, int r, int segment, uint64_t (&words)[3]) {
+        const int octets = a.vocab / 8, each = (octets + segments - 1) / segments;
         const int o0 = min(segment * each, octets), o1 = min(o0 + each, octets);
-        const bool tail = segment == a.segments - 1;
+        const bool tail = segment == segments - 1;
         Found f;
-        if (j.kind == kRows) {
+        if (kind == kRows) {
             const int node = __builtin_amdgcn_readfirstlane(s.row[drafted ? r >> 1 : r]);
             const bool second = drafted && (r & 1);
             const int first = child_from(node, node + 1);
@@ -450,7 +452,7 @@ struct Team {
             }
             f = scan(second ? draft_of(node) : logits_of(node), o0, o1, tail, race, node, excludes);
         } else {
-            f = residual(j, o0, o1, tail, j.kind == kRace);
+            f = residual(o0, o1, tail, kind == kRace);
         }
         f.join(heat);
         words[0] = both(__float_as_uint(f.top), (uint32_t)f.top_at);
@@ -461,7 +463,7 @@ struct Team {
     // What the segments of a row found together, lane i holding segment i's words; by a whole wave
     __device__ __forceinline__ void keep(int r, uint64_t x, uint64_t y, uint64_t z) {
         Found f = kNothing;
-        if (lane < a.segments)
+        if (lane < segments)
             f = Found{__uint_as_float((uint32_t)x), (int)(x >> 32), __builtin_bit_cast(double, y), __uint_as_float((uint32_t)z), (int)(z >> 32)};
         f.join(heat);
         if (lane == 0) s.found[r] = f;
@@ -599,23 +601,28 @@ __global__ __launch_bounds__(kThreads, 3) void verify_kernel(VerifyArgs a) {
     if (team.member == 0 && tid == 0 && n > 0) a.path[b * a.width] = 0;
     __syncthreads();
 
-    Job job{};
-    job.kept = 1;
+    if (tid == 0) {
+        s.job = Job{};
+        s.job.kept = 1;
+    }
+    __syncthreads();
     bool alone = !shared, more = n > 0;
     uint64_t* posted = shared ? a.control->posted + b * a.team : nullptr;
-    uint64_t* parts = a.parts + (int64_t)b * 2 * a.slots * 3;
+    uint64_t* parts = a.parts + (int64_t)b * 2 * kSlots * 3;
     if (!more) team.finish(0, -1);
     for (uint32_t jobs = 1; more; ++jobs) {
-        if (job.kind == kRows) team.list_rows(job.node, jobs == 1 && n <= a.wide);
-        const int rows = job.kind == kRows ? team.rows() : 1;
+        const int kind = __builtin_amdgcn_readfirstlane(s.job.kind);
+        if (kind == kRows) team.list_rows(__builtin_amdgcn_readfirstlane(s.job.node), jobs == 1 && n <= a.wide);
+        const int rows = kind == kRows ? team.rows() : 1;
+        team.segments = min(max((shared ? a.team : 4) * kWaves / rows, 1), a.finest);
         // together with the others first; alone, a row at a time, when they are not seen
         for (int r = alone ? 0 : -1; r < rows; ++r) {
             const bool mine = r >= 0;
-            uint64_t* to = parts + (jobs & 1 ? 0 : (int64_t)a.slots * 3);
+            uint64_t* to = parts + (jobs & 1 ? 0 : (int64_t)kSlots * 3);
             __syncthreads();
-            for (int i = mine ? wave : team.member * kWaves + wave; i < (mine ? 1 : rows) * a.segments; i += mine ? kWaves : a.team * kWaves) {
+            for (int i = mine ? wave : team.member * kWaves + wave; i < (mine ? 1 : rows) * team.segments; i += mine ? kWaves : a.team * kWaves) {
                 uint64_t words[3] = {0, 0, 0};
-                team.work(job, mine ? r : i / a.segments, i % a.segments, words);
+                team.work(kind, mine ? r : i / team.segments, i % team.segments, words);
                 if (lane < 3) {
                     const uint64_t word = lane == 0 ? words[0] : lane == 1 ? words[1] : words[2];
                     if (mine) s.part[i][lane] = word;
@@ -625,7 +632,7 @@ __global__ __launch_bounds__(kThreads, 3) void verify_kernel(VerifyArgs a) {
             if (mine) {
                 __syncthreads();
                 if (wave == 0) {
-                    const int at = min(lane, a.segments - 1);
+                    const int at = min(lane, team.segments - 1);
                     team.keep(r, s.part[at][0], s.part[at][1], s.part[at][2]);
                 }
                 continue;
@@ -646,20 +653,23 @@ __global__ __launch_bounds__(kThreads, 3) void verify_kernel(VerifyArgs a) {
             alone = s.all_here == 0;
             if (alone) continue;
             for (int x = wave; x < rows; x += kWaves) {
-                const uint64_t* from = to + ((int64_t)x * a.segments + min(lane, a.segments - 1)) * 3;
+                const uint64_t* from = to + ((int64_t)x * team.segments + min(lane, team.segments - 1)) * 3;
                 team.keep(x, get(from), get(from + 1), get(from + 2));
             }
             break;
         }
         __syncthreads();
+        Job job = s.job;
         more = team.decide(job);
+        __syncthreads();
+        if (tid == 0) s.job = job;
         __syncthreads();
     }
     if (shared && n == 0 && tid == 0) team_counts_in(a, b, number);
 }
 
 struct Plan {
-    int team, segments, slots, wide, ahead;
+    int team, finest, wide, ahead;
 };
 
 Plan plan_of(int64_t tokens, int64_t requests, int64_t vocab, int rows_each) {
@@ -668,20 +678,17 @@ Plan plan_of(int64_t tokens, int64_t requests, int64_t vocab, int rows_each) {
     const int64_t nodes = ceil_div(tokens, requests);
     auto clamp = [](int64_t v, int64_t lo, int64_t hi) { return (int)(v < lo ? lo : v > hi ? hi : v); };
     p.wide = nodes <= 8 ? kMostRows : 1;
-    p.ahead = rows_each == 1 ? 4 : 2;
+    p.ahead = rows_each == 1 ? 2 : 1;
     const int64_t rows = (p.wide > 1 ? nodes : 1 + (nodes - 1 < p.ahead ? nodes - 1 : p.ahead)) * rows_each;
-    const int most = requests > kMostTeams ? 1 : clamp(kMostMembers * 3 / 4 / requests, 1, 64);
-    const int64_t coarse = ceil_div(vocab, 2048), fine = ceil_div(vocab, 512), even = rows > 0 ? most * kWaves / rows : 1;
-    p.segments = clamp(even > fine ? fine : even > coarse ? even : coarse, 1, clamp(kMostParts / requests, 4, kMostSegments));
-    p.team = clamp(ceil_div(p.segments * rows, kWaves), 1, most);
-    p.slots = 2 * kMostRows * p.segments;
+    p.finest = clamp(ceil_div(vocab, 512), 1, kMostSegments);
+    p.team = requests > kMostTeams ? 1 : clamp(ceil_div(p.finest * rows, kWaves), 1, clamp(kMostMembers * 3 / 4 / requests, 1, 64));
     return p;
 }
 
 // Parts of a team's rows, twice (a member may be a job ahead of another); a team of one keeps them in LDS.
 size_t workspace_bytes(int64_t requests) {
-    constexpr size_t all = (size_t)kMostParts * 2 * kMostRows * 2 * 24;
-    return kControlBytes + (requests < 64 ? all / 64 * requests : all);
+    const int64_t teams = requests < kMostTeams ? requests : kMostTeams;
+    return kControlBytes + (size_t)teams * 2 * kSlots * 24;
 }
 
 }  // namespace
@@ -719,7 +726,7 @@ extern "C" mx_status mx_verify(const void* logits, const void* draft, int32_t ty
     a.tokens = tokens; a.ldl = ldl; a.ldd = ldd; a.ldn = ldn; a.width = path_width;
     a.vocab = (int32_t)vocab; a.requests = (int32_t)requests;
     const Plan p = plan_of(tokens, requests, vocab, draft != nullptr ? 2 : 1);
-    a.team = p.team; a.segments = p.segments; a.slots = p.slots; a.wide = p.wide; a.ahead = p.ahead;
+    a.team = p.team; a.finest = p.finest; a.wide = p.wide; a.ahead = p.ahead;
     a.control = (Control*)workspace;
     a.parts = (uint64_t*)((uint8_t*)workspace + kControlBytes);
     const unsigned grid = (unsigned)(requests * p.team);
