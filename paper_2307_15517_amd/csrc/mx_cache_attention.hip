@@ -52,6 +52,8 @@ struct CacheAttnArgs {
     uint32_t flip;             // sign bit of the scale: carried by q
     const uint32_t* masks;     // kTree: [tokens][mask_words], bit j: new token j of the request is seen
     int32_t mask_words;        // 32-bit words of a token's mask
+    int32_t slots;             // cache_tree_kernel: its workgroups; tiles: units, at most
+    int32_t small_rows, small_run;   // rows that a small tile may have; its runs in eighths of a large one's
 };
 
 // One request as a workgroup sees it, every length bounded by what the arrays hold.
@@ -637,6 +639,7 @@ __global__ __launch_bounds__(256, 2) void cache_decode_kernel(CacheAttnArgs a) {
 // instructions leave the last quarter out (3 prompts of 1000 tokens, 8 heads x 4 of 96: 57.8 us with 128, 50.7 with 96; MXInt
 // 68.5 and 61.5).
 constexpr int kTileRows = 128, kTileKeys = 64;
+constexpr float kLag = 8.f;            // the maximum that probabilities are taken against follows the rows' own within this power of two
 
 // The request that tile number `tile` belongs to, and which of its tiles of rows it is; b < 0: none.  Every wave looks for itself, 64
 // requests at a time.
@@ -679,7 +682,6 @@ __device__ __forceinline__ int64_t part_row_of(const CacheAttnArgs& a, int h, co
 
 // The keys of the request that some row of the tile sees, and the splits that they are given: as many as there are runs of them.
 __device__ __forceinline__ int keys_seen(const CacheAttnArgs& a, const Tile& t) {
-    if (kTree) return t.rq.len;
     return max(0, t.rq.len - t.rq.n + min(t.index * kTileRows + kTileRows - 1, t.rq.n * a.group - 1) / a.group + 1);
 }
 __device__ __forceinline__ int splits_of(const CacheAttnArgs& a, int keys) {
@@ -727,10 +729,9 @@ __device__ __forceinline__ void pin(uint32_t x) { asm volatile("" ::"v"(x)); }
 // a register of its own, one for every place in every stage.
 __device__ __forceinline__ void opaque(uint32_t& x) { asm("" : "+v"(x)); }
 
-constexpr float kLag = 8.f;            // the maximum that probabilities are taken against follows the rows' own within this power of two
-
+// The arithmetic of one item: row tile `tile` for head h, keys begin .. stop, which are run `split` of `splits`.
 template <int TYPE, int DT, int BLOCK, int DC>
-__device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t* smem) {
+__device__ __forceinline__ void chunk_tile(const CacheAttnArgs& a, const Tile& tile, int h, int split, int splits, int begin, int stop, uint8_t* smem) {
     constexpr int QP = kQueryPieces<TYPE>, P = TYPE == MX_F32 ? 3 : 2;
     constexpr int NK = DC / 16, ND = DC / 32;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
@@ -740,38 +741,18 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int i = lane & 31, h2 = lane >> 5;
 
-    // Workgroup u runs on XCD u % 8: with a multiple of eight heads an XCD takes whole heads, so that its L2 holds few of them.
-    // The tiles with the most keys go first.
-    const int per_head = a.tiles * a.splits;
-    int h, rest;
-    if (a.heads % 8 == 0) {
-        const int j = index / 8;
-        h = index % 8 + 8 * (j / per_head);
-        rest = j % per_head;
-    } else {
-        h = index % a.heads;
-        rest = index / a.heads;
-    }
-    const int split = rest % a.splits, tile_id = a.tiles - 1 - rest / a.splits;
-    const Tile tile = find_tile(a, tile_id);
-    if (tile.b < 0) return;
     const int b = tile.b;
     PageWindow pages(a, b);
     const Request rq = tile.rq;
     const int rows = rq.n * a.group, r0 = tile.index * kTileRows;
     const int len = rq.len, dim = a.dim;
 
-    // the keys that some row of the tile sees, and this split's run of them in whole tiles
-    const int all = keys_seen(a, tile), splits = splits_of(a, all);
-    if (split >= splits) return;
-    const int per = (((all + kTileKeys - 1) / kTileKeys) + splits - 1) / splits * kTileKeys;
-    const int begin = min(split * per, all), stop = min(begin + per, all);
-
     // this wave's rows: q is the right operand of the scores, lane (i, h2) row i, elements 16kk + 8h2 ..
     const int r = min(r0 + 32 * wave + i, rows - 1);
     const int tok = r / a.group, head = h * a.group + (r - tok * a.group);
     const int last = min(kTree ? len - 1 : len - rq.n + tok, stop - 1);   // the last key of this split that the row sees
-    const int all_see = min(kTree ? len - rq.n - 1 : len - rq.n + min(r0 + 32 * wave, rows - 1) / a.group, stop - 1);   // the last one all of the wave's see
+    // the last one all of the wave's see
+    const int all_see = min(kTree ? len - rq.n - 1 : len - rq.n + min(r0 + 32 * wave, rows - 1) / a.group, stop - 1);
     v4u qf[QP][NK];
     load_q<TYPE, QP, NK>(a, (int64_t)(rq.t0 + tok) * a.ldq + (int64_t)head * dim, [&](int n) { return 16 * n + 8 * h2; }, qf);
 
@@ -1062,7 +1043,13 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
         const float ll = __uint_as_float(both[0]) + __uint_as_float(both[1]);
         const float inv = splits > 1 ? 1.f : ll > 0.f ? 1.f / ll : 0.f;
         const int64_t prow = part_row_of(a, h, rq, r) * a.splits + split;
-        if (splits > 1 && h2 == 0) a.part_ml[prow] = make_float2(m, ll);
+        const int64_t part0 = part_row_of(a, h, rq, r0) * a.splits;
+        const int tile_rows = min(kTileRows, rows - r0), at = (32 * wave + i) * a.splits + split;
+        const BufRsrc ro = make_rsrc(a.part_o + part0 * dim, (uint32_t)(tile_rows * a.splits * dim * 4));
+        if (splits > 1 && h2 == 0) {
+            if (kTree && a.join) __builtin_amdgcn_raw_buffer_store_b64(v2u{__float_as_uint(m), __float_as_uint(ll)}, make_rsrc(a.part_ml + part0, (uint32_t)(tile_rows * a.splits * 8)), at * 8, 0, kDeviceScope);
+            else a.part_ml[prow] = make_float2(m, ll);
+        }
         const int64_t to = (int64_t)(rq.t0 + tok) * a.ldo + (int64_t)head * dim;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt)
@@ -1074,12 +1061,543 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
                 for (int e = 0; e < 4; ++e) x[e] = o[dt][4 * q4 + e] * inv;
                 if (d < dim) {
                     if (splits == 1) store_out<TYPE, 4>(a, to + d, x);
+                    else if (kTree && a.join) __builtin_amdgcn_raw_buffer_store_b128(v4u{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])}, ro, (at * dim + d) * 4, 0, kDeviceScope);
                     else *reinterpret_cast<float4*>(a.part_o + prow * dim + d) = make_float4(x[0], x[1], x[2], x[3]);
                 }
             }
     }
 }
 
+#if !MX_CACHE_TREE
+template <int TYPE, int DT, int BLOCK, int DC>
+__device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t* smem) {
+    // Workgroup u runs on XCD u % 8: with a multiple of eight heads an XCD takes whole heads, so that its L2 holds few of them.
+    // The tiles with the most keys go first.
+    const int per_head = a.tiles * a.splits;
+    int h, rest;
+    if (a.heads % 8 == 0) {
+        const int j = index / 8;
+        h = index % 8 + 8 * (j / per_head);
+        rest = j % per_head;
+    } else {
+        h = index % a.heads;
+        rest = index / a.heads;
+    }
+    const int split = rest % a.splits, tile_id = a.tiles - 1 - rest / a.splits;
+    const Tile tile = find_tile(a, tile_id);
+    if (tile.b < 0) return;
+    // the keys that some row of the tile sees, and this split's run of them in whole tiles
+    const int all = keys_seen(a, tile), splits = splits_of(a, all);
+    if (split >= splits) return;
+    const int per = (((all + kTileKeys - 1) / kTileKeys) + splits - 1) / splits * kTileKeys;
+    const int begin = min(split * per, all);
+    chunk_tile<TYPE, DT, BLOCK, DC>(a, tile, h, split, splits, begin, min(begin + per, all), smem);
+}
+#else
+// ---- trees of more than sixteen rows --------------------------------------------------------------------
+// A workgroup takes a tile of up to 64 rows (32 of fp32 calls) of one request and key/value head; its four waves take blocks of 32 keys in
+// turn, as in decode(), and join at the end.  K and V go from memory to registers once for all rows of the tile, R groups of sixteen: an
+// MXInt block is converted once for them, and q, which all waves use, lies in LDS as the matrix instructions read it.  A block's K
+// registers are free for the next block's loads when its scores are there, V's after P V, so both are in flight during the rest.
+template <int TYPE>
+constexpr int kTreeGroups = TYPE == MX_F32 ? 2 : 4;
+
+// How a batch is shared out.  A unit is a tile of a request's rows and a key/value head; its keys are cut into runs of as few blocks of 64 as
+// leave no more items (a unit's runs) than workgroups.  A block of a large tile takes longer (3.6 us with an MXInt cache, 2.5 with
+// bfloat16; of a small one 2.1), so small tiles have runs of half as many again.  All know all lengths: there are no items without
+// work.  Every wave works it out for itself, a request a lane, 64 at a time.
+struct TreeItem {
+    Tile tile;                 // b < 0: nothing; index: of kTileRows rows
+    bool small;                // no more than a.small_rows of them
+    int h, split, splits;
+    int unit;                  // number of (tile, head)
+};
+
+__device__ __forceinline__ int over_wave(int v, bool largest) {
+#pragma unroll
+    for (int step = 0; step < 6; ++step) {
+        int o[2] = {v, v};
+        if (step == 0) o[1] = __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, true);
+        else if (step == 1) o[1] = __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true);
+        else if (step == 2) o[1] = __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true);
+        else if (step == 3) o[1] = __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true);
+        else {
+            const auto r = step == 4 ? __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false)
+                                     : __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+            o[0] = (int)r[0];
+            o[1] = (int)r[1];
+        }
+        v = largest ? max(o[0], o[1]) : o[0] + o[1];
+    }
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+struct TreePlan {
+    const CacheAttnArgs& a;
+    int lane, b0, index;       // requests b0 .. b0 + 63 are the lanes', each its `index`
+    Request rq;
+    int large, small, blocks;
+    int run;
+
+    __device__ __forceinline__ void look_at(int b) {
+        if (b == b0) return;
+        b0 = b;
+        rq = Request{0, 0, 0};
+        if (b + lane < a.requests) rq = request_of(a, b + lane);
+        const int rows = rq.n * a.group, rest = rows % kTileRows;
+        large = rows / kTileRows + (rest > a.small_rows);
+        small = rest > 0 && rest <= a.small_rows;
+        blocks = max(1, (rq.len + kTileKeys - 1) / kTileKeys);
+        index = b + lane;
+        if (a.sorted) {                                // the longest first: 64 requests at most
+            int rank = 0;
+            for (int j = 0; j < a.requests; ++j) {
+                const int other = __builtin_amdgcn_readlane(blocks, j);
+                rank += other > blocks || (other == blocks && j < lane);
+            }
+            index = __builtin_amdgcn_ds_permute((lane < a.requests ? rank : lane) * 4, lane);
+            rq = Request{__shfl(rq.t0, index), __shfl(rq.n, index), __shfl(rq.len, index)};
+            large = __shfl(large, index);
+            small = __shfl(small, index);
+            blocks = __shfl(blocks, index);
+        }
+    }
+    // How many runs of about `of` blocks the request's keys are cut into: any number will do that all agree on
+    __device__ __forceinline__ int runs(int of) const {
+        return min(max((int)((float)blocks * __builtin_amdgcn_rcpf((float)of) + 0.9999f), 1), a.splits);
+    }
+    // n / d: of small numbers the reciprocal is off by one at most
+    static __device__ __forceinline__ int over(int n, int d) {
+        if (n >= 1 << 21) return n / d;
+        int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d));
+        const int r = n - q * d;
+        q += r >= d ? 1 : r < 0 ? -1 : 0;
+        return q;
+    }
+    __device__ __forceinline__ int small_run() const { return max(run, run / 8 * a.small_run + run % 8 * a.small_run / 8); }
+
+    __device__ __forceinline__ explicit TreePlan(const CacheAttnArgs& args) : a(args), lane(threadIdx.x & 63), b0(-1), run(INT_MAX / 4) {
+        look_at(0);
+        if (a.splits <= 1) return;                     // one run a unit
+        float all = 0.f;
+        int most = 1, units = 0;
+        for (int base = 0; base < a.requests; base += 64) {
+            look_at(base);
+            const float v = (large + 8.f / (float)a.small_run * small) * blocks;
+            all += (float)over_wave((int)fminf(v, 1e7f), false);
+            most = max(most, over_wave(blocks, true));
+            units += over_wave(large + small, false);
+        }
+        // a unit's last run is half empty on average: a little less than fits is the first guess, then a sixteenth more at a time until the items
+        // are few enough, as they are with one run a unit
+        const float left = (float)a.slots - 0.45f * (float)a.heads * (float)units;
+        run = max(a.run, (int)fminf(all * (float)a.heads / fmaxf(left, 1.f), (float)most));
+        while (true) {
+            const int of_small = small_run();
+            int64_t items = 0;
+            for (int base = 0; base < a.requests; base += 64) {
+                look_at(base);
+                items += over_wave(large * runs(run) + small * runs(of_small), false);
+            }
+            if (items * a.heads <= a.slots || run >= most) break;
+            run += max(1, run >> 4);
+        }
+    }
+    // Item number `item`, or (UNIT) the first of unit number `item`
+    template <bool UNIT>
+    __device__ __forceinline__ TreeItem find(int item) {
+        int before = 0, units = 0;
+        for (int base = 0; base < a.requests; base += 64) {
+            look_at(base);
+            const int of_large = runs(run), of_small = runs(small_run());
+            const int count = (large * of_large + small * of_small) * a.heads, many = (large + small) * a.heads;
+            int upto = count, units_to = many;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int o = __shfl_up(upto, d, 64), u = __shfl_up(units_to, d, 64);
+                upto += lane >= d ? o : 0;
+                units_to += lane >= d ? u : 0;
+            }
+            const uint64_t past = __ballot(UNIT ? units + units_to > item : before + upto > item);
+            if (past != 0) {
+                const int at = __builtin_ctzll(past);
+                auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
+                const int n_large = of(large), s_large = of(of_large), s_small = of(of_small), first = units + of(units_to) - of(many);
+                const Request r{of(rq.t0), of(rq.n), of(rq.len)};
+                int h, tile, split;
+                bool is_small;
+                if constexpr (UNIT) {
+                    tile = over(item - first, a.heads);
+                    h = item - first - tile * a.heads;
+                    is_small = tile == n_large;
+                    split = 0;
+                } else {
+                    // Workgroup u runs on XCD u % 8: with a multiple of eight heads an XCD takes whole heads, so that its L2 holds few of them; the
+                    // tiles that read the same keys follow one another.
+                    const int rest = item - before - (of(upto) - of(count)), each = n_large * s_large + (of(small) ? s_small : 0);
+                    int y;
+                    if (a.heads % 8 == 0) {
+                        y = rest >> 3;
+                        const int eighth = over(y, each);
+                        h = (rest & 7) + 8 * eighth;
+                        y -= eighth * each;
+                    } else {
+                        y = over(rest, a.heads);
+                        h = rest - y * a.heads;
+                    }
+                    is_small = y >= n_large * s_large;
+                    split = is_small ? y - n_large * s_large : over(y, n_large);
+                    tile = is_small ? n_large : y - split * n_large;
+                }
+                const int unit = first + tile * a.heads + h;
+                if (unit >= a.tiles) break;            // (only where requests' tokens overlap)
+                return TreeItem{Tile{of(index), tile, r}, is_small, h, split, is_small ? s_small : s_large, unit};
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
+            units += __builtin_amdgcn_readlane(units_to, 63);
+        }
+        return TreeItem{Tile{-1, 0, Request{0, 0, 0}}, false, 0, 0, 0, 0};
+    }
+};
+
+// join_parts() for 8 U rows: eight groups of 32 lanes, a group U of the rows, S splits' parts of all of them in flight.
+template <int TYPE, int U, int S, int SCOPE>
+__device__ __forceinline__ void join_tile(const CacheAttnArgs& a, const Request& rq, int h, int r0, int rows, int splits) {
+    const int64_t part0 = part_row_of(a, h, rq, r0) * a.splits;
+    const BufRsrc ro = make_rsrc(a.part_o + part0 * a.dim, (uint32_t)(rows * a.splits * a.dim * 4));
+    const BufRsrc rm = make_rsrc(a.part_ml + part0, (uint32_t)(rows * a.splits * 8));
+    const int group = threadIdx.x >> 5, lane = threadIdx.x & 31, d = 4 * lane < a.dim ? 4 * lane : 0;
+    float x[U][4], m[U], l[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        m[u] = -__builtin_inff();
+        l[u] = x[u][0] = x[u][1] = x[u][2] = x[u][3] = 0.f;
+    }
+    for (int s0 = 0; s0 < splits; s0 += S) {
+        v4u y[U][S];
+        float2 ml[U][S];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                const int at = min(group + 8 * u, rows - 1) * a.splits + min(s0 + s, splits - 1);
+                const auto t = __builtin_amdgcn_raw_buffer_load_b64(rm, at * 8, 0, SCOPE);
+                ml[u][s] = make_float2(__uint_as_float(t[0]), __uint_as_float(t[1]));
+                y[u][s] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(ro, (at * a.dim + d) * 4, 0, SCOPE));
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+                if (s0 + s >= splits || ml[u][s].x == -__builtin_inff()) continue;      // a run that the row saw nothing of
+                const float top = __builtin_fmaxf(m[u], ml[u][s].x), f = exp2_of(m[u] - top), w = exp2_of(ml[u][s].x - top);
+                m[u] = top;
+                l[u] = l[u] * f + ml[u][s].y * w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[u][e] = x[u][e] * f + __uint_as_float(y[u][s][e]) * w;
+            }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (group + 8 * u >= rows || 4 * lane >= a.dim) continue;
+        const float inv = l[u] > 0.f ? 1.f / l[u] : 0.f;
+        const float o[4] = {x[u][0] * inv, x[u][1] * inv, x[u][2] * inv, x[u][3] * inv};
+        const int row = r0 + group + 8 * u, tok = row / a.group, head = h * a.group + (row - tok * a.group);
+        store_out<TYPE, 4>(a, (int64_t)(rq.t0 + tok) * a.ldo + (int64_t)head * a.dim + d, o);
+    }
+}
+
+template <int TYPE, int DT, int BLOCK, int R>
+__device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Tile& tile, int h, int split, int splits, int begin, int end, uint8_t* smem) {
+    constexpr int NS = DT / 32, NJ = DT / 16, VE = DT / 16;
+    constexpr int EB = BLOCK == 0 ? 2 : 1;
+    constexpr int QP = kQueryPieces<TYPE>, P = TYPE == MX_F32 ? 3 : 2;
+    using Block = KeyBlock<DT, BLOCK>;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int n = lane & 15, g = lane >> 4;
+    const Request rq = tile.rq;
+    PageWindow pages(a, tile.b);
+    const int rows = rq.n * a.group, r0 = tile.index * kTileRows, len = rq.len, dim = a.dim, base = len - rq.n;
+    pages.set_length(a, len);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)smem + lane * 16;
+
+    auto row_at = [&](int r, int i) { return min(r0 + 16 * r + i, rows - 1); };        // rows past the last repeat it
+    Block f;
+    int64_t at[2];
+    const int last_run = (len - 1) & ~15;
+    auto load_k = [&](int kb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            at[t] = pages.row(a, h, min(kb + 16 * t, last_run));
+            const uint8_t* kp = a.k + at[t] * dim * EB;
+            if constexpr (BLOCK == 0) {
+#pragma unroll
+                for (int s = 0; s < NS; ++s) {
+                    const int d = 32 * s + 8 * g;
+                    f.k[t][s] = *reinterpret_cast<const v4u*>(kp + (n * dim + (d < dim ? d : 0)) * 2);
+                }
+            } else {
+                const uint8_t* kx = a.k_exps + at[t] * (dim / BLOCK);
+#pragma unroll
+                for (int s = 0; s < Block::KC; ++s) {
+                    const int d = 64 * s + 16 * g, e = d < dim ? d : 0;
+                    f.k[t][s] = *reinterpret_cast<const v4u*>(kp + n * dim + e);
+                    f.ke[t][s] = kx[n * (dim / BLOCK) + e / BLOCK];
+                }
+            }
+        }
+    };
+    auto load_v = [&]() __attribute__((always_inline)) {
+        const int d = VE * n < dim ? VE * n : 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint8_t* src = a.v + at[t] * dim * EB + ((4 * g + i) * dim + d) * EB;
+                if constexpr (VE * EB == 16) {
+                    const v4u x = *reinterpret_cast<const v4u*>(src);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) f.v[4 * t + i][w] = x[w];
+                } else if constexpr (VE * EB == 8) {
+                    const v2u x = *reinterpret_cast<const v2u*>(src);
+                    f.v[4 * t + i][0] = x[0];
+                    f.v[4 * t + i][1] = x[1];
+                } else {
+                    f.v[4 * t + i][0] = *reinterpret_cast<const uint32_t*>(src);
+                }
+                if constexpr (BLOCK != 0) f.ve[4 * t + i] = (a.v_exps + at[t] * (dim / BLOCK))[(4 * g + i) * (dim / BLOCK) + d / BLOCK];
+            }
+    };
+    int kb = begin + 32 * wave;
+    if (kb < end) {
+        load_k(kb);
+        load_v();
+    }
+    for (int r = wave; r < R; r += 4) {
+        const int row = row_at(r, n), tok = row / a.group, head = h * a.group + (row - tok * a.group);
+        v4u qf[QP][NS];
+        load_q<TYPE, QP, NS>(a, (int64_t)(rq.t0 + tok) * a.ldq + (int64_t)head * dim,
+                             [&](int x) { return BLOCK == 0 ? 32 * x + 8 * g : 64 * (x >> 1) + 16 * g + 8 * (x & 1); }, qf);
+#pragma unroll
+        for (int p = 0; p < QP; ++p)
+#pragma unroll
+            for (int x = 0; x < NS; ++x) lds_write(lds0 + ((r * NS + x) * QP + p) * 1024, qf[p][x]);
+    }
+    __syncthreads();
+
+    float m[R], l[R];
+    v4f o[R][NJ];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        m[r] = -__builtin_inff();
+        l[r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) o[r][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+    for (; kb < end; kb += 128) {
+        v4f s[R][2];
+#pragma unroll
+        for (int r = 0; r < R; ++r) s[r][0] = s[r][1] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < NS; ++x) {
+            v4u kf[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if constexpr (BLOCK == 0) {
+                    kf[t] = f.k[t][x];
+                } else {
+                    const float sc = power2(f.ke[t][x >> 1] - a.exp_shift);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        int y = (int)f.k[t][x >> 1][2 * (x & 1) + (w >> 1)];
+                        asm("" : "+v"(y));            // the bytes are taken apart here, not when they arrive (four registers for one)
+                        const float lo = (float)(int8_t)(y >> (16 * (w & 1))) * sc, hi = (float)(int8_t)(y >> (16 * (w & 1) + 8)) * sc;
+                        kf[t][w] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+                    }
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int p = QP - 1; p >= 0; --p) {
+                    const v4u qf = lds_read(lds0 + ((r * NS + x) * QP + p) * 1024);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        s[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, kf[t]), __builtin_bit_cast(v8bf, qf), s[r][t], 0, 0, 0);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        load_k(kb + 128);                              // (past the end: the last run again, unused)
+        // V of this block is at the rows before
+        v4u pf[R][P];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (kb + 31 >= base || kb + 31 >= end) {
+                const int tok = row_at(r, n) / a.group, seen = end - 1 - kb - 4 * g;
+                const uint32_t bits = seen_from(a, rq.t0 + tok, kb - base) >> (4 * g);
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[r][t][e] = 16 * t + e <= seen && (bits >> (16 * t + e) & 1) ? s[r][t][e] : -__builtin_inff();
+            }
+            float top = max_of(s[r][0][0], s[r][0][1], s[r][0][2]);
+            top = max_of(top, s[r][0][3], s[r][1][0]);
+            top = max_of(top, s[r][1][1], s[r][1][2]);
+            top = max_across_16_32(max_of(top, s[r][1][3])) * a.c;
+            // the sums are kept against a maximum that follows the rows' own within 2^8
+            if (__any(top > m[r] + kLag)) {
+                const float m_new = __builtin_fmaxf(m[r], top);
+                const float alpha = m_new == -__builtin_inff() ? 1.f : exp2_of(m[r] - m_new);
+                m[r] = m_new;
+                l[r] *= alpha;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) o[r][j] *= alpha;
+            }
+            const float m_use = m[r] == -__builtin_inff() ? 0.f : m[r];
+            float sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float p0 = exp2_of(__builtin_fmaf(s[r][w >> 1][2 * (w & 1)], a.c, -m_use));
+                const float p1 = exp2_of(__builtin_fmaf(s[r][w >> 1][2 * (w & 1) + 1], a.c, -m_use));
+                sum += p0 + p1;
+                uint32_t y[P];
+                pieces_of<P>(p0, p1, y);
+#pragma unroll
+                for (int p = 0; p < P; ++p) pf[r][p][w] = y[p];
+            }
+            l[r] += sum;
+        }
+        // what lies past the request's end may be anything, NaN among it: it counts as zeros
+        const bool whole = kb + 32 <= len;
+        float sc[8];
+        if constexpr (BLOCK != 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool in = whole || kb + 16 * (i >> 2) + 4 * g + (i & 3) < len;
+                sc[i] = in ? power2(f.ve[i] - a.exp_shift) : 0.f;
+            }
+        } else if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool in = kb + 16 * (i >> 2) + 4 * g + (i & 3) < len;
+#pragma unroll
+                for (int w = 0; w < VE / 2; ++w) f.v[i][w] = in ? f.v[i][w] : 0u;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            v4u vf;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                if constexpr (BLOCK == 0) {
+                    vf[w] = __builtin_amdgcn_perm(f.v[2 * w + 1][j >> 1], f.v[2 * w][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
+                } else {
+                    int x = (int)f.v[2 * w][j >> 2], y = (int)f.v[2 * w + 1][j >> 2];
+                    asm("" : "+v"(x), "+v"(y));
+                    const float lo = (float)(int8_t)(x >> (8 * (j & 3))) * sc[2 * w];
+                    const float hi = (float)(int8_t)(y >> (8 * (j & 3))) * sc[2 * w + 1];
+                    vf[w] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int p = P - 1; p >= 0; --p)
+                    o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, vf), __builtin_bit_cast(v8bf, pf[r][p]), o[r][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        load_v();
+    }
+
+    // the four waves join, sixteen rows at a time: lane (n, g) holds row n, elements VE*(4g + e) + j
+    DecodeLds<DT>& lds = *reinterpret_cast<DecodeLds<DT>*>(smem);
+    const int tile_rows = min(16 * R, rows - r0);
+    const int64_t part0 = part_row_of(a, h, rq, r0);
+    const BufRsrc ro = make_rsrc(a.part_o + part0 * a.splits * dim, (uint32_t)(tile_rows * a.splits * dim * 4));
+    const BufRsrc rm = make_rsrc(a.part_ml + part0 * a.splits, (uint32_t)(tile_rows * a.splits * 8));
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        l[r] = sum_across_16_32(l[r]);
+        __syncthreads();                                                  // q, or the rows before, have been read
+        if (g == 0) lds.ml[wave][n] = make_float2(m[r], l[r]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) lds.o[wave][n][VE * (4 * g + e) + j] = o[r][j][e];
+        __syncthreads();
+        const int i = threadIdx.x >> 4, part = threadIdx.x & 15, row = r0 + 16 * r + i;
+        if (row < rows && VE * part < dim) {
+            float mm = -__builtin_inff();
+#pragma unroll
+            for (int w = 0; w < 4; ++w) mm = __builtin_fmaxf(mm, lds.ml[w][i].x);
+            float ll = 0.f, acc[VE];
+#pragma unroll
+            for (int j = 0; j < VE; ++j) acc[j] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float2 ml = lds.ml[w][i];
+                const float c = ml.x == -__builtin_inff() ? 0.f : exp2_of(ml.x - mm);
+                ll += ml.y * c;
+#pragma unroll
+                for (int j = 0; j < VE; ++j) acc[j] += lds.o[w][i][VE * part + j] * c;
+            }
+            if (splits == 1) {
+                const int tok = row / a.group, head = h * a.group + (row - tok * a.group);
+                const float inv = ll > 0.f ? 1.f / ll : 0.f;
+#pragma unroll
+                for (int j = 0; j < VE; ++j) acc[j] *= inv;
+                store_out<TYPE, VE>(a, (int64_t)(rq.t0 + tok) * a.ldo + (int64_t)head * dim + VE * part, acc);
+            } else {
+                // written through for the workgroup that joins them in this launch; a launch of its own finds them in any case
+                const int to = (16 * r + i) * a.splits + split;
+                const v2u ml = {__float_as_uint(mm), __float_as_uint(ll)};
+#pragma unroll
+                for (int j = 0; j < VE; j += 4) {
+                    const v4u x = {__float_as_uint(acc[j]), __float_as_uint(acc[j + 1]), __float_as_uint(acc[j + 2]), __float_as_uint(acc[j + 3])};
+                    if (a.join) __builtin_amdgcn_raw_buffer_store_b128(x, ro, (to * dim + VE * part + j) * 4, 0, kDeviceScope);
+                    else __builtin_amdgcn_raw_buffer_store_b128(x, ro, (to * dim + VE * part + j) * 4, 0, 0);
+                }
+                if (part == 0) {
+                    if (a.join) __builtin_amdgcn_raw_buffer_store_b64(ml, rm, to * 8, 0, kDeviceScope);
+                    else __builtin_amdgcn_raw_buffer_store_b64(ml, rm, to * 8, 0, 0);
+                }
+            }
+        }
+    }
+}
+
+template <int TYPE, int DT, int BLOCK, int DC>
+__global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_tree_kernel(CacheAttnArgs a) {
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    constexpr int G = kTreeGroups<TYPE>;
+    static_assert(G * (DT / 32) * kQueryPieces<TYPE> * 1024 <= (int)sizeof(DecodeLds<DT>), "q and the waves' results share the workgroup's LDS");
+    const TreeItem i = TreePlan(a).find<false>(blockIdx.x);
+    if (i.tile.b >= 0) {
+        const Request& rq = i.tile.rq;
+        const int r0 = i.tile.index * kTileRows, rows = min(rq.n * a.group - r0, kTileRows), len = rq.len;
+        const int per = ((len + kTileKeys - 1) / kTileKeys + i.splits - 1) / i.splits * kTileKeys;
+        const int begin = min(i.split * per, len), end = min(begin + per, len);
+        if (!i.small) chunk_tile<TYPE, DT, BLOCK, DC>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
+        else if (G == 4 && rows > 32) tree_tile<TYPE, DT, BLOCK, G>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
+        else tree_tile<TYPE, DT, BLOCK, 2>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
+        if (i.splits > 1 && a.join && came_last(a.counters + i.unit, i.splits, reinterpret_cast<uint32_t*>(smem)))
+            for (int r = 0; r < rows; r += 64) join_tile<TYPE, 8, 2, kDeviceScope>(a, rq, i.h, r0 + r, min(64, rows - r), i.splits);
+    }
+    fill_padding<TYPE>(a);
+}
+
+// The parts of eight rows of a unit as one, where units have many of them.
+constexpr int kJoinRows = 8;
+template <int TYPE>
+__global__ __launch_bounds__(256) void cache_tree_join_kernel(CacheAttnArgs a) {
+    const TreeItem i = TreePlan(a).find<true>(blockIdx.x / (kTileRows / kJoinRows));
+    const int r0 = i.tile.index * kTileRows + blockIdx.x % (kTileRows / kJoinRows) * kJoinRows;
+    const int rows = i.tile.b < 0 ? 0 : min(i.tile.rq.n * a.group - r0, kJoinRows);
+    if (rows > 0 && i.splits > 1) join_tile<TYPE, kJoinRows / 8, 8, 0>(a, i.tile.rq, i.h, r0, rows, i.splits);
+}
+#endif
+
+#if !MX_CACHE_TREE
 // Requests of many rows and, in the workgroups after `chunks`, of few: in a batch that has both they run side by side.
 template <int TYPE, int DT, int BLOCK, int DC>
 __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_mixed_kernel(CacheAttnArgs many, CacheAttnArgs few, int chunks) {
@@ -1088,6 +1606,7 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_mixed_kerne
     else decode<TYPE, DT, BLOCK>(few, blockIdx.x - chunks, *reinterpret_cast<DecodeLds<DT>*>(smem));
     fill_padding<TYPE>(many);
 }
+#endif
 
 // ---- joining the splits ---------------------------------------------------------------------------------
 // o = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m), in an order that the number of splits gives, whatever order they ended in.
@@ -1245,6 +1764,8 @@ struct Plan {
     bool decode, chunk;
     int part_rows, splits;         // of cache_decode_kernel
     int tiles, chunk_splits, run;
+    int grid;                      // cache_tree_kernel
+    bool join;                     // in it
     size_t few_bytes;
 };
 
@@ -1314,6 +1835,20 @@ Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, 
                                                               p.chunk ? 0 : p.part_rows) : 1;
     const int64_t rows = tokens * group;
     const int64_t big = p.decode ? (rows / (kFewRows + 1) < requests ? rows / (kFewRows + 1) : requests) : 1;   // requests with more rows
+    if (kTree && p.chunk) {
+        const int64_t big = rows < requests ? rows : requests, units = (rows / kTileRows + big) * c.heads, slots = type == MX_F32 ? 256 : 512;
+        p.decode = false;
+        p.tiles = clamp(units, INT32_MAX);
+        p.run = 2;
+        // Few units are cut to fill the GPU once; of many there is room for the longest to be cut, of more than there are counters for none is.
+        p.grid = clamp(2 * units > slots ? units + slots : slots, INT32_MAX);
+        p.chunk_splits = units > kCounterBytes / 4 ? 1 : clamp(rows * c.heads > 0 ? kMostChunks * kTileRows / (rows * c.heads) : 1, kMaxSplits);
+        if (p.chunk_splits > ceil_div(max_len, kTileKeys)) p.chunk_splits = clamp(ceil_div(max_len, kTileKeys), kMaxSplits);
+        // Many units have few parts each, which the last workgroup to come joins (24 requests of 320 to 504 rows: 379 us, 414 with a launch
+        // for the joins); the many parts of few units are joined by a launch, over the whole GPU.
+        p.join = 2 * units > slots;
+        return p;
+    }
     p.tiles = p.chunk ? clamp(p.decode ? rows / kTileRows + big : ceil_div(rows, kTileRows), INT32_MAX) : 0;
     // (128 keys of a request of one token take about as long as a tile)
     p.chunk_splits = p.chunk ? chunk_splits((rows / kTileRows + 1) * c.heads, ceil_div(max_len, kTileKeys), type == MX_F32 ? 256 : 512,
@@ -1365,12 +1900,32 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         many_rows = (int64_t)p.tiles * base.heads * kTileRows;
         many.part_o = (float*)parts;
         many.part_ml = (float2*)(many.part_o + base.tokens * base.heads_q * p.chunk_splits * base.dim);
+#if MX_CACHE_TREE
+        many.counters = (uint32_t*)workspace;
+        many.slots = p.grid;
+        many.small_rows = TYPE == MX_F32 ? 32 : 64;
+        many.small_run = BLOCK == 0 ? 10 : 14;
+        many.join = p.join;
+        many.sorted = 2 * p.tiles > p.grid && base.requests > 1 && base.requests <= 64;
+        constexpr int lds = 4 * kTileKeys * DT * 2;
+        static_assert(sizeof(DecodeLds<DT>) <= lds, "both kinds of tile share the workgroup's LDS");
+        static std::atomic<uint64_t> raised{0};
+        if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_tree_kernel<TYPE, DT, BLOCK, DC>, lds, raised)) return MX_ERR_DEVICE;
+        cache_tree_kernel<TYPE, DT, BLOCK, DC><<<(unsigned)p.grid, 256, lds, stream>>>(many);
+        MX_HIP_LAUNCH_CHECK();
+        if (!p.join && p.chunk_splits > 1) {
+            cache_tree_join_kernel<TYPE><<<(unsigned)((int64_t)p.tiles * (kTileRows / kJoinRows)), 256, 0, stream>>>(many);
+            MX_HIP_LAUNCH_CHECK();
+        }
+        return MX_OK;
+#else
+        const int64_t chunks = (int64_t)p.tiles * base.heads * p.chunk_splits;
         constexpr int lds = 4 * kTileKeys * DT * 2;
         static_assert(sizeof(DecodeLds<DT>) <= lds, "both share the workgroup's LDS");
         static std::atomic<uint64_t> raised{0};
         if (lds > 60 * 1024 && !allow_dynamic_lds((const void*)cache_mixed_kernel<TYPE, DT, BLOCK, DC>, lds, raised)) return MX_ERR_DEVICE;
-        const int64_t chunks = (int64_t)p.tiles * base.heads * p.chunk_splits;
         cache_mixed_kernel<TYPE, DT, BLOCK, DC><<<(unsigned)(chunks + (p.decode ? units * p.splits : 0)), 256, lds, stream>>>(many, few, (int)chunks);
+#endif
     } else {
         cache_decode_kernel<TYPE, DT, BLOCK><<<(unsigned)(units * p.splits), 256, 0, stream>>>(few);
     }
@@ -1444,7 +1999,7 @@ mx_status attend(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32
     if (tokens == 0) return MX_OK;
     const Plan p = plan_of(c, type, tokens, requests, heads_q, max_new, max_len);
     // the threads of a launch, 256 a workgroup, are counted in 32 bits (joins, of few workgroups by kMostChunks, stay far below)
-    if ((int64_t)p.tiles * c.heads * p.chunk_splits + (p.decode ? requests * c.heads * p.splits : 0) >= 1 << 24) return MX_ERR_UNSUPPORTED;
+    if (kTree ? p.grid >= 1 << 24 : (int64_t)p.tiles * c.heads * p.chunk_splits + (p.decode ? requests * c.heads * p.splits : 0) >= 1 << 24) return MX_ERR_UNSUPPORTED;
     CacheAttnArgs a{};
     a.q = q; a.out = out; a.ldq = ldq; a.ldo = ldo;
     a.k = (const uint8_t*)k_data; a.v = (const uint8_t*)v_data;
