@@ -169,7 +169,6 @@ static_assert(sizeof(Control) <= kControlBytes, "the workspace's first part");
 
 struct Shared {
     Found found[2 * kMostRows];
-    int row[kMostRows];
     Job job;                            // (not in registers: the walk's state is read between the passes only)
     uint64_t part[kMostSegments][3];    // of a row that a workgroup reads alone
     int excluded[kWaves][kExcluded];
@@ -197,6 +196,24 @@ __device__ __forceinline__ void team_counts_in(const VerifyArgs& a, int b, uint6
     put(&c->number, number + 1);
 }
 
+// Sums of the lanes' values up to and including each
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double moved(double v) {
+    const uint64_t x = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)x, CTRL, ROWS, 0xF, ROWS == 0xF);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(x >> 32), CTRL, ROWS, 0xF, ROWS == 0xF);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double scan_wave(double v) {
+    v += moved<0x111, 0xF>(v);                          // from the lane one before in the row of sixteen, two, four, eight
+    v += moved<0x112, 0xF>(v);
+    v += moved<0x114, 0xF>(v);
+    v += moved<0x118, 0xF>(v);
+    v += moved<0x142, 0xA>(v);                          // the first and third row's last lane to the row after
+    v += moved<0x143, 0xC>(v);                          // the second row's last lane to the second half
+    return v;
+}
+
 __device__ __forceinline__ double lane_of(double v, int lane) {
     const uint64_t x = __builtin_bit_cast(uint64_t, v);
     const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x, lane), hi = __builtin_amdgcn_readlane((uint32_t)(x >> 32), lane);
@@ -215,7 +232,8 @@ struct Team {
     int lane, wave;
     int base, up, id;          // of node base + lane: parent, token, random number, its logits in its parent's rows
     float uniform, lp, lq;
-    int nodes;                 // on the list of rows
+    int nodes, row0, row1, row2;   // on the list of rows
+    bool every;
     int segments;              // of a row, in this job: as many as give every wave of the team one
 
     __device__ __forceinline__ Team(const VerifyArgs& args, Shared& shared)
@@ -250,10 +268,33 @@ struct Team {
         while (from < n) {
             look_at(from & ~63);
             const uint64_t is = __ballot(up == node) & ~0ull << (from & 63);
-            if (is != 0) return base + __builtin_ctzll(is);
+            if (is != 0) return __builtin_amdgcn_readfirstlane(base + __builtin_ctzll(is));
             from = base + 64;
         }
         return n;
+    }
+    // Without a draft: the first child that is accepted, -1 for none.  Both sides of the test are left as they are summed; a lane a child,
+    // 64 nodes at a time: what its earlier siblings leave is the sum less theirs.
+    __device__ __forceinline__ int first_accepted(int node, const Found& p) {
+        double mass = p.sum;
+        for (int at = (node + 1) & ~63; at < n; at += 64) {
+            look_at(at);
+            const uint64_t kids = __ballot(up == node);
+            if (kids == 0) continue;
+            bool again = false;                          // an earlier sibling has the same token
+            for (uint64_t k = kids; k != 0; k &= k - 1) {
+                const int i = __builtin_ctzll(k);
+                again |= lane > i && id == __builtin_amdgcn_readlane(id, i);
+                if (at > ((node + 1) & ~63) && tried_before(node, base + i)) again |= lane == i;
+            }
+            const bool counts = up == node && !again && id >= 0 && id < a.vocab && p.sum > 0.0;
+            const double e = counts ? exp(((double)lp - (double)p.top) * heat.inv) : 0.0;
+            const double upto = scan_wave(e);
+            const uint64_t yes = __ballot(counts && (double)uniform * fmax(mass - (upto - e), 0.0) < e);
+            if (yes != 0) return base + __builtin_ctzll(yes);
+            mass = fmax(mass - lane_of(upto, 63), 0.0);
+        }
+        return -1;
     }
     // Whether a child of `node` before number `i` (which is looked at) has the same token
     __device__ __forceinline__ bool tried_before(int node, int i) {
@@ -264,27 +305,25 @@ struct Team {
         return false;
     }
 
-    // The nodes whose rows the walk may come to next, in s.row: all of a small tree, or the node and, as far as there is room, its children.
-    // Each counts for two rows, its logits and its draft's, when the draft plays a part.
+    // The nodes whose rows the walk may come to next: all of a small tree, or the node and its first children, a.ahead (two) of them at most.  Each
+    // counts for two rows, its logits and its draft's, when the draft plays a part.
     __device__ __forceinline__ void list_rows(int node, bool all) {
-        int rows = all ? n : 1;
-        __syncthreads();
-        if (threadIdx.x < kMostRows) s.row[threadIdx.x] = all ? threadIdx.x : node;
-        __syncthreads();
-        for (int at = (node + 1) & ~63; !all && at < n && rows <= a.ahead; at += 64) {
-            look_at(at);
-            const uint64_t is = __ballot(up == node);
-            const int place = rows + __popcll(is & ((1ull << lane) - 1));
-            if (wave == 0 && up == node && place <= a.ahead) s.row[place] = base + lane;
-            rows = min(rows + (int)__popcll(is), 1 + a.ahead);
-        }
-        nodes = rows;
-        __syncthreads();
+        every = all;
+        nodes = all ? n : 1;
+        if (all) return;
+        row0 = node;
+        row1 = a.ahead > 0 ? child_from(node, node + 1) : n;
+        row2 = a.ahead > 1 && row1 < n ? child_from(node, row1 + 1) : n;
+        nodes += (row1 < n) + (row2 < n);
     }
     __device__ __forceinline__ int rows() const { return drafted ? 2 * nodes : nodes; }
+    __device__ __forceinline__ int node_of(int row) const {
+        const int k = drafted ? row >> 1 : row;
+        return __builtin_amdgcn_readfirstlane(every ? k : k == 0 ? row0 : k == 1 ? row1 : row2);
+    }
     __device__ __forceinline__ int row_of(int node) const {              // -1: not on the list
-        const uint64_t is = __ballot(lane < nodes && s.row[min(lane, kMostRows - 1)] == node);
-        return is == 0 ? -1 : drafted ? 2 * __builtin_ctzll(is) : __builtin_ctzll(is);
+        const int k = every ? node : node == row1 ? 1 : node == row2 ? 2 : -1;
+        return k < 0 ? -1 : drafted ? 2 * k : k;
     }
 
     // Elements 8 o0 .. 8 o1 of a row (`tail`: and those behind them), by one wave; with `race` the race too, without the `excludes` tokens of
@@ -435,7 +474,7 @@ struct Team {
         const bool tail = segment == segments - 1;
         Found f;
         if (kind == kRows) {
-            const int node = __builtin_amdgcn_readfirstlane(s.row[drafted ? r >> 1 : r]);
+            const int node = node_of(r);
             const bool second = drafted && (r & 1);
             const int first = child_from(node, node + 1);
             if (second && first >= n) return;          // nobody looks at it
@@ -450,8 +489,10 @@ struct Team {
                     ++excludes;
                 }
             }
+            base = -1;                                 // (what it stands for is not kept in registers over the pass)
             f = scan(second ? draft_of(node) : logits_of(node), o0, o1, tail, race, node, excludes);
         } else {
+            base = -1;
             f = residual(o0, o1, tail, kind == kRace);
         }
         f.join(heat);
@@ -507,7 +548,7 @@ struct Team {
                 child = child_from(node, node + 1);
                 leaf = child >= n;
                 j.c = 0.0;
-                j.mass = drafted ? 1.0 : p.sum;          // without a draft both sides of the test are left as they are summed
+                j.mass = 1.0;
             }
             const bool full = j.kept >= a.width;
             int to = -1;
@@ -519,35 +560,24 @@ struct Team {
                     return false;
                 }
             } else {
-                // p and q of the nodes' tokens are computed for 64 neighbours at once, a lane each
-                int known = -1;
-                double ps = 0.0, qs = 1.0;
-                for (int i = full ? n : child; i < n; i = child_from(node, i + 1)) {
-                    look_at(i & ~63);
-                    if (known != base) {
-                        known = base;
-                        const bool in = id >= 0 && id < a.vocab;
-                        ps = in && j.p_sum > 0.0 ? exp(((double)lp - (double)j.p_top) * heat.inv) : 0.0;
-                        if (drafted) ps = in && j.p_sum > 0.0 ? ps / j.p_sum : 0.0;
-                        if (drafted) qs = in && j.q_sum > 0.0 ? exp(((double)lq - (double)j.q_top) * heat.inv) / j.q_sum : 0.0;
+                if (!drafted) {
+                    if (!full) to = first_accepted(node, p);
+                } else if (!full && child < n) {
+                    // one child a job: what is left of p when it is rejected takes a pass
+                    look_at(child & ~63);
+                    const bool in = id >= 0 && id < a.vocab;
+                    const double pc = in && j.p_sum > 0.0 ? exp(((double)lp - (double)j.p_top) * heat.inv) / j.p_sum : 0.0;
+                    const double qc = in && j.q_sum > 0.0 ? exp(((double)lq - (double)j.q_top) * heat.inv) / j.q_sum : 0.0;
+                    const bool yes = (double)uniform * j.mass * qc < fmax(pc - j.c * qc, 0.0);
+                    if (__ballot(yes) >> (child - base) & 1) {
+                        to = child;
+                    } else {
+                        j.c += j.mass;
+                        j.node = node;
+                        j.next_child = child_from(node, child + 1);
+                        j.kind = j.next_child < n ? kSum : kRace;
+                        return true;
                     }
-                    const double drawn = lane_of(qs, i - base);
-                    double r = lane_of(ps, i - base);
-                    if (drafted) r = fmax(r - j.c * drawn, 0.0);
-                    else if (tried_before(node, i)) r = 0.0;
-                    if ((double)__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(uniform), i - base)) * j.mass * drawn < r) {
-                        to = i;
-                        break;
-                    }
-                    if (!drafted) {
-                        j.mass = fmax(j.mass - r, 0.0);
-                        continue;
-                    }
-                    j.c += j.mass;
-                    j.node = node;
-                    j.next_child = child_from(node, i + 1);
-                    j.kind = j.next_child < n ? kSum : kRace;
-                    return true;
                 }
                 if (to < 0) {
                     if (j.kind == kRows && (leaf || (!drafted && !full && p.best_at >= 0))) {
