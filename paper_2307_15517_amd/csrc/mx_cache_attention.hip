@@ -1904,7 +1904,7 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         many.counters = (uint32_t*)workspace;
         many.slots = p.grid;
         many.small_rows = TYPE == MX_F32 ? 32 : 64;
-        many.small_run = BLOCK == 0 ? 10 : 14;
+        many.small_run = BLOCK == 0 ? 9 : 14;
         many.join = p.join;
         many.sorted = 2 * p.tiles > p.grid && base.requests > 1 && base.requests <= 64;
         constexpr int lds = 4 * kTileKeys * DT * 2;
