@@ -493,8 +493,9 @@ MX_API mx_status mx_tree_plan(const int32_t* parents, const int32_t* q_start, co
 /*
  * mx_cache_attention with a mask in place of the causal order among the new tokens: new token i of a request with n of them sees the
  * kv_len - n cached ones and those new ones whose bits are set in its mask (of mx_tree_plan, or any other; bits at n and past it
- * mean nothing, tokens past the words are not seen).  A token that sees no key gives zeros.  Everything else, arguments, numerics and
- * refusals, is as there; masks is 8-byte aligned, words 1 .. MX_TREE_MAX_NODES / 64.
+ * mean nothing, tokens past the words are not seen).  A token that sees no key gives zeros.  q_start does not fall (else rows of out may stay
+ * as they were; nothing outside the arrays is read or written).  Everything else, arguments, numerics and refusals, is as there;
+ * masks is 8-byte aligned, words 1 .. MX_TREE_MAX_NODES / 64.
  */
 MX_API size_t mx_cache_tree_attention_workspace_bytes(mx_cache c, int64_t tokens, int64_t requests, int32_t heads_q, int64_t max_new,
                                                       int64_t max_len);

@@ -1162,9 +1162,10 @@ struct TreePlan {
             blocks = __shfl(blocks, index);
         }
     }
-    // How many runs of about `of` blocks the request's keys are cut into: any number will do that all agree on
+    // How many runs of about `of` blocks the request's keys are cut into: any number will do that all agree on, two kernels among them, so
+    // what is rounded once is written so
     __device__ __forceinline__ int runs(int of) const {
-        return min(max((int)((float)blocks * __builtin_amdgcn_rcpf((float)of) + 0.9999f), 1), a.splits);
+        return min(max((int)__builtin_fmaf((float)blocks, __builtin_amdgcn_rcpf((float)of), 0.9999f), 1), a.splits);
     }
     // n / d: of small numbers the reciprocal is off by one at most
     static __device__ __forceinline__ int over(int n, int d) {
@@ -1183,14 +1184,14 @@ struct TreePlan {
         int most = 1, units = 0;
         for (int base = 0; base < a.requests; base += 64) {
             look_at(base);
-            const float v = (large + 8.f / (float)a.small_run * small) * blocks;
+            const float v = __builtin_fmaf(8.f / (float)a.small_run, (float)small, (float)large) * (float)blocks;
             all += (float)over_wave((int)fminf(v, 1e7f), false);
             most = max(most, over_wave(blocks, true));
             units += over_wave(large + small, false);
         }
         // a unit's last run is half empty on average: a little less than fits is the first guess, then a sixteenth more at a time until the items
         // are few enough, as they are with one run a unit
-        const float left = (float)a.slots - 0.45f * (float)a.heads * (float)units;
+        const float left = __builtin_fmaf(-0.45f * (float)a.heads, (float)units, (float)a.slots);
         run = max(a.run, (int)fminf(all * (float)a.heads / fmaxf(left, 1.f), (float)most));
         while (true) {
             const int of_small = small_run();
@@ -1210,7 +1211,9 @@ struct TreePlan {
         for (int base = 0; base < a.requests; base += 64) {
             look_at(base);
             const int of_large = runs(run), of_small = runs(small_run());
-            const int count = (large * of_large + small * of_small) * a.heads, many = (large + small) * a.heads;
+            // (exact below 2^24, which is past all workgroups: only requests whose tokens overlap come there, and they stay in bounds)
+            auto items_of = [&](int l, int s) { return (int)fminf((float)(l + s) * (float)a.heads, 0x1p24f); };
+            const int count = items_of(large * of_large, small * of_small), many = items_of(large, small);
             int upto = count, units_to = many;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
@@ -1250,7 +1253,7 @@ struct TreePlan {
                     tile = is_small ? n_large : y - split * n_large;
                 }
                 const int unit = first + tile * a.heads + h;
-                if (unit >= a.tiles) break;            // (only where requests' tokens overlap)
+                if ((uint32_t)unit >= (uint32_t)a.tiles) break;            // (only where requests' tokens overlap)
                 return TreeItem{Tile{of(index), tile, r}, is_small, h, split, is_small ? s_small : s_large, unit};
             }
             before += __builtin_amdgcn_readlane(upto, 63);

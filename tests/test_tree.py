@@ -295,6 +295,22 @@ def test_attention_bad_indices_do_not_reach_memory():
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_attention_of_requests_that_claim_the_same_tokens(dtype):
+    """Starts that fall give rows that are unspecified, but nothing past the arrays is touched and the workspace serves on."""
+    s = TreeStep([(70, 300)] * 70, 2, 4, 64, 16, FORMATS["bf16"], dtype, seed=16)
+    workspace = mx.cache_tree_workspace(s.cache.c, s.tokens, 70, 8, s.max_new, s.max_len, DEV)
+    kept = s.q_start.clone()
+    for most in (s.max_new, 3):
+        s.q_start[::2] = 0
+        s.q_start[1::2] = 2 ** 31 - 1
+        s.run(max_new=most, opad=8, workspace=workspace)
+        s.q_start.copy_(kept)
+        assert not workspace[:65536].any()
+        s.check(workspace=workspace)
+
+
+@gpu
 @pytest.mark.parametrize("lens", [[(9, 5000), (64, 900)], [(25, 3000), (20, 20)], [(7, 4000), (2, 60)]])
 def test_attention_same_inputs_same_bits_also_on_another_stream(lens):
     s = TreeStep(lens, 2, 4, 128, 16, FORMATS["mx32"], torch.float32, seed=15)
