@@ -45,7 +45,7 @@ struct CacheAttnArgs {
     int32_t least, most;       // this launch takes the requests that have least .. most rows (token, head of a group)
     int32_t part_rows;         // decode(): part rows per unit; a request with more rows is not split
     int32_t tiles;             // chunk(): row tiles of all requests, at most
-    int32_t sorted;            // cache_decode_kernel: the longest requests go first
+    int32_t sorted;            // the longest requests go first
     int32_t join;              // the workgroup of a unit that comes last joins its parts; else a launch of its own does
     int32_t vec_q, vec_o;      // rows of q / out allow 16-byte (bfloat16 out: 8-byte) accesses
     float c;                   // |scale| * log2(e)
@@ -53,7 +53,7 @@ struct CacheAttnArgs {
     const uint32_t* masks;     // kTree: [tokens][mask_words], bit j: new token j of the request is seen
     int32_t mask_words;        // 32-bit words of a token's mask
     int32_t slots;             // cache_tree_kernel: its workgroups; tiles: units, at most
-    int32_t small_rows, small_run;   // rows that a small tile may have; its runs in eighths of a large one's
+    int32_t small_rows, small_run, least_run;   // rows that a small tile may have; its runs in eighths of a large one's, and of one of 32 rows
 };
 
 // One request as a workgroup sees it, every length bounded by what the arrays hold.
@@ -1095,17 +1095,23 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
 }
 #else
 // ---- trees of more than sixteen rows --------------------------------------------------------------------
-// A workgroup takes a tile of up to 64 rows (32 of fp32 calls) of one request and key/value head; its four waves take blocks of 32 keys in
-// turn, as in decode(), and join at the end.  K and V go from memory to registers once for all rows of the tile, R groups of sixteen: an
-// MXInt block is converted once for them, and q, which all waves use, lies in LDS as the matrix instructions read it.  A block's K
-// registers are free for the next block's loads when its scores are there, V's after P V, so both are in flight during the rest.
-template <int TYPE>
-constexpr int kTreeGroups = TYPE == MX_F32 ? 2 : 4;
+// o = sum_j p_j v_j over the cached keys and those of the new ones that the row's mask has, in tiles of one request, key/value head and up to
+// 128 rows: chunk_tile()'s, without a causal order, or a small tile of up to 32 rows, 64 in bfloat16 calls on an MXInt cache, where a
+// large one would convert each key for half as many rows.  A small tile's four waves take blocks of 32 keys in turn, as in decode(), and
+// join at the end: K and V go from memory to registers once for all rows, R groups of sixteen, an MXInt block is converted once
+// for them, and q, which all waves use, lies in LDS as the matrix instructions read it.  A block's K registers are free for the next
+// block's loads when its scores are there, V's after P V, so both are in flight during the rest.
+// Bound by the issue of vector arithmetic (softmax, pieces of P, MXInt) and of matrix instructions, which two waves a SIMD overlap little:
+// 24 requests of 320 to 504 rows, 8 heads, 128 elements, MXInt 32: 368 us, clock 2.1 GHz, matrix cores 0.29 and vector units 0.48 of
+// the time.  Eight requests of 36 / 52 / 64 rows on 500 to 4000 keys, 8 heads: MXInt as small tiles 31.6 / 33.0 / 33.7 us, as large ones
+// 33.3 / 34.4 / 35.3; a bfloat16 cache as small ones 34.0 / 35.8 / 37.0, as large ones 32.7 / 33.6 / 34.8, but of 20 rows 25.9 and 31.0.
+template <int TYPE, int BLOCK>
+constexpr int kTreeGroups = TYPE == MX_F32 || BLOCK == 0 ? 2 : 4;
 
 // How a batch is shared out.  A unit is a tile of a request's rows and a key/value head; its keys are cut into runs of as few blocks of 64 as
 // leave no more items (a unit's runs) than workgroups.  A block of a large tile takes longer (3.6 us with an MXInt cache, 2.5 with
-// bfloat16; of a small one 2.1), so small tiles have runs of half as many again.  All know all lengths: there are no items without
-// work.  Every wave works it out for itself, a request a lane, 64 at a time.
+// bfloat16; of a small one of 64 rows 2.3, of 32 1.6), so small tiles have longer runs.  All know all lengths: there are no items
+// without work.  Every wave works it out for itself, a request a lane, 64 at a time (2 to 3 us with the loads of the lengths).
 struct TreeItem {
     Tile tile;                 // b < 0: nothing; index: of kTileRows rows
     bool small;                // no more than a.small_rows of them
@@ -1113,30 +1119,29 @@ struct TreeItem {
     int unit;                  // number of (tile, head)
 };
 
-__device__ __forceinline__ int over_wave(int v, bool largest) {
-#pragma unroll
-    for (int step = 0; step < 6; ++step) {
-        int o[2] = {v, v};
-        if (step == 0) o[1] = __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, true);
-        else if (step == 1) o[1] = __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, true);
-        else if (step == 2) o[1] = __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, true);
-        else if (step == 3) o[1] = __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, true);
-        else {
-            const auto r = step == 4 ? __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false)
-                                     : __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
-            o[0] = (int)r[0];
-            o[1] = (int)r[1];
-        }
-        v = largest ? max(o[0], o[1]) : o[0] + o[1];
-    }
-    return __builtin_amdgcn_readfirstlane(v);
+// Lanes' values (none negative) up to and including each as one: from the lane one before in the row of sixteen, two, four, eight; then the
+// first and third row's last lane to the row after, the second row's to the second half.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, ROWS == 0xF); }
+template <typename Op>
+__device__ __forceinline__ int scan_wave(int v, Op op) {
+    v = op(v, moved<0x111, 0xF>(v));
+    v = op(v, moved<0x112, 0xF>(v));
+    v = op(v, moved<0x114, 0xF>(v));
+    v = op(v, moved<0x118, 0xF>(v));
+    v = op(v, moved<0x142, 0xA>(v));
+    return op(v, moved<0x143, 0xC>(v));
 }
+__device__ __forceinline__ int sums_of(int v) { return scan_wave(v, [](int x, int y) { return x + y; }); }
+__device__ __forceinline__ int sum_of(int v) { return __builtin_amdgcn_readlane(sums_of(v), 63); }
+__device__ __forceinline__ int largest_of(int v) { return __builtin_amdgcn_readlane(scan_wave(v, [](int x, int y) { return max(x, y); }), 63); }
 
 struct TreePlan {
     const CacheAttnArgs& a;
     int lane, b0, index;       // requests b0 .. b0 + 63 are the lanes', each its `index`
     Request rq;
     int large, small, blocks;
+    int eighths;               // of a large tile's run, for the small one's
     int run;
 
     __device__ __forceinline__ void look_at(int b) {
@@ -1147,6 +1152,7 @@ struct TreePlan {
         const int rows = rq.n * a.group, rest = rows % kTileRows;
         large = rows / kTileRows + (rest > a.small_rows);
         small = rest > 0 && rest <= a.small_rows;
+        eighths = rest <= 32 ? a.least_run : a.small_run;
         blocks = max(1, (rq.len + kTileKeys - 1) / kTileKeys);
         index = b + lane;
         if (a.sorted) {                                // the longest first: 64 requests at most
@@ -1159,6 +1165,7 @@ struct TreePlan {
             rq = Request{__shfl(rq.t0, index), __shfl(rq.n, index), __shfl(rq.len, index)};
             large = __shfl(large, index);
             small = __shfl(small, index);
+            eighths = __shfl(eighths, index);
             blocks = __shfl(blocks, index);
         }
     }
@@ -1175,7 +1182,7 @@ struct TreePlan {
         q += r >= d ? 1 : r < 0 ? -1 : 0;
         return q;
     }
-    __device__ __forceinline__ int small_run() const { return max(run, run / 8 * a.small_run + run % 8 * a.small_run / 8); }
+    __device__ __forceinline__ int small_run() const { return max(run, run / 8 * eighths + run % 8 * eighths / 8); }
 
     __device__ __forceinline__ explicit TreePlan(const CacheAttnArgs& args) : a(args), lane(threadIdx.x & 63), b0(-1), run(INT_MAX / 4) {
         look_at(0);
@@ -1184,28 +1191,24 @@ struct TreePlan {
         int most = 1, units = 0;
         for (int base = 0; base < a.requests; base += 64) {
             look_at(base);
-            const float v = __builtin_fmaf(8.f / (float)a.small_run, (float)small, (float)large) * (float)blocks;
-            all += (float)over_wave((int)fminf(v, 1e7f), false);
-            most = max(most, over_wave(blocks, true));
-            units += over_wave(large + small, false);
+            all += (float)sum_of((int)fminf(__builtin_fmaf(8.f * __builtin_amdgcn_rcpf((float)eighths), (float)small, (float)large) * (float)blocks, 1e7f));
+            most = max(most, largest_of(blocks));
+            units += sum_of(large + small);
         }
         // a unit's last run is half empty on average: a little less than fits is the first guess, then a sixteenth more at a time until the items
         // are few enough, as they are with one run a unit
         const float left = __builtin_fmaf(-0.45f * (float)a.heads, (float)units, (float)a.slots);
-        run = max(a.run, (int)fminf(all * (float)a.heads / fmaxf(left, 1.f), (float)most));
+        run = max(a.run, (int)fminf(all * (float)a.heads * __builtin_amdgcn_rcpf(fmaxf(left, 1.f)), (float)most));
         while (true) {
-            const int of_small = small_run();
             int64_t items = 0;
             for (int base = 0; base < a.requests; base += 64) {
                 look_at(base);
-                items += over_wave(large * runs(run) + small * runs(of_small), false);
+                items += sum_of(large * runs(run) + small * runs(small_run()));
             }
             if (items * a.heads <= a.slots || run >= most) break;
             run += max(1, run >> 4);
         }
     }
-    // Item number `item`, or (UNIT) the first of unit number `item`
-    template <bool UNIT>
     __device__ __forceinline__ TreeItem find(int item) {
         int before = 0, units = 0;
         for (int base = 0; base < a.requests; base += 64) {
@@ -1214,45 +1217,29 @@ struct TreePlan {
             // (exact below 2^24, which is past all workgroups: only requests whose tokens overlap come there, and they stay in bounds)
             auto items_of = [&](int l, int s) { return (int)fminf((float)(l + s) * (float)a.heads, 0x1p24f); };
             const int count = items_of(large * of_large, small * of_small), many = items_of(large, small);
-            int upto = count, units_to = many;
-#pragma unroll
-            for (int d = 1; d < 64; d *= 2) {
-                const int o = __shfl_up(upto, d, 64), u = __shfl_up(units_to, d, 64);
-                upto += lane >= d ? o : 0;
-                units_to += lane >= d ? u : 0;
-            }
-            const uint64_t past = __ballot(UNIT ? units + units_to > item : before + upto > item);
+            const int upto = sums_of(count), units_to = sums_of(many);
+            const uint64_t past = __ballot(before + upto > item);
             if (past != 0) {
                 const int at = __builtin_ctzll(past);
                 auto of = [&](int v) { return __builtin_amdgcn_readlane(v, at); };
-                const int n_large = of(large), s_large = of(of_large), s_small = of(of_small), first = units + of(units_to) - of(many);
+                const int n_large = of(large), s_large = of(of_large), s_small = of(of_small);
                 const Request r{of(rq.t0), of(rq.n), of(rq.len)};
-                int h, tile, split;
-                bool is_small;
-                if constexpr (UNIT) {
-                    tile = over(item - first, a.heads);
-                    h = item - first - tile * a.heads;
-                    is_small = tile == n_large;
-                    split = 0;
+                // Workgroup u runs on XCD u % 8: with a multiple of eight heads an XCD takes whole heads, so that its L2 holds few of them; the
+                // tiles that read the same keys follow one another.
+                const int rest = item - before - (of(upto) - of(count)), each = n_large * s_large + (of(small) ? s_small : 0);
+                int h, y;
+                if (a.heads % 8 == 0) {
+                    y = rest >> 3;
+                    const int eighth = over(y, each);
+                    h = (rest & 7) + 8 * eighth;
+                    y -= eighth * each;
                 } else {
-                    // Workgroup u runs on XCD u % 8: with a multiple of eight heads an XCD takes whole heads, so that its L2 holds few of them; the
-                    // tiles that read the same keys follow one another.
-                    const int rest = item - before - (of(upto) - of(count)), each = n_large * s_large + (of(small) ? s_small : 0);
-                    int y;
-                    if (a.heads % 8 == 0) {
-                        y = rest >> 3;
-                        const int eighth = over(y, each);
-                        h = (rest & 7) + 8 * eighth;
-                        y -= eighth * each;
-                    } else {
-                        y = over(rest, a.heads);
-                        h = rest - y * a.heads;
-                    }
-                    is_small = y >= n_large * s_large;
-                    split = is_small ? y - n_large * s_large : over(y, n_large);
-                    tile = is_small ? n_large : y - split * n_large;
+                    y = over(rest, a.heads);
+                    h = rest - y * a.heads;
                 }
-                const int unit = first + tile * a.heads + h;
+                const bool is_small = y >= n_large * s_large;
+                const int split = is_small ? y - n_large * s_large : over(y, n_large), tile = is_small ? n_large : y - split * n_large;
+                const int unit = units + of(units_to) - of(many) + tile * a.heads + h;
                 if ((uint32_t)unit >= (uint32_t)a.tiles) break;            // (only where requests' tokens overlap)
                 return TreeItem{Tile{of(index), tile, r}, is_small, h, split, is_small ? s_small : s_large, unit};
             }
@@ -1261,9 +1248,19 @@ struct TreePlan {
         }
         return TreeItem{Tile{-1, 0, Request{0, 0, 0}}, false, 0, 0, 0, 0};
     }
+    // The runs of the unit that a head's row number `row` of all packed ones belongs to; 0: none
+    __device__ __forceinline__ int runs_of_row(int row) {
+        for (int base = 0; base < a.requests; base += 64) {
+            look_at(base);
+            const int r = row - rq.t0 * a.group;
+            const uint64_t its = __ballot(r >= 0 && r < rq.n * a.group);
+            if (its != 0) return __builtin_amdgcn_readlane(runs(r / kTileRows < large ? run : small_run()), __builtin_ctzll(its));
+        }
+        return 0;
+    }
 };
 
-// join_parts() for 8 U rows: eight groups of 32 lanes, a group U of the rows, S splits' parts of all of them in flight.
+// The parts of 8 U rows as one: eight groups of 32 lanes, a group U of the rows, S splits' parts of all of them in flight.
 template <int TYPE, int U, int S, int SCOPE>
 __device__ __forceinline__ void join_tile(const CacheAttnArgs& a, const Request& rq, int h, int r0, int rows, int splits) {
     const int64_t part0 = part_row_of(a, h, rq, r0) * a.splits;
@@ -1572,9 +1569,9 @@ __device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Tile& ti
 template <int TYPE, int DT, int BLOCK, int DC>
 __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_tree_kernel(CacheAttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    constexpr int G = kTreeGroups<TYPE>;
+    constexpr int G = kTreeGroups<TYPE, BLOCK>;
     static_assert(G * (DT / 32) * kQueryPieces<TYPE> * 1024 <= (int)sizeof(DecodeLds<DT>), "q and the waves' results share the workgroup's LDS");
-    const TreeItem i = TreePlan(a).find<false>(blockIdx.x);
+    const TreeItem i = TreePlan(a).find(blockIdx.x);
     if (i.tile.b >= 0) {
         const Request& rq = i.tile.rq;
         const int r0 = i.tile.index * kTileRows, rows = min(rq.n * a.group - r0, kTileRows), len = rq.len;
@@ -1589,14 +1586,56 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_tree_kernel
     fill_padding<TYPE>(a);
 }
 
-// The parts of eight rows of a unit as one, where units have many of them.
-constexpr int kJoinRows = 8;
+// The parts of a row as one: a wave a row, its two halves every other part, kJoinParts of them in flight.  Bound by the latency of the lengths'
+// loads and of one or two rounds of parts (972 rows of up to 7 parts 7 us, 2440 of 22 parts 9).
+constexpr int kJoinParts = 8, kJoinGrid = 1792;
 template <int TYPE>
 __global__ __launch_bounds__(256) void cache_tree_join_kernel(CacheAttnArgs a) {
-    const TreeItem i = TreePlan(a).find<true>(blockIdx.x / (kTileRows / kJoinRows));
-    const int r0 = i.tile.index * kTileRows + blockIdx.x % (kTileRows / kJoinRows) * kJoinRows;
-    const int rows = i.tile.b < 0 ? 0 : min(i.tile.rq.n * a.group - r0, kJoinRows);
-    if (rows > 0 && i.splits > 1) join_tile<TYPE, kJoinRows / 8, 8, 0>(a, i.tile.rq, i.h, r0, rows, i.splits);
+    const int rows = (int)a.tokens * a.group, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    TreePlan plan(a);
+    for (int64_t item = (int64_t)blockIdx.x * 4 + wave; item < (int64_t)rows * a.heads; item += (int64_t)gridDim.x * 4) {
+        const int h = (int)item / rows, row = (int)item - h * rows;
+        const int splits = plan.runs_of_row(row);
+        if (splits <= 1) continue;
+        const int64_t part0 = ((int64_t)h * rows + row) * a.splits;
+        const BufRsrc ro = make_rsrc(a.part_o + part0 * a.dim, (uint32_t)(splits * a.dim * 4)), rm = make_rsrc(a.part_ml + part0, (uint32_t)(splits * 8));
+        const int half = (threadIdx.x >> 5) & 1, lane = threadIdx.x & 31, d = 4 * lane < a.dim ? 4 * lane : 0;
+        float m = -__builtin_inff(), l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+        // m, l and x take in another part's
+        auto take = [&](float pm, float pl, const float (&px)[4]) __attribute__((always_inline)) {
+            const float top = __builtin_fmaxf(m, pm), use = top == -__builtin_inff() ? 0.f : top, f = exp2_of(m - use), w = exp2_of(pm - use);
+            m = top;
+            l = l * f + pl * w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = x[e] * f + px[e] * w;
+        };
+        for (int s0 = half; s0 < splits; s0 += 2 * kJoinParts) {
+            v4u y[kJoinParts];
+            v2u ml[kJoinParts];
+#pragma unroll
+            for (int i = 0; i < kJoinParts; ++i) {
+                const int at = min(s0 + 2 * i, splits - 1);
+                ml[i] = __builtin_amdgcn_raw_buffer_load_b64(rm, at * 8, 0, 0);
+                y[i] = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(ro, (at * a.dim + d) * 4, 0, 0));
+            }
+#pragma unroll
+            for (int i = 0; i < kJoinParts; ++i) {
+                const float p[4] = {__uint_as_float(y[i][0]), __uint_as_float(y[i][1]), __uint_as_float(y[i][2]), __uint_as_float(y[i][3])};
+                if (s0 + 2 * i < splits && __uint_as_float(ml[i][0]) > -__builtin_inff()) take(__uint_as_float(ml[i][0]), __uint_as_float(ml[i][1]), p);
+            }
+        }
+        auto other = [](float v) __attribute__((always_inline)) {
+            const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+            return __uint_as_float(r[1]);                  // the upper half's, in both
+        };
+        const float p[4] = {other(x[0]), other(x[1]), other(x[2]), other(x[3])};
+        take(other(m), other(l), p);
+        if (half != 0 || 4 * lane >= a.dim) continue;
+        const int tok = row / a.group, head = h * a.group + (row - tok * a.group);
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float o[4] = {x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
+        store_out<TYPE, 4>(a, (int64_t)tok * a.ldo + (int64_t)head * a.dim + d, o);
+    }
 }
 #endif
 
@@ -1847,9 +1886,10 @@ Plan plan_of(const mx_cache& c, int32_t type, int64_t tokens, int64_t requests, 
         p.grid = clamp(2 * units > slots ? units + slots : slots, INT32_MAX);
         p.chunk_splits = units > kCounterBytes / 4 ? 1 : clamp(rows * c.heads > 0 ? kMostChunks * kTileRows / (rows * c.heads) : 1, kMaxSplits);
         if (p.chunk_splits > ceil_div(max_len, kTileKeys)) p.chunk_splits = clamp(ceil_div(max_len, kTileKeys), kMaxSplits);
-        // Many units have few parts each, which the last workgroup to come joins (24 requests of 320 to 504 rows: 379 us, 414 with a launch
-        // for the joins); the many parts of few units are joined by a launch, over the whole GPU.
-        p.join = 2 * units > slots;
+        // More units than the GPU holds workgroups have few parts each, and the last workgroup of a unit to come joins them beside others' work
+        // (24 requests of 320 to 504 rows, 8 heads: 375 us, 385 with a launch for the joins); the parts of fewer units are joined by a
+        // launch, over the whole GPU (16 requests of 4 to 100 rows: 54 us, 72 without; 30 of 52 rows: 83.9, 87.9).
+        p.join = units > slots;
         return p;
     }
     p.tiles = p.chunk ? clamp(p.decode ? rows / kTileRows + big : ceil_div(rows, kTileRows), INT32_MAX) : 0;
@@ -1906,8 +1946,9 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
 #if MX_CACHE_TREE
         many.counters = (uint32_t*)workspace;
         many.slots = p.grid;
-        many.small_rows = TYPE == MX_F32 ? 32 : 64;
-        many.small_run = BLOCK == 0 ? 9 : 14;
+        many.small_rows = 16 * kTreeGroups<TYPE, BLOCK>;
+        many.small_run = 12;
+        many.least_run = BLOCK == 0 ? 14 : 18;
         many.join = p.join;
         many.sorted = 2 * p.tiles > p.grid && base.requests > 1 && base.requests <= 64;
         constexpr int lds = 4 * kTileKeys * DT * 2;
@@ -1917,7 +1958,9 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         cache_tree_kernel<TYPE, DT, BLOCK, DC><<<(unsigned)p.grid, 256, lds, stream>>>(many);
         MX_HIP_LAUNCH_CHECK();
         if (!p.join && p.chunk_splits > 1) {
-            cache_tree_join_kernel<TYPE><<<(unsigned)((int64_t)p.tiles * (kTileRows / kJoinRows)), 256, 0, stream>>>(many);
+            many.sorted = 0;
+            const int64_t rows = base.tokens * base.heads_q;
+            cache_tree_join_kernel<TYPE><<<(unsigned)(rows < 4 * kJoinGrid ? ceil_div(rows, 4) : kJoinGrid), 256, 0, stream>>>(many);
             MX_HIP_LAUNCH_CHECK();
         }
         return MX_OK;
