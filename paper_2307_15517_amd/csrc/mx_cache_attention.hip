@@ -1588,7 +1588,7 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_tree_kernel
 
 // The parts of a row as one: a wave a row, its two halves every other part, kJoinParts of them in flight.  Bound by the latency of the lengths'
 // loads and of one or two rounds of parts (972 rows of up to 7 parts 7 us, 2440 of 22 parts 9).
-constexpr int kJoinParts = 8, kJoinGrid = 1792;
+constexpr int kJoinParts = 8, kJoinGrid = 1536;     // (as many workgroups as the GPU holds)
 template <int TYPE>
 __global__ __launch_bounds__(256) void cache_tree_join_kernel(CacheAttnArgs a) {
     const int rows = (int)a.tokens * a.group, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

@@ -103,3 +103,10 @@ def test_attention_with_kept_scores_stays_in_registers(scratch_bytes):
     """Up to eight tiles of scores per wave, 128 registers of the 256."""
     kernels = [n for n in scratch_bytes if re.search(r"\battention_(kept|short)_kernel<", n)]
     assert len(kernels) == 16 + 30 and not [n for n in kernels if scratch_bytes[n]]
+
+
+def test_verification_and_the_joins_of_trees_stay_in_registers(kernel_notes):
+    """Three workgroups of four waves a compute unit, as verification's teams are counted; six for the joins."""
+    for name, kernels, waves in ((r"\bverify_kernel<\d>", 2, 3), (r"\bcache_tree_join_kernel<\d>", 2, 6)):
+        found = [v for n, v in kernel_notes.items() if re.search(name, n)]
+        assert len(found) == kernels and all(scratch == 0 and waves_per_simd(vgprs) >= waves for scratch, vgprs in found), (name, found)
