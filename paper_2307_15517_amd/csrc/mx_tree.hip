@@ -6,7 +6,8 @@ namespace {
 
 // ---- mx_tree_plan ---------------------------------------------------------------------------------------
 // mask(i) = {i} or mask(parent(i)), depth(i) = depth(parent(i)) + 1.  Integers only, twelve bytes a node and word: bound by the
-// latency of one launch and of the chain of parents.
+// latency of one launch and of the chain of parents (4 requests of 5 nodes 2.1 us in the kernel, 200 of up to 180 nodes, three words,
+// 3.1; 5 with the call).
 struct TreeArgs {
     const int32_t* parents;
     const int32_t* q_start;
@@ -122,7 +123,8 @@ __global__ __launch_bounds__(kTreeThreads) void tree_words_kernel(TreeArgs a) {
 // ---- mx_cache_move --------------------------------------------------------------------------------------
 // Row path[i] of a request's new tokens goes to place i, path[i] >= i and rising, so a run of rows may be written once all of it has been
 // read: what later runs read lies past it.  A wave takes a request, a head and one of the two tensors, 16 bytes a lane, as many rows
-// at once as it holds.  A few kilobytes a request: bound by the chain of loads (lengths, path, table, row).
+// at once as it holds (four of 128 bfloat16 elements, eight of 128 MXInt ones).  A few kilobytes a request: bound by the chain of
+// loads lengths, path, table, row, each of which waits for the one before (one request 3.4 us in the kernel, 96 requests of 8 heads 5.5).
 struct MoveArgs {
     uint8_t* data[2];
     uint8_t* exps[2];
