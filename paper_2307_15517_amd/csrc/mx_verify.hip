@@ -263,6 +263,15 @@ struct Team {
         lp = s.lp[k];
         lq = s.lq[k];
     }
+    // The logits of the nodes' tokens in their parents' rows, thread i of `step`: nothing needs them before the first decision
+    __device__ __forceinline__ void look_up(int i, int step) const {
+        for (; i < n; i += step) {
+            const int p = s.parent[i], x = s.id[i];
+            const bool in = p >= 0 && p < i && x >= 0 && x < a.vocab;
+            s.lp[i] = in ? value_at<TYPE>(logits_of(p), x) : 0.f;
+            s.lq[i] = in && a.draft != nullptr ? value_at<TYPE>(draft_of(p), x) : 0.f;
+        }
+    }
     // The first child of `node` from number `from` on, n when there is none
     __device__ __forceinline__ int child_from(int node, int from) {
         while (from < n) {
@@ -631,15 +640,8 @@ __global__ __launch_bounds__(kThreads, 3) void verify_kernel(VerifyArgs a) {
         s.uniform[i] = a.uniform[team.t0 + i];
     }
     __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
-        const int up = s.parent[i], x = s.id[i];
-        const bool in = up >= 0 && up < i && x >= 0 && x < a.vocab;
-        s.lp[i] = in ? value_at<TYPE>(team.logits_of(up), x) : 0.f;
-        s.lq[i] = in && a.draft != nullptr ? value_at<TYPE>(team.draft_of(up), x) : 0.f;
-    }
+    if (!shared) team.look_up(tid, kThreads);
     if (team.member == 0 && tid == 0 && n > 0) a.path[b * a.width] = 0;
-    __syncthreads();
-
     if (tid == 0) {
         s.job = Job{};
         s.job.kept = 1;
@@ -685,10 +687,13 @@ __global__ __launch_bounds__(kThreads, 3) void verify_kernel(VerifyArgs a) {
                 for (int polls = 0; !here && polls < kMostPolls; ++polls)
                     here = __ballot(lane < a.team && get(posted + min(lane, a.team - 1)) < want) == 0;
                 if (lane == 0) s.all_here = here;
-            } else if (wave == 3 && jobs == 1 && lane == 0) {
-                team_counts_in(a, b, number);
+            } else if (wave == 3 && jobs == 1) {
+                if (lane == 0) team_counts_in(a, b, number);
+            } else if (jobs == 1) {
+                team.look_up(tid - 64, 128);
             }
             __syncthreads();
+            if (jobs == 1) team.base = -1;
             alone = s.all_here == 0;
             if (alone) continue;
             for (int x = wave; x < rows; x += kWaves) {
