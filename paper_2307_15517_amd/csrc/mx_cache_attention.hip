@@ -1136,7 +1136,9 @@ __device__ __forceinline__ int sums_of(int v) { return scan_wave(v, [](int x, in
 __device__ __forceinline__ int sum_of(int v) { return __builtin_amdgcn_readlane(sums_of(v), 63); }
 __device__ __forceinline__ int largest_of(int v) { return __builtin_amdgcn_readlane(scan_wave(v, [](int x, int y) { return max(x, y); }), 63); }
 
+template <int TYPE>
 struct TreePlan {
+    static constexpr int kResident = TYPE == MX_F32 ? 256 : 512;       // workgroups that the GPU holds
     const CacheAttnArgs& a;
     int lane, b0, index;       // requests b0 .. b0 + 63 are the lanes', each its `index`
     Request rq;
@@ -1195,18 +1197,39 @@ struct TreePlan {
             most = max(most, largest_of(blocks));
             units += sum_of(large + small);
         }
-        // a unit's last run is half empty on average: a little less than fits is the first guess, then a sixteenth more at a time until the items
-        // are few enough, as they are with one run a unit
-        const float left = __builtin_fmaf(-0.45f * (float)a.heads, (float)units, (float)a.slots);
-        run = max(a.run, (int)fminf(all * (float)a.heads * __builtin_amdgcn_rcpf(fmaxf(left, 1.f)), (float)most));
+        const float work = all * (float)a.heads;       // in blocks of a large tile
+        // The smallest run that leaves no more items than there are workgroups.  A unit's last run is half empty on average: a little less than fits
+        // is the first guess, then a sixteenth more at a time until the items are few enough, as they are with one run a unit.
+        // Items for more than one round even out ragged lengths; where all units fit one round, longer runs may be done sooner.  A run's start and end
+        // take as long as kStart blocks, and of the last round half a run stands alone on average.  (30 requests of 52 rows on 200 to 3000 keys of a
+        // bfloat16 cache 76 us, 86 in two rounds, of an MXInt one 64 and 75; 32 of 32 rows on 2000 keys 65 and 75.)
+        constexpr float kStart = 2.5f;
+        int slots = a.slots, several = 0;
+        float rounds = 0.f;
+#pragma unroll 1
         while (true) {
+            const float left = __builtin_fmaf(-0.45f * (float)a.heads, (float)units, (float)slots);
+            run = max(a.run, (int)fminf(work * __builtin_amdgcn_rcpf(fmaxf(left, 1.f)), (float)most));
             int64_t items = 0;
-            for (int base = 0; base < a.requests; base += 64) {
-                look_at(base);
-                items += sum_of(large * runs(run) + small * runs(small_run()));
+#pragma unroll 1
+            while (true) {
+                items = 0;
+                for (int base = 0; base < a.requests; base += 64) {
+                    look_at(base);
+                    items += sum_of(large * runs(run) + small * runs(small_run()));
+                }
+                items *= a.heads;
+                if (items <= slots || run >= most) break;
+                run += max(1, run >> 4);
             }
-            if (items * a.heads <= a.slots || run >= most) break;
-            run += max(1, run >> 4);
+            if (slots <= kResident) {
+                if (several > 0 && (float)run + kStart >= rounds) run = several;
+                return;
+            }
+            if (units * a.heads > kResident) return;
+            rounds = __builtin_fmaf(__builtin_fmaf(kStart, (float)items, work), __builtin_amdgcn_rcpf((float)kResident), 0.5f * (float)run);
+            several = run;
+            slots = kResident;
         }
     }
     __device__ __forceinline__ TreeItem find(int item) {
@@ -1571,7 +1594,7 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_tree_kernel
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     constexpr int G = kTreeGroups<TYPE, BLOCK>;
     static_assert(G * (DT / 32) * kQueryPieces<TYPE> * 1024 <= (int)sizeof(DecodeLds<DT>), "q and the waves' results share the workgroup's LDS");
-    const TreeItem i = TreePlan(a).find(blockIdx.x);
+    const TreeItem i = TreePlan<TYPE>(a).find(blockIdx.x);
     if (i.tile.b >= 0) {
         const Request& rq = i.tile.rq;
         const int r0 = i.tile.index * kTileRows, rows = min(rq.n * a.group - r0, kTileRows), len = rq.len;
@@ -1592,7 +1615,7 @@ constexpr int kJoinParts = 8, kJoinGrid = 1536;     // (as many workgroups as th
 template <int TYPE>
 __global__ __launch_bounds__(256) void cache_tree_join_kernel(CacheAttnArgs a) {
     const int rows = (int)a.tokens * a.group, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    TreePlan plan(a);
+    TreePlan<TYPE> plan(a);
     for (int64_t item = (int64_t)blockIdx.x * 4 + wave; item < (int64_t)rows * a.heads; item += (int64_t)gridDim.x * 4) {
         const int h = (int)item / rows, row = (int)item - h * rows;
         const int splits = plan.runs_of_row(row);

@@ -343,6 +343,16 @@ def test_attention_many_requests(dtype, requests, heads, group, most_new, longes
     TreeStep(lens, heads, group, 64, 16, FORMATS["mx32"], dtype, seed=requests).check()
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("requests,heads", [(35, 8), (70, 4), (17, 8), (40, 4)])
+@pytest.mark.parametrize("spread", [1.0, 0.02])
+def test_attention_of_about_as_many_units_as_workgroups(dtype, requests, heads, spread):
+    """Between half as many and as many (row tile, head) pairs as the GPU holds workgroups: in one round, or in shorter runs of ragged lengths."""
+    lens = [(9 + b % 5, int(1200 * spread ** (b / requests)) + 14) for b in range(requests)]
+    TreeStep(lens, heads, 4, 64, 16, FORMATS["mx32"], dtype, seed=31).check()
+
+
 def test_attention_smaller_batches_need_no_more_workspace():
     import random
     r = random.Random(6)
