@@ -343,6 +343,30 @@ def test_same_results_on_another_stream_and_one_workspace(drawn):
         assert bool((ws[most:] == 0xA5).all())
 
 
+@gpu
+@pytest.mark.parametrize("drawn", [False, True])
+def test_calls_at_once(drawn):
+    """Two streams with a workspace each and products on a third: members of a team may run late or one after another, with the same results."""
+    batches = [Batch([40] * 12, 32000, torch.float32, drawn, seed=41), Batch([6] * 24, 50272, torch.float32, drawn, seed=42)]
+    first = [b.check(b.run()) for b in batches]
+    args = [(b.logits, ints(b.ids.tolist()), ints(b.parents.tolist()), ints(b.starts), b.temperature, b.uniform, b.noise, b.width, b.draft,
+             mx.verify_workspace(len(b.ids), len(b.sizes), b.vocab, DEV)) for b in batches]
+    x = torch.randn((4096, 4096), device=DEV)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        with torch.cuda.stream(streams[2]):
+            x = x @ x * 2.0 ** -6
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                for _ in range(3):
+                    got[k].append(mx.verify(*args[k]))
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert all(torch.equal(p, q) for g in got[k] for p, q in zip(first[k], g))
+
+
 def test_smaller_batches_need_no_more_workspace():
     import random
     r = random.Random(7)
