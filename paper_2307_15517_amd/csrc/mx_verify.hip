@@ -267,7 +267,7 @@ struct Team {
     __device__ __forceinline__ void look_up(int i, int step) const {
         for (; i < n; i += step) {
             const int p = s.parent[i], x = s.id[i];
-            const bool in = p >= 0 && p < i && x >= 0 && x < a.vocab;
+            const bool in = p >= 0 && x >= 0 && x < a.vocab;
             s.lp[i] = in ? value_at<TYPE>(logits_of(p), x) : 0.f;
             s.lq[i] = in && a.draft != nullptr ? value_at<TYPE>(draft_of(p), x) : 0.f;
         }
@@ -635,7 +635,8 @@ __global__ __launch_bounds__(kThreads, 3) void verify_kernel(VerifyArgs a) {
     const bool shared = a.team > 1;
     const uint64_t number = shared ? get(&a.control->number) : 0;
     for (int i = tid; i < n; i += kThreads) {
-        s.parent[i] = i == 0 ? -1 : a.parents[team.t0 + i];
+        const int p = a.parents[team.t0 + i];
+        s.parent[i] = p >= 0 && p < i ? p : -1;           // so children come after their parent, here and wherever nodes are compared with it
         s.id[i] = a.ids[team.t0 + i];
         s.uniform[i] = a.uniform[team.t0 + i];
     }

@@ -374,3 +374,57 @@ def test_smaller_batches_need_no_more_workspace():
         top = [int(2 ** r.uniform(0, e)) for e in (15, 13, 20)]
         less = [r.choice([v, r.randint(1, v)]) for v in top]
         assert 65536 <= mx.mx_verify_workspace_bytes(*less) <= mx.mx_verify_workspace_bytes(*top), (less, top)
+
+
+def _other_parents(b, seed, least=0):
+    """Gives a third of the nodes of a batch a parent that is none: their own number, a later one, one far outside."""
+    r = np.random.default_rng(seed)
+    for lo, n in zip(b.starts, b.sizes):
+        for i in range(max(1, least), n):
+            if r.random() < 1 / 3:
+                b.parents[lo + i] = r.choice([i, int(r.integers(i, n)), int(r.integers(i, n)), n, -7, 2 ** 31 - 1, -2 ** 31])
+
+
+@gpu
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("greedy", [0.0, 0.5, 1.0])
+def test_parents_that_are_none(drawn, greedy):
+    """A node whose parent is not before it stands on the cached tokens: no walk comes to it, and it takes nothing from the children.  Logits are
+    far below 0, as logarithms of probabilities are; small random numbers, so that walks go deep."""
+    for sizes, branch in (([3] * 40, 2), ([12] * 30, 3), ([150, 64, 130, 65, 200] * 3, 6), ([190] * 6, 90)):
+        b = Batch(sizes, 300, torch.float32, drawn, seed=len(sizes), branch=branch, width=30, greedy=greedy)
+        b.logits -= 40.0
+        b.uniform *= 0.3
+        _other_parents(b, seed=sum(sizes))
+        path, kept, following = (t.cpu() for t in b.check(b.run()))
+        for line, k in zip(path.tolist(), kept.tolist()):
+            assert all(x < y for x, y in zip(line, line[1:k])) and line[0] == 0
+    # node 1 names node 2, which follows node 0: the path is 0, 2
+    for children in ([-1, 2, 0], [-1, 2, 0, 3], [-1, 3, 0, 2]):
+        b = Batch([len(children)] * 4, 9, torch.float32, drawn, seed=14, greedy=greedy)
+        b.logits[:] = -20.0
+        b.logits[:, 5] = 0.0
+        if drawn:
+            b.draft[:] = b.logits
+        b.parents[:], b.ids[:] = children * 4, 5
+        b.uniform[:] = 0.5
+        path, kept, following = b.check(b.run())
+        want = [0, 2, 3] if children[-1] == 2 else [0, 2]
+        assert path.tolist() == [want + [-1] * (8 - len(want))] * 4 and following.tolist() == [5] * 4
+
+
+@gpu
+@pytest.mark.parametrize("drawn", [False, True])
+def test_parents_that_are_none_in_later_blocks(drawn):
+    """Nodes of the same 64 as the node that they name, and of those after it, beside real children with the same tokens."""
+    n, B = 200, 12
+    b = Batch([n] * B, 50, torch.float32, drawn, seed=15, width=190, sharp=0.5)
+    b.logits -= 30.0
+    b.uniform *= 2.0 ** -12                                                  # every real child with a token is accepted
+    r = np.random.default_rng(16)
+    for lo in b.starts[:-1]:
+        for i in range(1, n):                                                # a line of all but every fifth, which names a later node
+            b.parents[lo + i] = i + int(r.integers(1, 90)) if i % 5 == 3 else i - 2 if i % 5 == 4 else i - 1
+        b.ids[lo:lo + n] = r.integers(0, 50, n)
+    path, kept, following = b.check(b.run())
+    assert kept.tolist() == [160] * B
