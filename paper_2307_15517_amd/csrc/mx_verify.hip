@@ -343,13 +343,14 @@ struct Team {
         // N elements from place `at` on: the largest is known to be no larger than f.top
         auto take = [&](int at, const float* x, float* z, auto count_c) __attribute__((always_inline)) {
             constexpr int N = decltype(count_c)::value;
-            float p[N], sum = 0.f;
+            float p[N];
+            double sum[2] = {0.0, 0.0};
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 p[e] = heat.exp_of(x[e] - f.top);
-                sum += p[e];
+                sum[e & 1] += (double)p[e];
             }
-            f.sum += sum;
+            f.sum += sum[0] + sum[1];
             if (!race) return;
             auto exclude = [&](int token) __attribute__((always_inline)) {
 #pragma unroll
@@ -436,18 +437,18 @@ struct Team {
         constexpr int U = 2;
         auto take = [&](int at, const float* x, const float* y, const float* z, auto count_c) __attribute__((always_inline)) {
             constexpr int N = decltype(count_c)::value;
-            float sum = 0.f;
+            double sum[2] = {0.0, 0.0};
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const float r = __builtin_fmaxf(__builtin_fmaf(heat.exp_of(x[e] - p_top), fp, -(heat.exp_of(y[e] - q_top) * fq)), 0.f);
-                sum += r;
+                sum[e & 1] += (double)r;
                 const float score = r * __builtin_amdgcn_rcpf(z[e]);
                 if (score > f.best) {
                     f.best = score;
                     f.best_at = at + e;
                 }
             }
-            f.sum += sum;
+            f.sum += sum[0] + sum[1];
         };
 #pragma unroll 1
         for (int o = o0 + lane; o < o1; o += 64 * U) {

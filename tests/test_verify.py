@@ -428,3 +428,22 @@ def test_parents_that_are_none_in_later_blocks(drawn):
         b.ids[lo:lo + n] = r.integers(0, 50, n)
     path, kept, following = b.check(b.run())
     assert kept.tolist() == [160] * B
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [8, 1000, 50272])
+def test_small_values_beside_a_large_one_count(dtype, vocab):
+    """Sums over a row are in 64 bits: seven values of 2e-8 next to a 1 are the difference between a rejected and an accepted child, and what is
+    left of the row after it.  (1 - 2^-24)(1 + 1.4e-7) = 1 + 8e-8 > 1, then 0.1 * 1.4e-7 = 1.4e-8 < 2e-8; exponentials are off by 4e-6 of
+    themselves at most, that is by 6e-13 of the sum.)"""
+    for at, top in [(x, y) for x in sorted({0, (vocab // 2) & ~7, (vocab - 8) & ~7}) for y in (0, 3, 7)]:
+        b = Batch([3] * 3, vocab, dtype, False, seed=17)
+        b.logits[:] = -np.inf
+        b.logits[:, at:at + 8] = float(np.log(2e-8))
+        b.logits[:, at + top] = 0.0
+        b.temperature.fill_(1.0)
+        b.parents[:], b.ids[:] = [-1, 0, 0] * 3, [0, at + top, at + (top + 1) % 8] * 3
+        b.uniform[:] = torch.tensor([0.0, 1 - 2.0 ** -24, 0.1] * 3, device=DEV)
+        path, kept, following = b.run()
+        assert path[:, :2].tolist() == [[0, 2]] * 3 and kept.tolist() == [2] * 3, (at, top)
