@@ -43,13 +43,17 @@ constexpr int kExcluded = 16;
 constexpr int kMostPolls = 512;
 constexpr size_t kControlBytes = 65536;
 
-// exp(x / T), x <= 0.  The subtraction that gives x, the factor and the product are rounded once each, which moves the exponent y of two by
-// 3 |y| 2^-24 at most; the instruction is off by one unit in the last place.
+// exp(x / T).  The subtraction that gives x, the factor and the product are rounded once each, which moves the exponent y (of e) by 3 |y| 2^-24 at
+// most; the instruction is off by one unit in the last place, 2 2^-24.  A row's exponentials are rescaled on the way to its top, through steps
+// of T or more and three others (the end of the lane's part, the wave, the row), each with an error of that kind; a value may lie T above
+// what it is first taken against.  In all 3 (y + 2) + 2 (y + 1) + 2 (1 + 3) = 5 y + 16 of 2^-24.
 struct Heat {
+    float t;                   // T
     float scale;               // log2(e) / T
     double inv;                // 1 / T
-    __device__ __forceinline__ explicit Heat(float t) {
-        inv = 1.0 / fmin(fmax((double)t, 1e-30), 1e30);     // so that 0 and minus infinity times it are what they are
+    __device__ __forceinline__ explicit Heat(float temperature) {
+        t = (float)fmin(fmax((double)temperature, 1e-30), 1e30);    // so that 0 and minus infinity times 1 / T are what they are
+        inv = 1.0 / (double)t;
         scale = (float)(inv * 1.4426950408889634);
     }
     __device__ __forceinline__ float exp_of(float x) const { return __builtin_amdgcn_exp2f(x * scale); }
@@ -340,14 +344,15 @@ struct Team {
     __device__ __forceinline__ Found scan(const void* row, int o0, int o1, bool tail, bool race, int node, int excludes) {
         Found f = kNothing;
         constexpr int U = 2;                       // octets of a lane at a time; the next ones are in flight
-        // N elements from place `at` on: the largest is known to be no larger than f.top
+        float ref = -__builtin_inff();
+        // N elements from place `at` on, none larger than ref + T
         auto take = [&](int at, const float* x, float* z, auto count_c) __attribute__((always_inline)) {
             constexpr int N = decltype(count_c)::value;
             float p[N];
             double sum[2] = {0.0, 0.0};
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                p[e] = heat.exp_of(x[e] - f.top);
+                p[e] = heat.exp_of(x[e] - ref);
                 sum[e & 1] += (double)p[e];
             }
             f.sum += sum[0] + sum[1];
@@ -370,11 +375,16 @@ struct Team {
                 }
             }
         };
+        // exp((x - ref) / T) is what is added up: ref follows the top when it is left behind by T, and at the end, so that a row that rises all
+        // along is rescaled no more often than its exponent grows.  The best score is rescaled in 64 bits, its roundings do not add up.
+        double best = 0.0;
         auto raise = [&](float top) __attribute__((always_inline)) {
-            const float less = f.top == -__builtin_inff() ? 0.f : heat.exp_of(f.top - top);
+            const double less = ref == -__builtin_inff() ? 0.f : heat.exp_of(ref - top);
+            if ((float)best != f.best) best = (double)f.best;         // another winner since
+            best *= less;
             f.sum *= less;
-            f.best *= less;
-            f.top = top;
+            f.best = (float)best;
+            ref = top;
         };
         float x[U][8], z[U][8], next_x[U][8], next_z[U][8];
         auto load = [&](int o) __attribute__((always_inline)) {
@@ -400,14 +410,15 @@ struct Team {
                 }
             if (o + 64 * U < o1) load(mine + 64 * U);
             if (top > f.top) {
-                raise(top);
+                f.top = top;
                 if (cold) {
 #pragma unroll
                     for (int e = 8 * U - 1; e >= 0; --e)
                         if (x[e / 8][e % 8] == top) f.top_at = 8 * (mine + e / 8 * 64) + e % 8;
                 }
             }
-            if (!cold && f.top > -__builtin_inff()) {
+            if (!cold && top - ref > heat.t) raise(top);
+            if (!cold && ref > -__builtin_inff()) {
 #pragma unroll
                 for (int u = 0; u < U; ++u)
                     if (u == 0 || mine + u * 64 < o1) take(8 * (mine + u * 64), x[u], z[u], std::integral_constant<int, 8>{});
@@ -416,11 +427,13 @@ struct Team {
         if (const int at = 8 * o1 + lane; tail && at < a.vocab) {
             float x[1] = {value_at<TYPE>(row, at)}, z[1] = {race ? noise[at] : 1.f};
             if (x[0] > f.top) {
-                raise(x[0]);
+                f.top = x[0];
                 f.top_at = at;
             }
-            if (!cold && f.top > -__builtin_inff()) take(at, x, z, std::integral_constant<int, 1>{});
+            if (!cold && x[0] - ref > heat.t) raise(x[0]);
+            if (!cold && ref > -__builtin_inff()) take(at, x, z, std::integral_constant<int, 1>{});
         }
+        if (!cold && f.top > ref) raise(f.top);
         return f;
     }
 

@@ -447,3 +447,65 @@ def test_small_values_beside_a_large_one_count(dtype, vocab):
         b.uniform[:] = torch.tensor([0.0, 1 - 2.0 ** -24, 0.1] * 3, device=DEV)
         path, kept, following = b.run()
         assert path[:, :2].tolist() == [[0, 2]] * 3 and kept.tolist() == [2] * 3, (at, top)
+
+
+def promised():
+    """(a, b) of the header's "off by (a + b y) 2^-22" of an exponential exp(-y)."""
+    import os
+    import re
+    text = " ".join(open(os.path.join(os.path.dirname(mx.__file__), "..", "include", "mx.h")).read().split())
+    a, b = re.search(r"exponentials exp\(-y\)[^.]*? off by \((\d+) \+ ([0-9.]* ?)y\) 2\^-22", text).groups()
+    return float(a), float(b or 1)
+
+
+def test_the_promised_error_covers_three_roundings_of_the_exponent():
+    """exp(x / T) as exp2 of a product of fp32 numbers: difference, factor and product are rounded once each, the result once more."""
+    a, b = promised()
+    r, f = np.random.default_rng(18), np.float32
+    for heat in (0.5, 0.7, 0.8, 1.0, 1.3, 2.9):
+        x = (r.standard_normal(400000) * 8).astype(f)
+        top = x.max()
+        got = np.exp2(((x - top) * f(1.4426950408889634 / float(f(heat)))).astype(np.float64)).astype(f)
+        y = (float(top) - x.astype(np.float64)) / float(f(heat))
+        near = y < 80
+        assert (np.abs(got[near] / np.exp(-y[near]) - 1) <= (a + b * y[near]) * 2.0 ** -22).all(), heat
+
+
+def step_that_rounds_badly(heat):
+    """A small step down of the logits whose factor exp(-step / T) fp32 has as badly as it can."""
+    steps = (np.arange(1, 4000) * 2.0 ** -20).astype(np.float32)
+    y = steps * np.float32(1.4426950408889634 / heat)
+    off = np.exp2(-y.astype(np.float64)).astype(np.float32) * np.exp(steps.astype(np.float64) / heat) - 1
+    return float(steps[np.abs(off).argmax()])
+
+
+@gpu
+@pytest.mark.parametrize("requests", [1, 400])
+@pytest.mark.parametrize("kind", ["normal", "rising", "falling", "flat"])
+def test_sums_are_as_near_as_promised(requests, kind):
+    """A row's sum S from outside: a child with the row's first token is accepted at a random number just below e / S and rejected just above, the
+    difference being what the header promises of the exponentials.  Teams, and workgroups alone (400 requests, most of them empty)."""
+    a, b = promised()
+    r, vocab, B = np.random.default_rng(19), 1 << (20 if requests > 1 else 18), 8 if requests > 1 else 1
+    for heat in (0.75, 1.0, 1.5):
+        heat = float(np.float32(heat))
+        step = step_that_rounds_badly(heat)
+        n = np.arange(vocab) // 1024                                         # what a wave reads at once
+        x = {"normal": 3.0 * r.standard_normal(vocab), "rising": n * step, "falling": -n * step, "flat": np.zeros(vocab)}[kind].astype(np.float32)
+        y = (x.max() - x.astype(np.float64)) / heat
+        e = np.exp(-y)
+        off = (e * (a + b * y)).sum() / e.sum() * 2.0 ** -22 + 2.0 ** -40    # (the test itself is in 64 bits)
+        lo, hi = np.float32(e[0] / e.sum() * (1 - off)), np.float32(e[0] / e.sum() * (1 + off))
+        lo = np.nextafter(lo, np.float32(0)) if float(lo) > e[0] / e.sum() * (1 - off) else lo
+        hi = np.nextafter(hi, np.float32(1)) if float(hi) < e[0] / e.sum() * (1 + off) else hi
+        logits = torch.from_numpy(x).to(DEV).expand(2 * B, vocab).contiguous()
+        starts = [min(2 * i, 2 * B) for i in range(requests + 1)]
+        u = [v for i in range(B) for v in (0.0, float(lo if i % 2 == 0 else hi))]
+        path, kept, following = mx.verify(logits, ints([0] * 2 * B), ints([-1, 0] * B), ints(starts),
+                                          torch.full((requests,), heat, device=DEV), torch.tensor(u, device=DEV),
+                                          torch.ones((requests, vocab), device=DEV), 4)
+        assert kept.tolist() == [2 if i % 2 == 0 else 1 for i in range(B)] + [0] * (requests - B), (heat, lo, hi)
+        if requests == 1:
+            path, kept, following = mx.verify(logits, ints([0, 0]), ints([-1, 0]), ints([0, 2]), torch.full((1,), heat, device=DEV),
+                                              torch.tensor([0.0, float(hi)], device=DEV), torch.ones((1, vocab), device=DEV), 4)
+            assert kept.tolist() == [1]
