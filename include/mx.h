@@ -520,14 +520,15 @@ MX_API mx_status mx_cache_tree_attention(const void* q, int32_t type, int64_t to
  * logits, draft: element type `type`, the row of packed token t at t * ldl / t * ldd, `vocab` values, aligned to their elements (rows need not
  * be).  Minus infinity is a token that cannot come; a row of nothing else accepts no child and gives next = -1.  NaN and plus infinity
  * give unspecified tokens (no fault).
- * ids[tokens], parents[tokens], uniform[tokens] (in [0, 1)); noise: a row of `vocab` positive floats for request b at b * ldn.
+ * ids[tokens], parents[tokens], uniform[tokens] (in [0, 1)); noise: a row of `vocab` positive floats for request b at b * ldn
+ * (below 2^-126 they count as 2^-126).
  * path[requests][path_width]: the indices of the accepted nodes, 0 first, then -1; kept[b]: how many, 0 (and next = -1) for a request without
  * new tokens.  The first MX_TREE_MAX_NODES new tokens of a request are its tree.  A token outside [0, vocab) is never accepted.
  * Numerics: exponentials exp(-y) in fp32, off by (4 + 1.25 y) 2^-22 of themselves, sums over a row and the acceptance test in 64 bits.
  * r is off as its exponentials are; after a rejected child of a draft r = p - c q in fp32, either term off by (2 + 0.75 y) 2^-22 of itself
  * beside the error of the sums.  Scores r / noise, in fp32, are off by 2^-21 more, and of tokens whose scores are no further apart than
- * their errors either may come.  Probabilities below 2^-126 of a row's largest may count as 0.  Same inputs, same
- * results.
+ * their errors either may come.  Probabilities, and scores, below 2^-126 of a row's largest probability may count as 0.
+ * Same inputs, same results.
  * workspace: mx_verify_workspace_bytes(...) bytes for the same arguments or larger ones (it grows with each), 256-byte aligned, caller-owned;
  * its first 65536 bytes must be zero before its first use and belong to the calls from then on (they number themselves there), the rest needs
  * no initial value.  One workspace serves call after call of any sizes it is large enough for.  Calls that may overlap in time need a

@@ -86,6 +86,9 @@ __device__ __forceinline__ const void* row_at(const void* base, int64_t element)
     return static_cast<const char*>(base) + element * (TYPE == MX_F32 ? 4 : 2);
 }
 
+// 1 / noise, no more than 2^126, so that no score is infinite: exponentials are no larger than e where they meet it
+__device__ __forceinline__ float inverse_of(float noise) { return __builtin_amdgcn_rcpf(__builtin_amdgcn_fmed3f(noise, 0x1p-126f, 0x1p127f)); }
+
 // All lanes' values as one, in every lane, without LDS: neighbours, quads, rows of sixteen mirrored, then the rows.
 template <int STEP>
 __device__ __forceinline__ void pair_of(uint32_t v, uint32_t& x, uint32_t& y) {
@@ -368,7 +371,7 @@ struct Team {
             }
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const float score = p[e] * __builtin_amdgcn_rcpf(z[e]);
+                const float score = p[e] * inverse_of(z[e]);
                 if (score > f.best) {
                     f.best = score;
                     f.best_at = at + e;
@@ -455,7 +458,7 @@ struct Team {
             for (int e = 0; e < N; ++e) {
                 const float r = __builtin_fmaxf(__builtin_fmaf(heat.exp_of(x[e] - p_top), fp, -(heat.exp_of(y[e] - q_top) * fq)), 0.f);
                 sum[e & 1] += (double)r;
-                const float score = r * __builtin_amdgcn_rcpf(z[e]);
+                const float score = r * inverse_of(z[e]);
                 if (score > f.best) {
                     f.best = score;
                     f.best_at = at + e;

@@ -509,3 +509,32 @@ def test_sums_are_as_near_as_promised(requests, kind):
             path, kept, following = mx.verify(logits, ints([0, 0]), ints([-1, 0]), ints([0, 2]), torch.full((1,), heat, device=DEV),
                                               torch.tensor([0.0, float(hi)], device=DEV), torch.ones((1, vocab), device=DEV), 4)
             assert kept.tolist() == [1]
+
+
+@gpu
+@pytest.mark.parametrize("drawn", [False, True])
+def test_the_smallest_and_largest_noise(drawn):
+    """Any positive float is a random number: below 2^-126 it counts as that, and what it meets in a row stays in the race."""
+    least = 2.0 ** -126
+    r = np.random.default_rng(20)
+    for sizes, width in (([1] * 60, 4), ([6] * 40, 5), ([4] * 30, 1)):
+        b = Batch(sizes, 3001, torch.float32, drawn, seed=len(sizes), width=width)
+        z = b.noise.cpu().numpy().copy()
+        for row in z:
+            at = r.permutation(3001)
+            row[at[:200]] = np.float32(1e-45) * r.integers(1, 8000000, 200)                # subnormal
+            row[at[200:400]] = 3e38
+            row[at[400:410]] = np.float32(least)
+        b.noise = torch.from_numpy(z).to(DEV)
+        got = b.run()
+        b.noise = torch.from_numpy(np.maximum(z, np.float32(least))).to(DEV)
+        b.check(got)
+    # a small token with a subnormal number, a large one that the same lane comes to later; two subnormal numbers
+    b = Batch([1] * 4, 5000, torch.float32, drawn, seed=21)
+    b.logits[:] = -1000.0
+    b.logits[:, 3], b.logits[:, 4099], b.logits[2:, 7] = 0.0, 500.0, 499.0
+    b.temperature.fill_(1.0)
+    b.noise[:] = 1.0
+    b.noise[:, 3], b.noise[2:, 7] = 1e-40, 1e-45
+    b.noise[3, 4099] = 1e-41
+    assert b.run()[2].tolist() == [4099, 4099, 7, 4099]
