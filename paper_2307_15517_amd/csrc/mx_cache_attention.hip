@@ -251,6 +251,7 @@ constexpr int kQueryPieces = TYPE == MX_F32 ? 3 : 1;
 // from the level that all compute units share (device scope), so that no cache has to be written back or invalidated as a whole.
 constexpr int kDeviceScope = 0x10;
 constexpr int kMaxSplits = 64;
+constexpr int kFewRows = 16;           // (token, head of a group) of a request that decode() takes at once
 
 // The parts of `rows` rows (16 or, with 32 lanes a row, eight at a time), `splits` each, of a unit whose workgroups have all
 // stored theirs: o = sum_s o_s 2^(m_s - m) / sum_s l_s 2^(m_s - m).  Called by the 256 threads of the workgroup that came last; the
@@ -1099,8 +1100,11 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
 // 128 rows: chunk_tile()'s, without a causal order, or a small tile of up to 32 rows, 64 in bfloat16 calls on an MXInt cache, where a
 // large one would convert each key for half as many rows.  A small tile's four waves take blocks of 32 keys in turn, as in decode(), and
 // join at the end: K and V go from memory to registers once for all rows, R groups of sixteen, an MXInt block is converted once
-// for them, and q, which all waves use, lies in LDS as the matrix instructions read it.  A block's K registers are free for the next
-// block's loads when its scores are there, V's after P V, so both are in flight during the rest.
+// for them, and q, which all waves use, lies in LDS as the matrix instructions read it.  bfloat16 calls have two pieces of P, as
+// chunk_tile() has, but three in tiles of up to sixteen rows (R = 1), as decode() has: a request's results are as exact beside larger
+// ones as alone (24 requests of 16 rows beside one of 64, 2000 keys of an MXInt cache: 39.5 us, 41.2 as R = 2 with two pieces).  A
+// block's K registers are free for the next block's loads when its scores are there, V's after P V, so both are in flight during
+// the rest.
 // Bound by the issue of vector arithmetic (softmax, pieces of P, MXInt) and of matrix instructions, which two waves a SIMD overlap little:
 // 24 requests of 320 to 504 rows, 8 heads, 128 elements, MXInt 32: 368 us, clock 2.1 GHz, matrix cores 0.29 and vector units 0.48 of
 // the time.  Eight requests of 36 / 52 / 64 rows on 500 to 4000 keys, 8 heads: MXInt as small tiles 31.6 / 33.0 / 33.7 us, as large ones
@@ -1334,7 +1338,7 @@ template <int TYPE, int DT, int BLOCK, int R>
 __device__ __forceinline__ void tree_tile(const CacheAttnArgs& a, const Tile& tile, int h, int split, int splits, int begin, int end, uint8_t* smem) {
     constexpr int NS = DT / 32, NJ = DT / 16, VE = DT / 16;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
-    constexpr int QP = kQueryPieces<TYPE>, P = TYPE == MX_F32 ? 3 : 2;
+    constexpr int QP = kQueryPieces<TYPE>, P = TYPE == MX_F32 || R == 1 ? 3 : 2;     // (up to sixteen rows: all bits of P, as in decode())
     using Block = KeyBlock<DT, BLOCK>;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int n = lane & 15, g = lane >> 4;
@@ -1600,9 +1604,11 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_tree_kernel
         const int r0 = i.tile.index * kTileRows, rows = min(rq.n * a.group - r0, kTileRows), len = rq.len;
         const int per = ((len + kTileKeys - 1) / kTileKeys + i.splits - 1) / i.splits * kTileKeys;
         const int begin = min(i.split * per, len), end = min(begin + per, len);
-        if (!i.small) chunk_tile<TYPE, DT, BLOCK, DC>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
+        // (in this order; with tiles of 32 rows, the most frequent ones, last these take 2 % longer)
+        if (i.small && rows <= 32 && (TYPE == MX_F32 || rows > kFewRows)) tree_tile<TYPE, DT, BLOCK, 2>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
+        else if (!i.small) chunk_tile<TYPE, DT, BLOCK, DC>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
         else if (G == 4 && rows > 32) tree_tile<TYPE, DT, BLOCK, G>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
-        else tree_tile<TYPE, DT, BLOCK, 2>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
+        else if constexpr (TYPE == MX_BF16) tree_tile<TYPE, DT, BLOCK, 1>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
         if (i.splits > 1 && a.join && came_last(a.counters + i.unit, i.splits, reinterpret_cast<uint32_t*>(smem)))
             for (int r = 0; r < rows; r += 64) join_tile<TYPE, 8, 2, kDeviceScope>(a, rq, i.h, r0 + r, min(64, rows - r), i.splits);
     }
@@ -1823,8 +1829,6 @@ __global__ __launch_bounds__(256) void cache_zero_kernel(CacheAttnArgs a) {
 // have more rows by them, cache_decode_kernel takes all (any number of rows is right there, sixteen at a time), else
 // cache_mixed_kernel has workgroups of both, each of which leaves the other's requests alone; a single request needs those of
 // the one or the other only.  (24 mixed requests, with one half-precision piece of a probability: 66 us in one launch, 80 in two.)
-constexpr int kFewRows = 16;
-
 struct Plan {
     bool decode, chunk;
     int part_rows, splits;         // of cache_decode_kernel

@@ -440,3 +440,64 @@ def test_move_of_anything_stays_in_the_pool():
     torch.cuda.synchronize()
     for t, g in zip((cache.k, cache.v, cache.k_exps, cache.v_exps), guard):
         assert torch.equal(t, g)                             # (zeros over zeros)
+
+
+# ---- precision ----------------------------------------------------------------------------------------------
+def probabilities_in_three_pieces():
+    """Scores s, multiples of 2^-7, whose probability p = exp(s) against a maximum of 1 two bfloat16 numbers miss by 2^-19.5 or more."""
+    s = -np.arange(3, 88) / 128.0
+    p = np.exp(s)
+    near = lambda v: torch.from_numpy(v).to(torch.bfloat16).double().numpy()  # noqa: E731
+    rest = p - near(p)
+    return s[np.abs(rest - near(rest)) >= 2.0 ** -19.5]
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bf16", "mx16", "mx32"])
+@pytest.mark.parametrize("dim,group,big", [(64, 1, 40), (128, 2, 17), (96, 4, 130), (128, 1, 0), (64, 3, 300)])
+def test_attention_of_few_rows_keeps_all_bits_of_the_probabilities(kind, dim, group, big):
+    """bfloat16 requests of up to sixteen rows, next to a request of many or none.  Row j sees three keys with scores 0, 0, s_j and values -h, -m, 1 in
+    element j, h and m being seven bits of p each, so that p - h - m is what is left: (2 + p) times the result.  fp32 has it within 2^-21: p is
+    off by 2.4 2^-24 (two roundings of an exponent up to 1, one of the instruction), the sum of numbers up to 1 by 2^-24 for
+    each of four terms.  Two bfloat16 pieces of p would leave 2^-19.5 or more."""
+    s = probabilities_in_three_pieces()
+    assert len(s) >= 16
+    sizes = ([big] if big else []) + [16 // group, 1, 2]
+    picks = [np.roll(s, 5 * b) for b in range(len(sizes))]
+    r = np.random.default_rng(41)
+    cache = mx.Cache(64, 16, 1, dim, FORMATS[kind], DEV)
+    table = torch.full((len(sizes), 24), -1, dtype=torch.int32, device=DEV)
+    free = torch.arange(64, dtype=torch.int32, device=DEV)
+    B = len(sizes)
+    # the three cached keys of each, then the new tokens
+    k, v = np.zeros((3 * B, dim)), np.zeros((3 * B, dim))
+    for b in range(B):
+        j = np.arange(min(16, len(s)))
+        p = np.exp(picks[b][j])
+        h = np.round(p * 128) / 128
+        m = np.round((p - h) * 2.0 ** 15) / 2.0 ** 15
+        k[3 * b + 2, j], v[3 * b, j], v[3 * b + 1, j], v[3 * b + 2, j] = picks[b][j], -h, -m, 1.0
+    up = lambda x: torch.from_numpy(np.asarray(x, np.float32)).to(DEV)  # noqa: E731
+    q_start, kv_len, slots, _, _ = mx.cache_plan(ints([0] * B), ints([3] * B), 16, free, table, 3 * B)
+    mx.cache_append(cache, up(k), up(v), slots)
+    T = sum(sizes)
+    used = int((table >= 0).sum())
+    q_start, kv_len, slots, _, counts = mx.cache_plan(ints([3] * B), ints(sizes), 16, free[used:].contiguous(), table, T)
+    assert counts.tolist()[1] == 0
+    mx.cache_append(cache, up(r.standard_normal((T, dim))), up(r.standard_normal((T, dim))), slots)
+    q = np.zeros((T, group, dim))
+    starts = np.concatenate([[0], np.cumsum(sizes)])
+    for b, n in enumerate(sizes):
+        for row in range(n * group):
+            q[starts[b] + row // group, row % group, row % 16] = 1.0
+    o = mx.cache_tree_attention(cache, up(q.reshape(T, -1)).to(torch.bfloat16), table, q_start, kv_len,
+                                torch.zeros((T, 1), dtype=torch.int64, device=DEV), max(sizes), 400, 1.0)
+    o = o.double().cpu().numpy().reshape(T, group, dim)
+    for b, n in enumerate(sizes):
+        if n * group > 16:
+            continue
+        for row in range(n * group):
+            p = np.exp(picks[b][row])
+            left = p + v[3 * b, row] + v[3 * b + 1, row]
+            got = (2.0 + p) * o[starts[b] + row // group, row % group, row]
+            assert abs(got - left) <= 2.0 ** -21, (b, row, got, left)
