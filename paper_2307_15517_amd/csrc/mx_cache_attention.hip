@@ -1808,8 +1808,14 @@ __global__ __launch_bounds__(256) void cache_join_tiles_kernel(CacheAttnArgs a) 
 
 template <int TYPE, bool CHUNK>
 mx_status launch_join(const CacheAttnArgs& a, int64_t rows, hipStream_t stream) {
-    if (CHUNK && a.splits <= 16) cache_join_tiles_kernel<TYPE><<<(unsigned)(rows / 32), 256, 0, stream>>>(a);
-    else cache_join_kernel<TYPE, CHUNK><<<(unsigned)rows, 256, 0, stream>>>(a);
+    if constexpr (CHUNK) {
+        if (a.splits <= 16) {
+            cache_join_tiles_kernel<TYPE><<<(unsigned)(rows / 32), 256, 0, stream>>>(a);
+            MX_HIP_LAUNCH_CHECK();
+            return MX_OK;
+        }
+    }
+    cache_join_kernel<TYPE, CHUNK><<<(unsigned)rows, 256, 0, stream>>>(a);
     MX_HIP_LAUNCH_CHECK();
     return MX_OK;
 }
@@ -1947,7 +1953,7 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
     CacheAttnArgs few = base, many = base;
     uint8_t* parts = workspace + kCounterBytes;
     const int64_t units = (int64_t)base.requests * base.heads;
-    int64_t few_rows = 0, many_rows = 0;
+    int64_t few_rows = 0;
     if (p.decode) {
         few.least = 1;
         few.most = p.chunk ? kFewRows : INT32_MAX;
@@ -1967,7 +1973,6 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         many.splits = p.chunk_splits;
         many.run = p.run;
         many.tiles = p.tiles;
-        many_rows = (int64_t)p.tiles * base.heads * kTileRows;
         many.part_o = (float*)parts;
         many.part_ml = (float2*)(many.part_o + base.tokens * base.heads_q * p.chunk_splits * base.dim);
 #if MX_CACHE_TREE
@@ -2007,7 +2012,11 @@ mx_status launch_kernels(const CacheAttnArgs& base, const Plan& p, uint8_t* work
         const mx_status st = launch_join<TYPE, false>(few, few_rows, stream);
         if (st != MX_OK) return st;
     }
-    return p.chunk && p.chunk_splits > 1 ? launch_join<TYPE, true>(many, many_rows, stream) : MX_OK;
+#if MX_CACHE_TREE
+    return MX_OK;
+#else
+    return p.chunk && p.chunk_splits > 1 ? launch_join<TYPE, true>(many, (int64_t)p.tiles * base.heads * kTileRows, stream) : MX_OK;
+#endif
 }
 
 template <int TYPE, int DT, int DC>

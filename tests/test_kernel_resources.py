@@ -110,3 +110,28 @@ def test_verification_and_the_joins_of_trees_stay_in_registers(kernel_notes):
     for name, kernels, waves in ((r"\bverify_kernel<\d>", 2, 3), (r"\bcache_tree_join_kernel<\d>", 2, 6)):
         found = [v for n, v in kernel_notes.items() if re.search(name, n)]
         assert len(found) == kernels and all(scratch == 0 and waves_per_simd(vgprs) >= waves for scratch, vgprs in found), (name, found)
+
+
+def kernels_by_unit():
+    """Names of the kernels of every code object of the library, one set a translation unit."""
+    data = open(mx.LIB_PATH, "rb").read()
+    at, units = data.find(b"__CLANG_OFFLOAD_BUNDLE__"), []
+    while at >= 0:
+        entry = at + 32
+        for _ in range(struct.unpack_from("<Q", data, at + 24)[0]):
+            offset, size, length = struct.unpack_from("<QQQ", data, entry)
+            target = data[entry + 24:entry + 24 + length].decode()
+            entry += 24 + length
+            if "gfx950" in target and size:
+                units.append(set(re.findall(rb"_ZN2mx[A-Za-z0-9_]*kernel[A-Za-z0-9_]*\.kd", data[at + offset:at + offset + size])))
+        at = data.find(b"__CLANG_OFFLOAD_BUNDLE__", at + 24)
+    return units
+
+
+def test_the_unit_of_trees_holds_what_it_launches(kernel_notes):
+    """Attention of trees joins the parts of its tiles by itself: no joins of chunks, which go by the causal order, beside it."""
+    trees = [u for u in kernels_by_unit() if any(b"cache_tree_kernel" in n for n in u)]
+    assert len(trees) == 1
+    kinds = {re.search(rb"\d+(cache_\w+?_kernel)(?:I|E)", n).group(1) for n in trees[0]}
+    assert kinds == {b"cache_tree_kernel", b"cache_tree_join_kernel", b"cache_decode_kernel", b"cache_join_kernel", b"cache_zero_kernel"}, kinds
+    assert len([n for n in trees[0] if b"cache_join_kernel" in n]) == 2      # of the parts of few rows, fp32 and bfloat16
