@@ -19,6 +19,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmx.so")
 PROBES_SRC = os.path.join(CSRC, "probes", "mx_probes.hip")
 PROBES_LIB = os.path.join(HERE, "libmx_probes.so")      # roofline probes of the benchmark, not part of libmx
+EARLY_LIB = os.path.join(HERE, "libmx_verify_early.so")  # verification whose members can be told not to wait, for a test
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -59,6 +60,17 @@ def _compile(unit: List[str]) -> str:
     return out
 
 
+def _link_alone(src: str, lib: str, verbose: bool, *extra: str) -> None:
+    """A library of one source."""
+    tmp = lib + ".tmp.%d" % os.getpid()
+    p = subprocess.run([HIPCC] + FLAGS + list(extra) + ["-shared", src, "-o", tmp], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if p.returncode != 0:
+        raise RuntimeError("hipcc failed for %s:\n%s" % (src, p.stdout))
+    os.replace(tmp, lib)
+    if verbose:
+        print("linked", os.path.relpath(lib, ROOT), flush=True)
+
+
 def build(verbose: bool = True, jobs: int = 8) -> str:
     os.makedirs(OBJ, exist_ok=True)
     units = translation_units()
@@ -74,14 +86,8 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
     os.replace(tmp, LIB)
     if verbose:
         print("linked", os.path.relpath(LIB, ROOT), flush=True)
-    tmp = PROBES_LIB + ".tmp.%d" % os.getpid()
-    p = subprocess.run([HIPCC] + FLAGS + ["-shared", PROBES_SRC, "-o", tmp], stdout=subprocess.PIPE,
-                       stderr=subprocess.STDOUT, text=True)
-    if p.returncode != 0:
-        raise RuntimeError("hipcc failed for %s:\n%s" % (PROBES_SRC, p.stdout))
-    os.replace(tmp, PROBES_LIB)
-    if verbose:
-        print("linked", os.path.relpath(PROBES_LIB, ROOT), flush=True)
+    _link_alone(PROBES_SRC, PROBES_LIB, verbose)
+    _link_alone(os.path.join(CSRC, "mx_verify.hip"), EARLY_LIB, verbose, "-DMX_VERIFY_EARLY=1")
     return LIB
 
 

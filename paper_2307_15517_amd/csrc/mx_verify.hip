@@ -1,4 +1,5 @@
-// Verification of drafted tokens against the model's logits, from given random numbers.
+// Verification of drafted tokens against the model's logits, from given random numbers.  (Compiled with MX_VERIFY_EARLY=1 for a test: the
+// workspace says who does not wait for whom.)
 #include <type_traits>
 
 #include "mx_cache.h"
@@ -168,7 +169,9 @@ struct Job {
 // has read it puts the next one there.
 struct Control {
     uint64_t number;
-    uint32_t teams, unused;             // teams of this call whose members have all read the number
+    uint32_t teams;                     // of this call, whose members have all read the number
+    uint32_t early;                     // with MX_VERIFY_EARLY: from job number early & 0xffff on members do not look out for others, those
+                                        // of odd numbers only with 1 << 16; 0: they do
     uint32_t members[kMostTeams];       // of a team
     uint64_t posted[kMostMembers];      // number << 16 | jobs done, of every member
 };
@@ -702,7 +705,12 @@ __global__ __launch_bounds__(kThreads, 3) void verify_kernel(VerifyArgs a) {
             if (tid == 0) put(posted + team.member, want);
             if (wave == 0) {
                 bool here = false;
-                for (int polls = 0; !here && polls < kMostPolls; ++polls)
+                int polls = 0;
+#if MX_VERIFY_EARLY
+                const uint32_t early = __hip_atomic_load(&a.control->early, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (early != 0 && jobs >= (early & 0xffff) && (team.member & 1) >= (int)(early >> 16)) polls = kMostPolls;
+#endif
+                for (; !here && polls < kMostPolls; ++polls)
                     here = __ballot(lane < a.team && get(posted + min(lane, a.team - 1)) < want) == 0;
                 if (lane == 0) s.all_here = here;
             } else if (wave == 3 && jobs == 1) {

@@ -1,9 +1,11 @@
 """Verification of drafted tokens: the walk against a plain implementation in 64 bits, and what it draws against the distribution."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
-from paper_2307_15517_amd import mx
+from paper_2307_15517_amd import build, mx
 from test_cache import DEV, ints
 
 gpu = pytest.mark.gpu
@@ -538,3 +540,51 @@ def test_the_smallest_and_largest_noise(drawn):
     b.noise[:, 3], b.noise[2:, 7] = 1e-40, 1e-45
     b.noise[3, 4099] = 1e-41
     assert b.run()[2].tolist() == [4099, 4099, 7, 4099]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("drawn,greedy", [(False, 0.0), (True, 0.0), (False, 1.0), (True, 0.3)])
+def test_members_that_do_not_wait_find_the_same(dtype, drawn, greedy, monkeypatch):
+    """A member of a team that does not see the others goes on alone, at any job, all of them or some, with the same bits, and the workspace
+    serves on.  Of the library whose members can be told so by the fourth word of the workspace, against libmx."""
+    early = ctypes.CDLL(build.EARLY_LIB)
+    early.mx_verify.argtypes, early.mx_verify.restype = mx.load().mx_verify.argtypes, ctypes.c_int32
+
+    class Libraries:
+        mx_verify = early.mx_verify
+
+        def __getattr__(self, name):
+            return getattr(libmx, name)
+    libmx, both = mx.load(), Libraries()
+    for sizes, vocab, branch in (([5], 32000, 1), ([6] * 24, 50272, 1), ([40] * 8, 9001, 3), ([20, 3, 0, 61], 30000, 6), ([130], 2000, 4)):
+        b = Batch(sizes, vocab, dtype, drawn, seed=50 + len(sizes), branch=branch, greedy=greedy)
+        ws = mx.verify_workspace(len(b.ids), len(sizes), vocab, DEV)
+        first = b.check(b.run(ws))
+        monkeypatch.setattr(mx, "_lib", both)
+        for odd in (0, 1 << 16):
+            for job in (1, 2, 3, 5):
+                ws[:16].view(torch.int32)[3] = odd | job
+                again = b.run(ws)
+                assert all(torch.equal(x, y) for x, y in zip(first, again)), (sizes, odd, job)
+                if (odd, job) == (0, 1):                       # all left after the first job: nobody said anything of a second
+                    posted = ws[2064:2064 + 8 * 1024].view(torch.int64)
+                    posted = posted[posted > 0]
+                    assert len(posted) > 1 and bool((posted == (1 << 16 | 1)).logical_or(posted >> 16 == 0).all())
+        ws[:16].view(torch.int32)[3] = 0
+        assert all(torch.equal(x, y) for x, y in zip(first, b.run(ws)))
+        monkeypatch.undo()
+        calls = ws[:8].view(torch.int64).item()
+        assert calls == 10                                     # teams worked: every call has numbered itself
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("drawn", [False, True])
+def test_many_requests_read_their_rows_alone(dtype, drawn):
+    """More requests than teams of two: a workgroup each, which reads a row in several segments of its own."""
+    for sizes, vocab in (([3] * 600, 2000), ([1, 0, 7, 2] * 100, 5001), ([20, 4] * 260, 1003)):
+        b = Batch(sizes, vocab, dtype, drawn, seed=len(sizes), greedy=0.2)
+        ws = mx.verify_workspace(len(b.ids), len(sizes), vocab, DEV)
+        b.check(b.run(ws))
+        assert not ws[:65536].any()                            # no teams
