@@ -205,3 +205,25 @@ def test_a_step_against_plain_ones(draft):
                 for w, row in zip(new, rows):
                     assert torch.equal(w[table[b, (ctx + k) // 16], :, (ctx + k) % 16], row[ctx + node])
             t0 += n
+
+
+@gpu
+@pytest.mark.parametrize("draft", [False, True])
+def test_the_walks_of_steps_are_decided_and_right(draft):
+    """Paths, their lengths, the rest of their rows and the tokens after them against 64 bits, in steps whose decisions stand clear of their borders."""
+    x, unsure, steps = Loop(None, torch.float32, B=5, nodes=16, vocab=300, draft=draft), 0, 12
+    for seed in range(steps):
+        sizes, parents = x.fill(60 + seed, 16 * (seed % 4))
+        _, _, _, path, kept, following = (t.cpu() for t in x.step())
+        t0 = 0
+        for b, n in enumerate(sizes):
+            rng = slice(t0, t0 + n)
+            want, token, sure = walk(x.logits[rng].double().cpu().numpy(), None if x.draft is None else x.draft[rng].double().cpu().numpy(),
+                                     x.ids[rng].tolist(), parents[rng], 1.0, x.uniform[rng].double().cpu().numpy(),
+                                     x.noise[b].double().cpu().numpy(), 6)
+            t0 += n
+            if not sure:
+                unsure += 1
+                continue
+            assert int(kept[b]) == len(want) and path[b].tolist() == want + [-1] * (6 - len(want)) and int(following[b]) == token
+    assert unsure <= 2, unsure                                   # of 60 walks
