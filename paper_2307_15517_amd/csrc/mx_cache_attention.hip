@@ -1106,8 +1106,8 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
 // block's K registers are free for the next block's loads when its scores are there, V's after P V, so both are in flight during
 // the rest.
 // Bound by the issue of vector arithmetic (softmax, pieces of P, MXInt) and of matrix instructions, which two waves a SIMD overlap little:
-// 24 requests of 320 to 504 rows, 8 heads, 128 elements, MXInt 32: 368 us, clock 2.1 GHz, matrix cores 0.29 and vector units 0.48 of
-// the time.  Eight requests of 36 / 52 / 64 rows on 500 to 4000 keys, 8 heads: MXInt as small tiles 31.6 / 33.0 / 33.7 us, as large ones
+// 24 requests of 320 to 504 rows, 8 heads, 128 elements, MXInt 32: 368 to 388 us, clock 2.1 GHz, matrix cores 0.30 and vector units 0.49
+// of the time (heads over 64 with an MXInt cache: 256 registers and 28 bytes spilled, addresses that the copies of a stage read back).  Eight requests of 36 / 52 / 64 rows on 500 to 4000 keys, 8 heads: MXInt as small tiles 31.6 / 33.0 / 33.7 us, as large ones
 // 33.3 / 34.4 / 35.3; a bfloat16 cache as small ones 34.0 / 35.8 / 37.0, as large ones 32.7 / 33.6 / 34.8, but of 20 rows 25.9 and 31.0.
 template <int TYPE, int BLOCK>
 constexpr int kTreeGroups = TYPE == MX_F32 || BLOCK == 0 ? 2 : 4;
@@ -1115,7 +1115,8 @@ constexpr int kTreeGroups = TYPE == MX_F32 || BLOCK == 0 ? 2 : 4;
 // How a batch is shared out.  A unit is a tile of a request's rows and a key/value head; its keys are cut into runs of as few blocks of 64 as
 // leave no more items (a unit's runs) than workgroups.  A block of a large tile takes longer (3.6 us with an MXInt cache, 2.5 with
 // bfloat16; of a small one of 64 rows 2.3, of 32 1.6), so small tiles have longer runs.  All know all lengths: there are no items
-// without work.  Every wave works it out for itself, a request a lane, 64 at a time (2 to 3 us with the loads of the lengths).
+// without work.  Every wave works it out for itself, a request a lane, 64 at a time (2 to 3 us with the loads of the lengths for up to 64
+// requests; of more each pass loads them again: 128, 256, 512 of 20 rows on 20 keys take 18, 38, 82 us in all).
 struct TreeItem {
     Tile tile;                 // b < 0: nothing; index: of kTileRows rows
     bool small;                // no more than a.small_rows of them

@@ -641,7 +641,7 @@ struct Team {
 // the latency of a job: 2.5 to 5 us of reading, 2 to 4 until all members' parts are seen, 1 to fetch them, 2 to decide.  With the call, a
 // chain of five over 32000 tokens / 24 chains with their drafts over 50272 / those trees / six trees drawn from bfloat16 drafts, 100003: a
 // workgroup a request 27 / 156 / 250 / 184 us; teams 13 / 33 / 45 / 52; segments over all waves of a team 13 / 28 / 36 / 47; a lane a child
-// 11 / 26 / 33 / 45.  The rows of the first two children are read with a node's (36 us for the trees; 44 with four or with none), those
+// 11 / 26 / 33 / 45; sums in 64 bits 11 / 27 / 34 / 46.  The rows of the first two children are read with a node's (36 us for the trees; 44 with four or with none), those
 // of all nodes where a tree has eight on average or fewer.
 // A team of workgroups a request.  A job's rows are read in segments, each by a wave of its own; members hand in what their segments gave,
 // look out for the others' a bounded number of times, join all parts in the order of the segments and decide, every one for itself

@@ -135,3 +135,18 @@ def test_the_unit_of_trees_holds_what_it_launches(kernel_notes):
     kinds = {re.search(rb"\d+(cache_\w+?_kernel)(?:I|E)", n).group(1) for n in trees[0]}
     assert kinds == {b"cache_tree_kernel", b"cache_tree_join_kernel", b"cache_decode_kernel", b"cache_join_kernel", b"cache_zero_kernel"}, kinds
     assert len([n for n in trees[0] if b"cache_join_kernel" in n]) == 2      # of the parts of few rows, fp32 and bfloat16
+
+
+def test_attention_of_trees_spills_no_more_than_addresses(kernel_notes):
+    """Two workgroups a compute unit in bfloat16 calls, one in fp32 ones.  With an MXInt cache and heads over 64 the large tile keeps up to seven
+    registers of addresses in memory, which the copies of a stage of 64 keys read back; nothing else does."""
+    seen = 0
+    for name, (scratch, vgprs) in kernel_notes.items():
+        m = re.search(r"\bcache_tree_kernel<(\d), (\d+), (\d+), (\d+)>", name)
+        if not m:
+            continue
+        type_, heads, block, _ = (int(v) for v in m.groups())
+        most = 28 if (type_, heads) == (mx.MX_BF16, 128) and block else 0
+        assert scratch <= most and waves_per_simd(vgprs) >= (2 if type_ == mx.MX_BF16 else 1), (name, scratch, vgprs)
+        seen += 1
+    assert seen == 2 * 3 * 3
