@@ -50,10 +50,12 @@ struct CacheAttnArgs {
     int32_t vec_q, vec_o;      // rows of q / out allow 16-byte (bfloat16 out: 8-byte) accesses
     float c;                   // |scale| * log2(e)
     uint32_t flip;             // sign bit of the scale: carried by q
-    const uint32_t* masks;     // kTree: [tokens][mask_words], bit j: new token j of the request is seen
+#if MX_CACHE_TREE                // (the causal kernels take two of these: with more fields scalar registers spill, 3 to 8 % of chunks over MXInt)
+    const uint32_t* masks;     // [tokens][mask_words], bit j: new token j of the request is seen
     int32_t mask_words;        // 32-bit words of a token's mask
     int32_t slots;             // cache_tree_kernel: its workgroups; tiles: units, at most
     int32_t small_rows, small_run, least_run;   // rows that a small tile may have; its runs in eighths of a large one's, and of one of 32 rows
+#endif
 };
 
 // One request as a workgroup sees it, every length bounded by what the arrays hold.
@@ -70,6 +72,7 @@ __device__ __forceinline__ Request request_of(const CacheAttnArgs& a, int b) {
     return r;
 }
 
+#if MX_CACHE_TREE
 // Which of 32 keys from new token `at` on (negative: cached ones) packed token `t` sees, a bit each.
 __device__ __forceinline__ uint32_t seen_from(const CacheAttnArgs& a, int64_t t, int at) {
     const uint32_t* mask = a.masks + t * a.mask_words;
@@ -77,6 +80,9 @@ __device__ __forceinline__ uint32_t seen_from(const CacheAttnArgs& a, int64_t t,
     const uint32_t lo = mask[min(max(w, 0), a.mask_words - 1)], hi = mask[min(max(w + 1, 0), a.mask_words - 1)];
     return __builtin_amdgcn_alignbit(w + 1 < 0 ? ~0u : w + 1 < a.mask_words ? hi : 0u, w < 0 ? ~0u : w < a.mask_words ? lo : 0u, at & 31);
 }
+#else
+__device__ __forceinline__ uint32_t seen_from(const CacheAttnArgs&, int64_t, int) { return ~0u; }
+#endif
 
 // Zeros for the tokens before the first request's and after the last one's.
 template <int TYPE>
@@ -730,9 +736,13 @@ __device__ __forceinline__ void pin(uint32_t x) { asm volatile("" ::"v"(x)); }
 // a register of its own, one for every place in every stage.
 __device__ __forceinline__ void opaque(uint32_t& x) { asm("" : "+v"(x)); }
 
-// The arithmetic of one item: row tile `tile` for head h, keys begin .. stop, which are run `split` of `splits`.
+// The arithmetic of one item: row tile `tile` for head h, run number `split` of its keys.  The causal unit finds that run while the first pages
+// are on their way (found before, fp32 chunks take 1 % longer); of trees it is `run`.
+struct Run {
+    int splits, begin, end;
+};
 template <int TYPE, int DT, int BLOCK, int DC>
-__device__ __forceinline__ void chunk_tile(const CacheAttnArgs& a, const Tile& tile, int h, int split, int splits, int begin, int stop, uint8_t* smem) {
+__device__ __forceinline__ void chunk_tile(const CacheAttnArgs& a, const Tile& tile, int h, int split, Run run, uint8_t* smem) {
     constexpr int QP = kQueryPieces<TYPE>, P = TYPE == MX_F32 ? 3 : 2;
     constexpr int NK = DC / 16, ND = DC / 32;
     constexpr int EB = BLOCK == 0 ? 2 : 1;
@@ -747,6 +757,15 @@ __device__ __forceinline__ void chunk_tile(const CacheAttnArgs& a, const Tile& t
     const Request rq = tile.rq;
     const int rows = rq.n * a.group, r0 = tile.index * kTileRows;
     const int len = rq.len, dim = a.dim;
+#if MX_CACHE_TREE
+    const int splits = run.splits, begin = run.begin, stop = run.end;
+#else
+    // the keys that some row of the tile sees, and this split's run of them in whole tiles
+    const int all = keys_seen(a, tile), splits = splits_of(a, all);
+    if (split >= splits) return;
+    const int per = (((all + kTileKeys - 1) / kTileKeys) + splits - 1) / splits * kTileKeys;
+    const int begin = min(split * per, all), stop = min(begin + per, all);
+#endif
 
     // this wave's rows: q is the right operand of the scores, lane (i, h2) row i, elements 16kk + 8h2 ..
     const int r = min(r0 + 32 * wave + i, rows - 1);
@@ -1087,12 +1106,7 @@ __device__ __forceinline__ void chunk(const CacheAttnArgs& a, int index, uint8_t
     const int split = rest % a.splits, tile_id = a.tiles - 1 - rest / a.splits;
     const Tile tile = find_tile(a, tile_id);
     if (tile.b < 0) return;
-    // the keys that some row of the tile sees, and this split's run of them in whole tiles
-    const int all = keys_seen(a, tile), splits = splits_of(a, all);
-    if (split >= splits) return;
-    const int per = (((all + kTileKeys - 1) / kTileKeys) + splits - 1) / splits * kTileKeys;
-    const int begin = min(split * per, all);
-    chunk_tile<TYPE, DT, BLOCK, DC>(a, tile, h, split, splits, begin, min(begin + per, all), smem);
+    chunk_tile<TYPE, DT, BLOCK, DC>(a, tile, h, split, Run{}, smem);
 }
 #else
 // ---- trees of more than sixteen rows --------------------------------------------------------------------
@@ -1607,7 +1621,7 @@ __global__ __launch_bounds__(256, TYPE == MX_F32 ? 1 : 2) void cache_tree_kernel
         const int begin = min(i.split * per, len), end = min(begin + per, len);
         // (in this order; with tiles of 32 rows, the most frequent ones, last these take 2 % longer)
         if (i.small && rows <= 32 && (TYPE == MX_F32 || rows > kFewRows)) tree_tile<TYPE, DT, BLOCK, 2>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
-        else if (!i.small) chunk_tile<TYPE, DT, BLOCK, DC>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
+        else if (!i.small) chunk_tile<TYPE, DT, BLOCK, DC>(a, i.tile, i.h, i.split, Run{i.splits, begin, end}, smem);
         else if (G == 4 && rows > 32) tree_tile<TYPE, DT, BLOCK, G>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
         else if constexpr (TYPE == MX_BF16) tree_tile<TYPE, DT, BLOCK, 1>(a, i.tile, i.h, i.split, i.splits, begin, end, smem);
         if (i.splits > 1 && a.join && came_last(a.counters + i.unit, i.splits, reinterpret_cast<uint32_t*>(smem)))
@@ -2098,8 +2112,10 @@ mx_status attend(const void* q, int32_t type, int64_t tokens, int64_t ldq, int32
     a.vec_o = aligned(out, 4 * tb) && ldo % 4 == 0;
     a.c = __builtin_fmaxf(__builtin_fabsf(scale) * 1.4426950408889634f, 0x1p-126f);   // never 0: minus infinity stays a mask
     a.flip = scale < 0.f ? 0x80000000u : 0u;
+#if MX_CACHE_TREE
     a.masks = (const uint32_t*)masks;
     a.mask_words = 2 * words;
+#endif
     uint8_t* ws = (uint8_t*)workspace;
     return type == MX_F32 ? launch<MX_F32>(a, p, c.f.block, ws, (hipStream_t)stream) : launch<MX_BF16>(a, p, c.f.block, ws, (hipStream_t)stream);
 }
